@@ -381,6 +381,111 @@ int rq_gbs_search_asym(const rq_hadamard_t* h, const void* X, int dtype, int64_t
                        float* trace_mse, int* n_evals);
 
 /*
+ * The 4-bit paged key / value cache: where the keys and values of a served model go once they are rotated and quantized
+ * (section 5.1: asymmetric, a group a head row), and attention that reads them.
+ *
+ * A cache is `pages` pages of page_size tokens in one piece of device memory, page after page.  A token is named by its slot,
+ * page * page_size + place in the page.  For each kv head a page has one block of page_size * (head_dim + 8) bytes:
+ *     key codes         page_size rows of head_dim / 2 bytes; element j is the nibble at bits [4 j, 4 j + 4) of the row's
+ *                       little-endian bit stream
+ *     value codes       [page_size / 4][16][head_dim / 64][4] halfwords: halfword [t / 4][r][f][t % 4] holds elements
+ *                       r * head_dim / 16 + 4 f + 0 .. 3 of token t, the first in its low bits
+ *     key parameters    page_size dwords: step in the low half, centre in the high half, both bfloat16
+ *     value parameters  likewise
+ * and an element is (code - 7.5) * step + centre.  Quantizer, per head row y (fp32, every operation rounded to nearest even):
+ *     lo = clip * min(y), hi = clip * max(y), step = bf16((hi - lo) / 15), centre = bf16((hi + lo) / 2),
+ *     code = clamp(rne((y - centre) * (1 / step) + 7.5), 0, 15);
+ * a step below 2^-100 is stored as 0.  A row with infinities or NaN has a step that is NaN; other rows are not affected.
+ * Keys are rotated by the handle's H_n / sqrt(n), n = head_dim (a Sylvester order: 64, 128); h NULL: not at all.  Queries
+ * then carry the same rotation, which rq_kv4_attention applies to them.  Values are stored as they come: their rotation is folded into
+ * the neighbouring weights (section 2.2).
+ * The calls take the current device, enqueue on `stream` and neither wait nor allocate; all of them can be captured in a graph.
+ */
+#define RQ_KV4_MAX_HEADS 1024
+
+typedef struct rq_kv4 {
+    void* data;        /* DEVICE, pages * rq_kv4_page_bytes(...) bytes, 16-byte aligned; caller-owned */
+    int64_t pages;     /* at most 2^31 - 1 */
+    int kv_heads;      /* 1 .. RQ_KV4_MAX_HEADS */
+    int head_dim;      /* 64 or 128 */
+    int page_size;     /* tokens of a page: 16, 32, 64, 128 or 256 */
+} rq_kv4_t;
+
+/* Bytes of a page: kv_heads * page_size * (head_dim + 8); 0 on bad arguments. */
+size_t rq_kv4_page_bytes(int kv_heads, int head_dim, int page_size);
+
+/*
+ * Rotate (keys), quantize and write the rows of `tokens` tokens to their slots.
+ *   K, V      [in]  DEVICE, element [token][head][i] at token * *_token_stride + head * *_head_stride + i (strides in elements, >= 0)
+ *   dtype     [in]  RQ_BF16, RQ_F16 or RQ_F32
+ *   slots     [in]  DEVICE, tokens int64; a token whose slot is negative or not in the cache is left out.  Two tokens of a
+ *                   call must not have the same slot.
+ *   clip      [in]  clip ratio in (0, 1]
+ * Errors: RQ_ERR_ARG (bad cache, order of h not head_dim, dtype, clip, negative stride, NULL or misaligned pointer), RQ_ERR_HIP.
+ */
+int rq_kv4_append(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* K, const void* V, int dtype, int64_t tokens,
+                  int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                  const int64_t* slots, float clip, void* stream);
+
+/*
+ * The rows of `rows` slots as numbers: K and V [rows][kv_heads][head_dim] of out_dtype, rounded to nearest even.  With h the keys
+ * are rotated back to the original basis, with NULL they are the values that are stored.  A slot that is negative or not in
+ * the cache gives zeros.
+ *   K, V      [out] DEVICE, 16-byte aligned
+ * Errors: RQ_ERR_ARG, RQ_ERR_HIP.
+ */
+int rq_kv4_read(const rq_hadamard_t* h, const rq_kv4_t* cache, const int64_t* slots, int64_t rows, void* K, void* V, int out_dtype,
+                void* stream);
+
+/*
+ * Copy whole pages, page src[i] to page dst[i] in each of `layers` caches that lie layer_stride bytes apart: forked sequences whose
+ * last page becomes their own, and compaction.  No page may be named twice in dst, nor be both in src and in dst (but for
+ * src[i] == dst[i], which does nothing); a pair with a page that is not in the cache is left out.
+ *   src, dst      [in]  DEVICE, `pairs` int32 each
+ *   layer_stride  [in]  at least pages * page bytes, a multiple of 16; not looked at with one layer
+ * Errors: RQ_ERR_ARG, RQ_ERR_HIP.
+ */
+int rq_kv4_copy_pages(const rq_kv4_t* cache, int layers, int64_t layer_stride, const int32_t* src, const int32_t* dst, int64_t pairs,
+                      void* stream);
+
+/*
+ * Bytes of device workspace rq_kv4_attention needs for such a call on the current device; 0 where it needs none and on bad
+ * arguments.  decode: q_start will be NULL.
+ */
+size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int heads, int batch, int decode, int window, int64_t max_len);
+
+/*
+ * Attention of a batch of sequences over their cached keys and values:
+ *     o = sum_j softmax_j(scale * q . k_j) v_j   over the positions j that the query sees.
+ * Sequence b has kv_lens[b] positions, position j in slot table[b][j / page_size] * page_size + j % page_size.  Its queries are tokens
+ * q_start[b] .. q_start[b + 1] - 1 and stand at its last positions: query i of n at kv_lens[b] - n + i.  A causal query sees
+ * positions up to its own, others all of the sequence; with a window w > 0 only those later than its own minus w.  A query that sees
+ * nothing gets zeros (and -infinity in lse).
+ * Query head x reads kv head x / (heads / kv_heads).  Queries are rotated as the keys were (h), rounded to fp16 after scaling each
+ * row by a power of two, and multiplied with the codes; probabilities are rounded to bf16, all else is fp32.
+ *   Q            [in]  DEVICE, element [token][head][i] at token * q_token_stride + head * q_head_stride + i
+ *   dtype        [in]  RQ_BF16 or RQ_F16, of Q and O
+ *   tokens       [in]  0 .. 2^24
+ *   heads        [in]  a multiple of kv_heads, at most 256 times it
+ *   table        [in]  DEVICE, batch x width int32 page numbers; those behind a sequence's last page are not read, a number
+ *                      that is not in the cache stands for page 0
+ *   kv_lens      [in]  DEVICE, batch int32; values are taken to be in 0 .. max_len
+ *   q_start      [in]  DEVICE, batch + 1 int32, ascending from 0 to tokens; NULL: one token a sequence (tokens == batch)
+ *   scale        [in]  of the scores, finite, > 0
+ *   causal       [in]  0 or 1;  window [in]  0: none
+ *   max_len      [in]  no sequence is longer; at most width * page_size and 2^30.  It bounds the work that is laid out.
+ *   O            [out] as Q with its own strides; must not overlap Q
+ *   lse          [out] DEVICE, tokens x heads floats, log of the sum of exp(scale * q . k_j), or NULL
+ *   workspace    [in]  DEVICE, >= rq_kv4_attention_workspace(...) bytes, 16-byte aligned, scratch; NULL where that is 0
+ * Long sequences are split over workgroups and joined in a fixed order: the same call gives the same bits.
+ * Errors: RQ_ERR_ARG, RQ_ERR_HIP.
+ */
+int rq_kv4_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* Q, int dtype, int64_t tokens, int heads,
+                     int64_t q_token_stride, int64_t q_head_stride, const int32_t* table, int batch, int width, const int32_t* kv_lens,
+                     const int32_t* q_start, float scale, int causal, int window, int64_t max_len, void* O, int64_t o_token_stride,
+                     int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Select the kernel family for subsequent hot-path calls on this handle (testing /
  * measurement): 0 = automatic (fastest available), 1 = the general LDS kernel; for long
  * power-of-two rows 2 = one wave per row at any row count, 3 / 4 = a row split over 2 / 4 waves

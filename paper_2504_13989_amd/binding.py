@@ -25,6 +25,12 @@ _lib = None
 _nat = None
 
 
+class RqKv4(C.Structure):
+    """rq_kv4_t of include/rotq.h."""
+    _fields_ = [("data", C.c_void_p), ("pages", C.c_int64), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("page_size", C.c_int)]
+
+
 class RotqError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -72,6 +78,16 @@ def lib() -> C.CDLL:
     L.rq_hadamard_set_variant.argtypes = [vp, i32]
     L.rq_hadamard_last_kernel.argtypes = [vp]
     L.rq_hadamard_last_kernel.restype = C.c_char_p
+    L.rq_kv4_page_bytes.argtypes = [i32, i32, i32]
+    L.rq_kv4_page_bytes.restype = C.c_size_t
+    kv4p = C.POINTER(RqKv4)
+    L.rq_kv4_append.argtypes = [vp, kv4p, vp, vp, i32, i64, i64, i64, i64, i64, vp, C.c_float, vp]
+    L.rq_kv4_read.argtypes = [vp, kv4p, vp, i64, vp, vp, i32, vp]
+    L.rq_kv4_copy_pages.argtypes = [kv4p, i32, i64, vp, vp, i64, vp]
+    L.rq_kv4_attention_workspace.argtypes = [kv4p, i64, i32, i32, i32, i32, i64]
+    L.rq_kv4_attention_workspace.restype = C.c_size_t
+    L.rq_kv4_attention.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, i32, i32, vp, vp, C.c_float, i32, i32, i64, vp,
+                                   i64, i64, vp, vp, C.c_size_t, vp]
     L.rq_strerror.argtypes = [i32]
     L.rq_strerror.restype = C.c_char_p
     for name in ("rq_hadamard_build", "rq_hadamard_info", "rq_hadamard_dense", "rq_next_order",
@@ -275,3 +291,83 @@ def gbs_search(h: Hadamard, x, bits: int, eps: float, max_evals: int = 64, works
     (clip, mse, trace) with trace a list of (probe, objective) pairs in the algorithm's order.
     Waits for the result; not for a stream under capture."""
     return (_nat or _native()).gbs_search(h._p, x, bits, eps, max_evals, workspace, stream, asym)
+
+
+class KV4Cache:
+    """A 4-bit paged key/value cache on the GPU (layout and quantizer: rq_kv4_t in include/rotq.h): `data` is a uint8 tensor
+    [pages, page bytes], or [layers, pages, page bytes] for all layers of a model, one of which is cache.layer(i)."""
+
+    __slots__ = ("data", "kv_heads", "head_dim", "page_size")
+
+    def __init__(self, data, kv_heads: int, head_dim: int, page_size: int):
+        need = kv4_page_bytes(kv_heads, head_dim, page_size)
+        if data.dim() not in (2, 3) or data.shape[-1] != need:
+            raise ValueError(f"data must be [(layers,) pages, {need}] for {kv_heads} heads of {head_dim} in pages of {page_size}")
+        self.data, self.kv_heads, self.head_dim, self.page_size = data, int(kv_heads), int(head_dim), int(page_size)
+
+    @property
+    def pages(self) -> int:
+        return self.data.shape[-2]
+
+    @property
+    def layers(self) -> int:
+        return self.data.shape[0] if self.data.dim() == 3 else 1
+
+    def layer(self, i: int) -> "KV4Cache":
+        """The cache of one layer, on the same memory."""
+        return KV4Cache(self.data[i] if self.data.dim() == 3 else self.data[None][i], self.kv_heads, self.head_dim, self.page_size)
+
+
+def kv4_page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
+    """rq_kv4_page_bytes; raises where there is no such page."""
+    big = max(int(kv_heads), int(head_dim), int(page_size)) > 1 << 30
+    n = 0 if big else int(lib().rq_kv4_page_bytes(int(kv_heads), int(head_dim), int(page_size)))
+    if n == 0:
+        raise RotqError(RQ_ERR_ARG, f"rq_kv4_page_bytes({kv_heads}, {head_dim}, {page_size})")
+    return n
+
+
+def kv4_cache(pages: int, kv_heads: int, head_dim: int, page_size: int = 64, layers: int = 1, device="cuda") -> KV4Cache:
+    """A new cache of zeros."""
+    import torch
+    size = (int(pages), kv4_page_bytes(kv_heads, head_dim, page_size))
+    return KV4Cache(torch.zeros(size if layers == 1 else (int(layers), *size), dtype=torch.uint8, device=device),
+                    kv_heads, head_dim, page_size)
+
+
+def _rotation(h: Optional[Hadamard]) -> int:
+    if h is None:
+        return 0
+    if not h._p:                       # a closed handle is not "no rotation"
+        raise RotqError(RQ_ERR_ARG, "rotation of the heads")
+    return h._p
+
+
+def kv4_append(h: Optional[Hadamard], cache: KV4Cache, k, v, slots, clip: float = 1.0, stream=None) -> None:
+    """rq_kv4_append: the keys (rotated by h, or h=None) and values [tokens, kv_heads, head_dim] of new tokens, quantized to 4 bits,
+    into their slots (int64, page * page_size + place; negative: left out).  Tokens and heads may be strided."""
+    (_nat or _native()).kv4_append(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, k, v, slots,
+                                   clip, stream)
+
+
+def kv4_read(h: Optional[Hadamard], cache: KV4Cache, slots, out_dtype=None, k=None, v=None, stream=None):
+    """rq_kv4_read: (keys, values) [rows, kv_heads, head_dim] of the slots, bfloat16 unless out_dtype says otherwise; with h the keys
+    in the original basis, with None as they are stored.  A negative slot gives zeros."""
+    return (_nat or _native()).kv4_read(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, slots,
+                                        out_dtype, k, v, stream)
+
+
+def kv4_copy_pages(cache: KV4Cache, src, dst, stream=None) -> None:
+    """rq_kv4_copy_pages: page src[i] to page dst[i] (int32) in all layers of the cache; no page both read and written, nor
+    written twice."""
+    (_nat or _native()).kv4_copy_pages(cache.data, cache.kv_heads, cache.head_dim, cache.page_size, src, dst, stream)
+
+
+def kv4_attention(h: Optional[Hadamard], cache: KV4Cache, q, table, kv_lens, q_start=None, scale: Optional[float] = None, causal: bool = True,
+                  window: int = 0, max_len: Optional[int] = None, out=None, lse=None, workspace=None, stream=None):
+    """rq_kv4_attention: attention of q [tokens, heads, head_dim] (bfloat16 or float16) over the cached sequences of a batch, table
+    int32 [batch, width] of page numbers, kv_lens int32 [batch].  Queries of sequence b are tokens q_start[b] .. q_start[b + 1] - 1
+    (int32 [batch + 1]; None: one token a sequence) and stand at its last positions.  scale: 1 / sqrt(head_dim).  `lse` (float32
+    [tokens, heads]) receives the logarithms of the softmax sums."""
+    return (_nat or _native()).kv4_attention(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q,
+                                             table, kv_lens, q_start, scale, causal, window, max_len, out, lse, workspace, stream)

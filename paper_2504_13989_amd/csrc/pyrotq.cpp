@@ -9,11 +9,14 @@
 #include <Python.h>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/StreamGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstring>
+#include <optional>
 #include <vector>
 
 #include "../../include/rotq.h"
@@ -500,6 +503,198 @@ PyObject* gbs_search(PyObject* const* a) {
     return Py_BuildValue("(ddN)", (double)clip, (double)mse, trace);
 }
 
+// A cache as its Python object holds it: (data, kv_heads, head_dim, page_size), data [pages, page bytes] or [layers, pages, page bytes].
+struct Cache {
+    rq_kv4_t c;
+    int64_t layers, layer_stride;
+    c10::Device device;
+    Cache(PyObject* const* a, const char* where) : c{}, layers(1), layer_stride(0), device(c10::kCPU) {
+        const at::Tensor& t = tensor(a[0]);
+        const long heads = integer(a[1]), dim = integer(a[2]), page = integer(a[3]);
+        if (heads < 1 || heads > RQ_KV4_MAX_HEADS || dim < 1 || dim > 128 || page < 1 || page > 256) check(RQ_ERR_ARG, where);
+        const size_t bytes = rq_kv4_page_bytes((int)heads, (int)dim, (int)page);
+        if (!bytes) check(RQ_ERR_ARG, where);
+        const int64_t nd = t.dim();
+        if (!t.is_cuda() || t.scalar_type() != at::kByte || nd < 2 || nd > 3 || t.size(nd - 1) != (int64_t)bytes ||
+            t.stride(nd - 1) != 1 || (t.size(nd - 2) > 1 && t.stride(nd - 2) != (int64_t)bytes))
+            raise(PyExc_ValueError, "the cache must be a uint8 device tensor [(layers,) pages, page bytes], a layer's pages one behind the other");
+        if (nd == 3) {
+            layers = t.size(0);
+            layer_stride = t.stride(0);
+        }
+        device = t.device();
+        c = rq_kv4_t{t.data_ptr(), t.size(nd - 2), (int)heads, (int)dim, (int)page};
+    }
+    void one_layer() const {
+        if (layers != 1) raise(PyExc_ValueError, "a cache of one layer is expected: take cache.layer(i)");
+    }
+};
+
+// Makes the caller's stream the current one while results and workspace are allocated: their memory then goes back to
+// that stream's pool and is not handed out again before the call's work on it is done.
+struct AllocateOn {
+    std::optional<c10::StreamGuard> guard;
+    explicit AllocateOn(PyObject* o) {
+        if (o == Py_None) return;
+        int64_t v[3];
+        const char* name[3] = {"stream_id", "device_index", "device_type"};
+        for (int i = 0; i < 3; ++i) {
+            PyObject* x = PyObject_GetAttrString(o, name[i]);
+            if (!x) throw Raised{};
+            v[i] = PyLong_AsLongLong(x);
+            Py_DECREF(x);
+            if (v[i] == -1 && PyErr_Occurred()) throw Raised{};
+        }
+        guard.emplace(c10::Stream::unpack3(v[0], (c10::DeviceIndex)v[1], (c10::DeviceType)v[2]));
+    }
+};
+
+// [tokens, heads, head_dim] with any strides of tokens and heads.
+struct HeadRows {
+    void* data;
+    int dtype;
+    int64_t tokens, heads, token, head;
+    HeadRows(const at::Tensor& t, const Cache& c, const char* text) {
+        if (!t.is_cuda() || t.device() != c.device || t.dim() != 3 || t.size(2) != c.c.head_dim || t.stride(2) != 1) raise(PyExc_ValueError, text);
+        dtype = dtype_code(t.scalar_type());
+        if (dtype < 0) raise(PyExc_TypeError, "unsupported input dtype");
+        data = const_cast<void*>(t.const_data_ptr());
+        tokens = t.size(0);
+        heads = t.size(1);
+        token = tokens > 1 ? t.stride(0) : t.size(1) * t.size(2);
+        head = heads > 1 ? t.stride(1) : t.size(2);
+    }
+};
+
+// A contiguous device tensor of whole numbers.
+const at::Tensor& numbers(PyObject* o, at::ScalarType type, int64_t dims, const Cache& c, const char* text) {
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.device() != c.device || t.scalar_type() != type || t.dim() != dims || !t.is_contiguous()) raise(PyExc_ValueError, text);
+    return t;
+}
+
+// (handle, data, kv_heads, head_dim, page_size, k, v, slots, clip, stream)
+PyObject* kv4_append(PyObject* const* a) {
+    const char* where = "rq_kv4_append";
+    const rq_hadamard_t* h = handle(a[0]);
+    const Cache c(a + 1, where);
+    c.one_layer();
+    const HeadRows k(tensor(a[5]), c, "k must be a device tensor [tokens, kv_heads, head_dim] with contiguous rows");
+    const HeadRows v(tensor(a[6]), c, "v must be a device tensor [tokens, kv_heads, head_dim] with contiguous rows");
+    if (k.heads != c.c.kv_heads || v.heads != c.c.kv_heads || k.tokens != v.tokens || k.dtype != v.dtype)
+        raise(PyExc_ValueError, "k and v must have the cache's kv_heads, the same tokens and one dtype");
+    const at::Tensor& slots = numbers(a[7], at::kLong, 1, c, "slots must be a contiguous int64 device tensor [tokens]");
+    if (slots.size(0) != k.tokens) raise(PyExc_ValueError, "slots must be a contiguous int64 device tensor [tokens]");
+    const float clip = real(a[8]);
+    void* s = stream(a[9]);
+    check(unlocked([&] {
+        return rq_kv4_append(h, &c.c, k.data, v.data, k.dtype, k.tokens, k.token, k.head, v.token, v.head, static_cast<const int64_t*>(slots.const_data_ptr()), clip, s);
+    }), where);
+    Py_RETURN_NONE;
+}
+
+// (handle, data, kv_heads, head_dim, page_size, slots, out_dtype, k, v, stream)
+PyObject* kv4_read(PyObject* const* a) {
+    const char* where = "rq_kv4_read";
+    const rq_hadamard_t* h = handle(a[0]);
+    const Cache c(a + 1, where);
+    c.one_layer();
+    const at::Tensor& slots = numbers(a[5], at::kLong, 1, c, "slots must be a contiguous int64 device tensor [rows]");
+    const int64_t rows = slots.size(0);
+    at::ScalarType t = at::kBFloat16;
+    if (a[6] != Py_None) {
+        if (!THPDtype_Check(a[6])) raise(PyExc_TypeError, "out_dtype must be a torch dtype");
+        t = reinterpret_cast<THPDtype*>(a[6])->scalar_type;
+    } else if (a[7] != Py_None) {
+        t = tensor(a[7]).scalar_type();
+    }
+    const int code = dtype_code(t);
+    if (code < 0) raise(PyExc_ValueError, "output dtype must be float32, bfloat16 or float16");
+    for (PyObject* o : {a[7], a[8]})
+        if (o != Py_None) {
+            const at::Tensor& y = tensor(o);
+            if (!y.is_cuda() || y.device() != c.device || y.scalar_type() != t || !y.is_contiguous() || y.numel() != rows * c.c.kv_heads * c.c.head_dim)
+                raise(PyExc_ValueError, "k and v must be contiguous device tensors [rows, kv_heads, head_dim] of out_dtype");
+        }
+    void* s = stream(a[9]);
+    const AllocateOn on(a[9]);
+    Out k, v;
+    k.make(a[7], {rows, c.c.kv_heads, c.c.head_dim}, t, c.device);
+    v.make(a[8], {rows, c.c.kv_heads, c.c.head_dim}, t, c.device);
+    check(unlocked([&] { return rq_kv4_read(h, &c.c, static_cast<const int64_t*>(slots.const_data_ptr()), rows, k.data, v.data, code, s); }), where);
+    return tuple2(k, v);
+}
+
+// (data, kv_heads, head_dim, page_size, src, dst, stream)
+PyObject* kv4_copy_pages(PyObject* const* a) {
+    const char* where = "rq_kv4_copy_pages";
+    const Cache c(a, where);
+    const at::Tensor& src = numbers(a[4], at::kInt, 1, c, "src must be a contiguous int32 device tensor [pairs]");
+    const at::Tensor& dst = numbers(a[5], at::kInt, 1, c, "dst must be a contiguous int32 device tensor [pairs]");
+    if (src.size(0) != dst.size(0)) raise(PyExc_ValueError, "src and dst must have the same length");
+    if (c.layers > (1 << 16)) check(RQ_ERR_ARG, where);
+    void* s = stream(a[6]);
+    check(unlocked([&] {
+        return rq_kv4_copy_pages(&c.c, (int)c.layers, c.layer_stride, static_cast<const int32_t*>(src.const_data_ptr()), static_cast<const int32_t*>(dst.const_data_ptr()), src.size(0), s);
+    }), where);
+    Py_RETURN_NONE;
+}
+
+// (handle, data, kv_heads, head_dim, page_size, q, table, kv_lens, q_start, scale, causal, window, max_len, out, lse, workspace, stream)
+PyObject* kv4_attention(PyObject* const* a) {
+    const char* where = "rq_kv4_attention";
+    const rq_hadamard_t* h = handle(a[0]);
+    const Cache c(a + 1, where);
+    c.one_layer();
+    const at::Tensor& qt = tensor(a[5]);
+    const HeadRows q(qt, c, "q must be a device tensor [tokens, heads, head_dim] with contiguous rows");
+    const at::Tensor& table = numbers(a[6], at::kInt, 2, c, "table must be a contiguous int32 device tensor [batch, width]");
+    const int64_t batch = table.size(0), width = table.size(1);
+    const at::Tensor& lens = numbers(a[7], at::kInt, 1, c, "kv_lens must be a contiguous int32 device tensor [batch]");
+    if (lens.size(0) != batch) raise(PyExc_ValueError, "kv_lens must be a contiguous int32 device tensor [batch]");
+    const int32_t* start = nullptr;
+    if (a[8] != Py_None) {
+        const at::Tensor& t = numbers(a[8], at::kInt, 1, c, "q_start must be a contiguous int32 device tensor [batch + 1]");
+        if (t.size(0) != batch + 1) raise(PyExc_ValueError, "q_start must be a contiguous int32 device tensor [batch + 1]");
+        start = static_cast<const int32_t*>(t.const_data_ptr());
+    } else if (q.tokens != batch) {
+        raise(PyExc_ValueError, "without q_start there must be one token a sequence");
+    }
+    const float scale = a[9] == Py_None ? (float)(1.0 / std::sqrt((double)c.c.head_dim)) : real(a[9]);
+    const int causal = truth(a[10]);
+    const long window = integer(a[11]);
+    const int64_t most = width * c.c.page_size;
+    const int64_t max_len = a[12] == Py_None ? most : integer(a[12]);
+    if (window < 0 || window > INT32_MAX || width > INT32_MAX || batch > INT32_MAX || q.heads > INT32_MAX || max_len < 0) check(RQ_ERR_ARG, where);
+    if (a[13] != Py_None) {
+        const at::Tensor& t = tensor(a[13]);
+        if (t.scalar_type() != qt.scalar_type() || t.dim() != 3 || t.size(0) != q.tokens || t.size(1) != q.heads)
+            raise(PyExc_ValueError, "out must have q's shape and dtype");
+    }
+    float* lse = nullptr;
+    if (a[14] != Py_None) {
+        const at::Tensor& t = tensor(a[14]);
+        if (!t.is_cuda() || t.device() != c.device || t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() != q.tokens * q.heads)
+            raise(PyExc_ValueError, "lse must be a contiguous float32 device tensor [tokens, heads]");
+        lse = static_cast<float*>(t.data_ptr());
+    }
+    void* s = stream(a[16]);
+    const AllocateOn on(a[16]);
+    Out o;
+    o.make(a[13], {q.tokens, q.heads, c.c.head_dim}, qt.scalar_type(), c.device);
+    const HeadRows y(THPVariable_Unpack(o.ref), c, "out must be a device tensor [tokens, heads, head_dim] with contiguous rows");
+    const int64_t len = max_len < most ? max_len : most;
+    const size_t need = rq_kv4_attention_workspace(&c.c, q.tokens, (int)q.heads, (int)batch, start == nullptr, (int)window, len);
+    std::optional<Scratch> ws;
+    if (need) ws.emplace(a[15], need, c.device);
+    check(unlocked([&] {
+        return rq_kv4_attention(h, &c.c, q.data, q.dtype, q.tokens, (int)q.heads, q.token, q.head, static_cast<const int32_t*>(table.const_data_ptr()), (int)batch,
+                                (int)width, static_cast<const int32_t*>(lens.const_data_ptr()), start, scale, causal, (int)window, len, y.data, y.token, y.head, lse,
+                                ws ? ws->data : nullptr, ws ? ws->bytes : 0, s);
+    }), where);
+    return o.take();
+}
+
 // Called once by the binding: the class of the errors raised for the library's error codes.
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
@@ -513,7 +708,8 @@ PyMethodDef methods[] = {
     RQ_ENTRY(rotate_quantize, 7),   RQ_ENTRY(rotate_quantize_asym, 8), RQ_ENTRY(quantize, 6),
     RQ_ENTRY(quantize_asym, 7),     RQ_ENTRY(rotate, 7),               RQ_ENTRY(dequantize_rotate, 10),
     RQ_ENTRY(dequantize, 7),        RQ_ENTRY(quant_error, 8),          RQ_ENTRY(quant_error_noalloc, 6),
-    RQ_ENTRY(gbs_search, 8),        {"set_error", set_error, METH_O, nullptr},
+    RQ_ENTRY(gbs_search, 8),        RQ_ENTRY(kv4_append, 10),          RQ_ENTRY(kv4_read, 10),
+    RQ_ENTRY(kv4_copy_pages, 7),    RQ_ENTRY(kv4_attention, 17),       {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 #undef RQ_ENTRY
 
