@@ -1,0 +1,244 @@
+// What the kernels of attention over the 4-bit paged cache share (kernels_kv4_attention.hip: few queries, kernels_kv4_prompt.hip: many).
+#pragma once
+#include "kv4_layout.h"
+#include "wave_common.h"
+
+namespace rq {
+
+struct KvJob {
+    Kv4 cache;
+    Kv4Attention a;
+    int group;                                    // query heads of a kv head
+    int tiles;                                    // row tiles (bound)
+    int workers;                                  // few rows: workgroups of a kv head that share its tiles out, 0: one a row tile
+    int chunk, chunks;                            // many rows: keys of a chunk, chunks (bound)
+    bool wide_q, wide_o;                          // rows of q, of o begin on 16 bytes
+    float* part;                                  // workspace
+};
+
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 64;                         // keys a step
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t pack_f16(float x, float y) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)x, (_Float16)y}); }
+template <bool F16>
+__device__ __forceinline__ uint32_t pack16(float x, float y) {
+    if constexpr (F16) return pack_f16(x, y);
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (x & mask) | bits; }
+
+// Sums and maxima over the lanes of a column: of 16 columns lanes n, n + 16, n + 32, n + 48, of 32 columns lanes n, n + 32.
+__device__ __forceinline__ void other_rows(float x, bool far, float& a, float& b) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r = far ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    a = __uint_as_float(r[0]);
+    b = __uint_as_float(r[1]);
+}
+template <int COLUMNS>
+__device__ __forceinline__ float column_sum(float x) {
+    float a, b;
+    if constexpr (COLUMNS == 16) {
+        other_rows(x, false, a, b);
+        x = a + b;
+    }
+    other_rows(x, true, a, b);
+    return a + b;
+}
+template <int COLUMNS>
+__device__ __forceinline__ float column_max(float x) {
+    float a, b;
+    if constexpr (COLUMNS == 16) {
+        other_rows(x, false, a, b);
+        x = fmaxf(a, b);
+    }
+    other_rows(x, true, a, b);
+    return fmaxf(a, b);
+}
+
+// A query row as the matrix cores take it, over 64 / COLUMNS lanes: lane g of a column holds the g-th part of the row, eights of
+// it in the order (0, 4), (1, 5), (2, 6), (3, 7) in which codes leave a dword.
+template <int D, int COLUMNS>
+struct Query {
+    static constexpr int E = D * COLUMNS / 64;    // elements of a lane
+    f16x8 hi[E / 8], lo[E / 8];                   // q = hi + lo; lo only where it is asked for
+    float even, odd;                              // sums of elements 0, 2, 4, 6 and 1, 3, 5, 7 of the eights
+    float f;                                      // log2 of e^(scale q.k) for a unit of hi.k, a power of two
+};
+
+// A lane's part of a row as it is stored; zeros where there is none.
+template <int D, int COLUMNS>
+struct RawQuery {
+    u32x4 w[D * COLUMNS / 512];
+};
+template <int D, int COLUMNS>
+__device__ __forceinline__ RawQuery<D, COLUMNS> load_query(const KvJob& job, bool there, int token, int head, int lane) {
+    const Kv4Attention& a = job.a;
+    constexpr int E = Query<D, COLUMNS>::E;
+    RawQuery<D, COLUMNS> raw{};
+    const uint16_t* x = static_cast<const uint16_t*>(a.q) + (int64_t)token * a.q_token + (int64_t)head * a.q_head + E * (lane / COLUMNS);
+    if (there) {
+        if (job.wide_q) {
+#pragma unroll
+            for (int e = 0; e < E / 8; ++e) raw.w[e] = reinterpret_cast<const u32x4*>(x)[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) raw.w[e / 8][e / 2 % 4] = (uint32_t)x[e] | ((uint32_t)x[e + 1] << 16);
+        }
+    }
+    return raw;
+}
+
+// Rotates a row, scales it by a power of two and rounds it.
+template <int D, int COLUMNS, bool F16, bool PRECISE>
+__device__ __forceinline__ void take_query(Query<D, COLUMNS>& r, const KvJob& job, const RawQuery<D, COLUMNS>& raw, int lane) {
+    const Kv4Attention& a = job.a;
+    constexpr int E = Query<D, COLUMNS>::E;
+    float q[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const uint32_t u = raw.w[e / 8][e / 2 % 4];
+        q[e] = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(e % 2 ? u >> 16 : u)) : __uint_as_float(e % 2 ? u & 0xffff0000u : u << 16);
+    }
+    if (a.rotate) {
+#pragma unroll
+        for (int w = 1; w < E; w *= 2)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (!(e & w)) {
+                    const float y = q[e], z = q[e + w];
+                    q[e] = y + z;
+                    q[e + w] = y - z;
+                }
+#pragma unroll
+        for (int w = COLUMNS; w < 64; w *= 2)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float y, z;
+                other_rows(q[e], w == 32, y, z);
+                q[e] = lane & w ? y - z : y + z;
+            }
+    }
+    // log2(e) and the scale of the scores are in the row, so that f is a power of two and f * (s - m) exact, however large
+    const float unit = a.scale * kLog2e * (a.rotate ? (D == 128 ? 0.08838834764831845f : 0.125f) : 1.0f);
+    float most = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        q[e] *= unit;
+        most = fmaxf(most, fabsf(q[e]));
+    }
+    most = column_max<COLUMNS>(most);
+    // 2^-x with most < 2^x: 1 for rows of zeros; infinite rows stay what they are
+    int x2 = (int)((__float_as_uint(most) >> 23) & 255) - 126;
+    x2 = most == 0.0f || x2 > 128 ? 0 : x2 < -100 ? -100 : x2;
+    const float by = __uint_as_float((uint32_t)(127 - (x2 > 126 ? 126 : x2)) << 23);
+    r.f = 1.0f / by;
+    float even = 0.0f, odd = 0.0f;
+#pragma unroll
+    for (int j = 0; j < E / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = q[8 * j + e / 2 + 4 * (e % 2)] * by;
+            const _Float16 hi = (_Float16)v;
+            float sum = (float)hi;
+            r.hi[j][e] = hi;
+            if constexpr (PRECISE) {
+                const _Float16 lo = (_Float16)(v - sum);
+                r.lo[j][e] = lo;
+                sum += (float)lo;
+            }
+            (e / 2 % 2 ? odd : even) += sum;
+        }
+    r.even = column_sum<COLUMNS>(even);
+    r.odd = column_sum<COLUMNS>(odd);
+}
+
+// N consecutive results of a row.
+template <int N, bool F16>
+__device__ __forceinline__ void store_row(uint16_t* o, const float (&y)[N], bool wide) {
+    if constexpr (N == 1) {
+        o[0] = (uint16_t)pack16<F16>(y[0], 0.0f);
+        return;
+    } else {
+        uint32_t w[N / 2];
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) w[e] = pack16<F16>(y[2 * e], y[2 * e + 1]);
+        if (wide) {
+            if constexpr (N % 8 == 0) {
+#pragma unroll
+                for (int e = 0; e < N / 8; ++e) reinterpret_cast<u32x4*>(o)[e] = u32x4{w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < N / 2; ++e) reinterpret_cast<uint32_t*>(o)[e] = w[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N / 2; ++e) {
+                o[2 * e] = (uint16_t)w[e];
+                o[2 * e + 1] = (uint16_t)(w[e] >> 16);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// Page numbers through the scalar cache: they are the same for all lanes, and a wait for them must not be one for the codes.
+typedef const int32_t __attribute__((address_space(4)))* TableRow;
+
+// A tile of BM rows: where they lie, and the positions that they see.
+struct Place {
+    int b, q0, nq, base;                          // sequence, its first token, its tokens, the tile's first row
+    int len;                                      // positions of the sequence
+    int from, to;                                 // some row of the tile sees; `from` a multiple of kTile
+};
+// Row r of a tile's sequence: its token.
+__device__ __forceinline__ int token_of(const KvJob& job, const Place& p, int r) { return p.nq == 1 ? 0 : r / job.group; }
+
+// Row tile `tile`: a sequence's tiles begin at floor(q_start * group / BM) + its number.  False where there is none.
+template <int BM>
+__device__ __forceinline__ bool find_rows(const KvJob& job, int tile, Place& p) {
+    const Kv4Attention& a = job.a;
+    int first;
+    if (a.q_start) {
+        int lo = 0, hi = a.batch - 1;
+        while (lo < hi) {
+            const int at = (lo + hi + 1) >> 1;
+            if ((int)((int64_t)a.q_start[at] * job.group / BM) + at <= tile) lo = at; else hi = at - 1;
+        }
+        p.b = lo;
+        int q0 = a.q_start[lo], q1 = a.q_start[lo + 1];
+        q0 = q0 < 0 ? 0 : q0 > a.tokens ? a.tokens : q0;
+        q1 = q1 < q0 ? q0 : q1 > a.tokens ? a.tokens : q1;
+        p.q0 = q0;
+        p.nq = q1 - q0;
+        first = (int)((int64_t)q0 * job.group / BM) + lo;
+    } else {
+        const int each = (job.group + BM - 1) / BM;
+        p.b = p.q0 = each == 1 ? tile : tile / each;
+        p.nq = 1;
+        first = p.b * each;
+    }
+    p.base = (tile - first) * BM;
+    const int rows = p.nq * job.group;
+    if (p.base < 0 || p.base >= rows) return false;
+    const int len = a.kv_lens[p.b];
+    p.len = len < 0 ? 0 : len > a.max_len ? (int)a.max_len : len;          // (max_len <= width * page size)
+    const int last = (p.base + BM < rows ? p.base + BM : rows) - 1;
+    const int p0 = p.len - p.nq + token_of(job, p, p.base), p1 = p.len - p.nq + token_of(job, p, last);
+    const int from = a.window ? p0 - a.window + 1 : 0;
+    p.from = (from < 0 ? 0 : from) & ~(kTile - 1);
+    p.to = a.causal && p1 + 1 < p.len ? p1 + 1 : p.len;
+    return true;
+}
+
+}  // namespace
+
+// kernels_kv4_prompt.hip: many rows, 32 a wave, a workgroup of 4 or 8 waves
+void launch_prompt(const KvJob& job, int waves, hipStream_t s);
+
+}  // namespace rq
