@@ -25,6 +25,7 @@
 // two a unit take 109).  The waves take a workgroup's tiles in turn.  A tile's codes are read into the registers of the one before
 // as soon as those are used up, keys during the softmax, values during the next keys' products.
 #include "kv4_attention.h"
+#include <cstdlib>
 
 namespace rq {
 namespace {
@@ -32,17 +33,15 @@ namespace {
 constexpr int kWaves = 4;
 
 // Eight key codes as fp16: elements (0, 4), (1, 5), (2, 6), (3, 7) of the dword, 1024 + c in the even ones, 64 + c in the odd ones.
-__device__ __forceinline__ f16x8 key_operand(uint32_t w) {
+__device__ __forceinline__ f16x8 key_operand(uint32_t w, const CodeBits& bits) {
     const uint32_t h = w >> 8;
-    const u32x4 x{and_or(w, 0x000f000fu, 0x64006400u), and_or(w, 0x00f000f0u, 0x54005400u), and_or(h, 0x000f000fu, 0x64006400u),
-                  and_or(h, 0x00f000f0u, 0x54005400u)};
-    return __builtin_bit_cast(f16x8, x);
+    return __builtin_bit_cast(f16x8, u32x4{bits.low(w), bits.high(w), bits.low(h), bits.high(h)});
 }
 // Nibble J of both halves of a dword as fp16: 1024 + c for even J, 64 + c for odd J.
 template <int J>
-__device__ __forceinline__ uint32_t value_pair(uint32_t w) {
+__device__ __forceinline__ uint32_t value_pair(uint32_t w, const CodeBits& bits) {
     const uint32_t x = J / 2 ? w >> 8 : w;
-    return J % 2 ? and_or(x, 0x00f000f0u, 0x54005400u) : and_or(x, 0x000f000fu, 0x64006400u);
+    return J % 2 ? bits.high(x) : bits.low(x);
 }
 
 // A tile's codes as they are stored, and its keys' parameters, a key a lane.
@@ -51,60 +50,54 @@ struct Codes {
     uint32_t k[4][D / 32], v[4][D / 32];          // [16 keys][dword]
     uint32_t kp, vp;
 };
-// Where a tile's 16 keys each begin: key codes, the parameters' array less 4 bytes a key before (both of the page's block).
+// Where a tile's codes and parameters lie: the head's block of its page, the place in the page; PAGED: of each 16 keys.
+template <bool PAGED>
 struct Source {
-    const uint8_t* block[4];
-    int at[4];                                    // place in the page
+    const uint8_t* block[PAGED ? 4 : 1];
+    int at[PAGED ? 4 : 1];
 };
-__device__ __forceinline__ Source find_tile(const Kv4& c, TableRow table, int head, int head_bytes, int k0, int end) {
-    const int shift = c.page_shift, p = 1 << shift;
-    Source s;
-    if (shift >= 6) {                             // a tile lies in one page
-        int page = table[k0 >> shift];
-        if ((uint32_t)page >= (uint32_t)c.pages) page = 0;
-        const uint8_t* block = c.data + (int64_t)page * c.page_bytes + (int64_t)head * head_bytes;
+template <bool PAGED>
+__device__ __forceinline__ Source<PAGED> find_tile(const Kv4& c, int pages, int n, int head_at, int k0, int end) {
+    Source<PAGED> s;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s.block[i] = block;
-            s.at[i] = (k0 & (p - 1)) + 16 * i;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int key = k0 + 16 * i;
-            if (key >= end) key = (end - 1) & ~15;                   // (those keys are masked)
-            int page = table[key >> shift];
-            if ((uint32_t)page >= (uint32_t)c.pages) page = 0;
-            s.block[i] = c.data + (int64_t)page * c.page_bytes + (int64_t)head * head_bytes;
-            s.at[i] = key & (p - 1);
-        }
+    for (int i = 0; i < (PAGED ? 4 : 1); ++i) {
+        s.block[i] = block_of<PAGED>(c, pages, n, i, head_at);
+        s.at[i] = place_of<PAGED>(c, k0, i, end);
     }
     return s;
 }
-template <int D>
-__device__ __forceinline__ void load_keys(Codes<D>& t, const Source& s, int page_shift, int lane) {
+template <int D, bool PAGED>
+__device__ __forceinline__ void load_keys(Codes<D>& t, const Source<PAGED>& s, int page_shift, int lane) {
     typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
     const uint32_t off = (uint32_t)((lane & 15) * (D / 2) + (lane >> 4) * (D / 8));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const words x = *reinterpret_cast<const words*>(s.block[i] + s.at[i] * (D / 2) + off);
+        const uint8_t* k = PAGED ? s.block[PAGED ? i : 0] + s.at[PAGED ? i : 0] * (D / 2) : s.block[0] + s.at[0] * (D / 2) + i * (8 * D);
+        const words x = __builtin_nontemporal_load(reinterpret_cast<const words*>(k + off));
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) t.k[i][j] = x[j];
     }
-    const int i = lane >> 4;
-    const uint8_t* block = i == 0 ? s.block[0] : i == 1 ? s.block[1] : i == 2 ? s.block[2] : s.block[3];
-    const int at = i == 0 ? s.at[0] : i == 1 ? s.at[1] : i == 2 ? s.at[2] : s.at[3];
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(block + (D << page_shift)) + (at + (lane & 15));
-    t.kp = w[0];
-    t.vp = w[1 << page_shift];
+    const uint8_t* w;
+    if constexpr (PAGED) {
+        const int i = lane >> 4;
+        const uint8_t* block = i == 0 ? s.block[0] : i == 1 ? s.block[1] : i == 2 ? s.block[2] : s.block[3];
+        const int at = i == 0 ? s.at[0] : i == 1 ? s.at[1] : i == 2 ? s.at[2] : s.at[3];
+        w = block + (uint32_t)((D << page_shift) + 4 * (at + (lane & 15)));
+    } else {
+        w = s.block[0] + ((D << page_shift) + 4 * s.at[0]) + (uint32_t)(4 * lane);
+    }
+    t.kp = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(w));
+    t.vp = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(w + (4 << page_shift)));
 }
-template <int D>
-__device__ __forceinline__ void load_values(Codes<D>& t, const Source& s, int page_shift, int lane) {
+template <int D, bool PAGED>
+__device__ __forceinline__ void load_values(Codes<D>& t, const Source<PAGED>& s, int page_shift, int lane) {
     typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
     const uint32_t off = (uint32_t)((lane >> 4) * (2 * D) + (lane & 15) * (D / 8));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const words x = *reinterpret_cast<const words*>(s.block[i] + ((1 << page_shift) + s.at[i]) * (D / 2) + off);
+        const int at = (1 << page_shift) + s.at[PAGED ? i : 0];
+        const uint8_t* v = s.block[PAGED ? i : 0] + at * (D / 2) + (PAGED ? 0 : i * (8 * D));
+        const words x = __builtin_nontemporal_load(reinterpret_cast<const words*>(v + off));
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) t.v[i][j] = x[j];
     }
@@ -162,13 +155,13 @@ __device__ __forceinline__ void take_parameters(Columns<D>& r, const Codes<D>& t
 
 // Scores of a tile: s[u], of 16 keys each that the lane's copy has.
 template <int D, int F, bool F16>
-__device__ __forceinline__ void take_keys(f32x4 (&s)[4 / F], const Columns<D>& r, const Codes<D>& t, int copy) {
+__device__ __forceinline__ void take_keys(f32x4 (&s)[4 / F], const Columns<D>& r, const Codes<D>& t, const CodeBits& bits, int copy) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f32x4 acc = f32x4{r.bias, r.bias, r.bias, r.bias};
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {
-            const f16x8 a = key_operand(t.k[i][j]);
+            const f16x8 a = key_operand(t.k[i][j], bits);
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, r.q.hi[j], acc, 0, 0, 0);
             if constexpr (F16) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, r.q.lo[j], acc, 0, 0, 0);
         }
@@ -223,7 +216,7 @@ __device__ __forceinline__ void take_scores(uint32_t (&p)[4 / F][2], Columns<D>&
 }
 
 template <int D, int F>
-__device__ __forceinline__ void take_values(Columns<D>& r, const Codes<D>& t, const uint32_t (&p)[4 / F][2], int copy) {
+__device__ __forceinline__ void take_values(Columns<D>& r, const Codes<D>& t, const uint32_t (&p)[4 / F][2], const CodeBits& bits, int copy) {
     const u32x4 less_even{0xe408e408u, 0xe408e408u, 0xe408e408u, 0xe408e408u}, less_odd{0xd480d480u, 0xd480d480u, 0xd480d480u, 0xd480d480u};   // -1032, -72
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -238,8 +231,8 @@ __device__ __forceinline__ void take_values(Columns<D>& r, const Codes<D>& t, co
 #define RQ_VALUES(J)                                                                                                            \
     {                                                                                                                           \
         constexpr int h = 2 * ((J) / 4);                                                                                        \
-        const u32x4 a{value_pair<(J) % 4>(t.v[2 * i][h]), value_pair<(J) % 4>(t.v[2 * i][h + 1]),                               \
-                      value_pair<(J) % 4>(t.v[2 * i + 1][h]), value_pair<(J) % 4>(t.v[2 * i + 1][h + 1])};                      \
+        const u32x4 a{value_pair<(J) % 4>(t.v[2 * i][h], bits), value_pair<(J) % 4>(t.v[2 * i][h + 1], bits),                               \
+                      value_pair<(J) % 4>(t.v[2 * i + 1][h], bits), value_pair<(J) % 4>(t.v[2 * i + 1][h + 1], bits)};                      \
         r.o[J] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, (J) % 2 ? less_odd : less_even), x, r.o[J], 0, 0, 0); \
         r.o[J] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), x, r.o[J], 0, 0, 0);                      \
     }
@@ -301,7 +294,7 @@ __device__ __forceinline__ int* part_workers(const KvJob& job) {
     return reinterpret_cast<int*>(part_sums<D, C>(job) + (int64_t)(job.workers + job.tiles) * job.cache.kv_heads * C);
 }
 
-template <int D, int F, bool F16>
+template <int D, int F, bool F16, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
     constexpr int C = 16 / F, E = D / 4;          // rows of the workgroup; elements of a row in a lane
     __shared__ __attribute__((aligned(16))) float lds_params[kWaves][4 * kTile];
@@ -311,23 +304,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
     const Kv4Attention& a = job.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int copy = (lane & 15) / C, g = lane >> 4;
-    const int64_t item = group_index();
-    const int kv = job.cache.kv_heads;
-    const int number = (int)(item / kv), head = (int)(item - (int64_t)number * kv);
-    const int head_bytes = (D + 8) << job.cache.page_shift;
+    const int kv = job.cache.kv_heads, number = item_number(), head = blockIdx.x;
+    const int head_at = head * ((D + 8) << job.cache.page_shift);    // of the kv head's block in a page
+    const CodeBits bits;
     float* lds = lds_params[wave];
     int tile = number, share = 0, share_end = 1;  // the workgroup's tiles of 64 keys, all row tiles counted
     if (job.workers) {
         const int each = share_out<C>(job, shares);
         share = number * each;
         share_end = share + each < shares.begin[job.tiles] ? share + each : shares.begin[job.tiles];
-        if (item == 0)
+        if (number == 0 && head == 0)
             for (int t = threadIdx.x; t < job.tiles; t += 64 * kWaves) {
                 int* w = part_workers<D, C>(job) + 2 * t;
                 w[0] = shares.begin[t] / each;
                 w[1] = shares.begin[t + 1] > shares.begin[t] ? (shares.begin[t + 1] - 1) / each : w[0];
             }
-        if (share >= share_end) return;
+        if (share >= share_end) return;           // (also of workers that only fill the grid)
         int lo = 0, hi = job.tiles - 1;           // the last row tile that begins at or before the share
         while (lo < hi) {
             const int at = (lo + hi + 1) >> 1;
@@ -364,12 +356,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
         const bool there = n < rows;
         const int token = there ? token_of(job, at, n) : 0;
         const RawQuery<D, 16> raw = load_query<D, 16>(job, there, at.q0 + token, head * job.group + (there ? n - token * job.group : 0), lane);
-        const TableRow table = (TableRow)(uintptr_t)(a.table + (int64_t)at.b * a.width);
+        const int32_t* table = a.table + (int64_t)at.b * a.width;
         const int shift = job.cache.page_shift;
-        int k0 = from + wave * kTile;
+        constexpr int stride = kWaves * kTile;
+        int k0 = from + wave * kTile, number_of = 0, pages = 0;      // the tile in hand, its number among those of `pages`
         Codes<D> t;
         if (k0 < to) {
-            const Source s = find_tile(job.cache, table, head, head_bytes, k0, to);
+            pages = load_pages<PAGED>(job.cache, table, k0, stride, to, lane);
+            const Source<PAGED> s = find_tile<PAGED>(job.cache, pages, 0, head_at, k0, to);
             load_keys<D>(t, s, shift, lane);
             load_values<D>(t, s, shift, lane);
         }
@@ -393,16 +387,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) r.o[j] = f32x4{0, 0, 0, 0};
         while (k0 < to) {
-            const int next = k0 + kWaves * kTile;
-            Source s;
-            if (next < to) s = find_tile(job.cache, table, head, head_bytes, next, to);
+            const int next = k0 + stride;
+            if (++number_of == kPagesOf<PAGED> && next < to) {
+                pages = load_pages<PAGED>(job.cache, table, next, stride, to, lane);
+                number_of = 0;
+            }
+            Source<PAGED> s;
+            if (next < to) s = find_tile<PAGED>(job.cache, pages, number_of, head_at, next, to);
             take_parameters<D>(r, t, lds, k0 + lane < to, lane);
             f32x4 x[4 / F];
-            take_keys<D, F, F16>(x, r, t, copy);
+            take_keys<D, F, F16>(x, r, t, bits, copy);
             if (next < to) load_keys<D>(t, s, shift, lane);
             uint32_t p[4 / F][2];
             take_scores<D, F>(p, r, x, lds, k0, k0 >= all_lo && k0 + kTile <= all_hi, copy, g);
-            take_values<D, F>(r, t, p, copy);
+            take_values<D, F>(r, t, p, bits, copy);
             if (next < to) load_values<D>(t, s, shift, lane);
             k0 = next;
         }
@@ -466,8 +464,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join_shares(KvJob job) {
     __shared__ float lds_o[kWaves][C * D], lds_l[kWaves][C];
     const Kv4Attention& a = job.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kv = job.cache.kv_heads;
-    const int64_t item = group_index();
-    const int tile = (int)(item / kv), head = (int)(item - (int64_t)tile * kv);
+    const int tile = item_number(), head = blockIdx.x;
     if (tile >= job.tiles) return;
     const int first = part_workers<D, C>(job)[2 * tile], last = part_workers<D, C>(job)[2 * tile + 1];
     Place at;
@@ -575,7 +572,7 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     p.chunks = 1;
     p.chunk = 1 << 30;
     p.copies = mean > 32 ? 0 : mean <= 4 ? 4 : mean <= 8 ? 2 : 1;
-    p.waves = mean <= 512 ? 4 : 8;
+    p.waves = getenv("RQ_PW") ? atoi(getenv("RQ_PW")) : mean <= 512 ? 4 : 8;
     const int bm = p.copies ? 16 / p.copies : 32 * p.waves;
     const int64_t tiles = a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm);
     p.tiles = (int)tiles;
@@ -587,7 +584,7 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     if (p.copies) {
         // two workgroups a compute unit share the keys out, unless the sequences are short or there are very many of them
         if (tiles <= kMostTiles && range > kLeast * kTile && tiles * (range / kTile + 1) < INT32_MAX) {
-            p.workers = (int)((2 * num_cu + c.kv_heads - 1) / c.kv_heads);
+            p.workers = (int)(((getenv("RQ_W") ? atoi(getenv("RQ_W")) : 2) * num_cu + c.kv_heads - 1) / c.kv_heads);
             p.bytes = ((size_t)(p.workers + p.tiles) * c.kv_heads * (16 / p.copies) * (c.head_dim + 1) + 2 * (size_t)p.tiles) * sizeof(float);
         }
         return p;
@@ -608,10 +605,10 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
 
 template <int D, int F, bool F16>
 void launch_few(const KvJob& job, hipStream_t s) {
-    const dim3 block(64 * kWaves);
-    const int64_t kv = job.cache.kv_heads;
-    launch_kernel(k_kv4_attention<D, F, F16>, group_grid((job.workers ? job.workers : job.tiles) * kv, 64 * kWaves), block, 0, s, job);
-    if (job.workers) launch_kernel(k_kv4_join_shares<D, F, F16>, group_grid(job.tiles * kv, 64 * kWaves), block, 0, s, job);
+    const dim3 block(64 * kWaves), grid = item_grid(job.cache.kv_heads, job.workers ? job.workers : job.tiles);
+    if (job.cache.page_shift >= 6) launch_kernel(k_kv4_attention<D, F, F16, false>, grid, block, 0, s, job);
+    else launch_kernel(k_kv4_attention<D, F, F16, true>, grid, block, 0, s, job);
+    if (job.workers) launch_kernel(k_kv4_join_shares<D, F, F16>, item_grid(job.cache.kv_heads, job.tiles), block, 0, s, job);
 }
 
 template <int D, bool F16>

@@ -6,7 +6,7 @@
 // operations, and codes that each wave unpacked for itself would cost as much again.  So the waves of a workgroup (4 or 8)
 // unpack a tile of 64 keys together, once, into LDS as fp16 operands: keys [key][element], values transposed, [element][key], keys in
 // the order in which scores leave the matrix cores, so that p enters them again as it is.  The next tile is unpacked into the
-// other half of LDS before the products on this one; its codes were loaded a step earlier.
+// other half of LDS beside the products of keys on this one; its codes were loaded two steps earlier.
 //   - bf16 results: operands are the elements themselves, (code - 7.5) step + mid, times a power of two that holds the largest
 //     seen so far in fp16's range (rounded to fp16 once, 2^-12: less than the result's rounding; steps and centres, bf16, are exact in fp16).  Scores need no step or centre.
 //   - fp16 results (EXACT): operands are codes - 7.5, which are exact, and steps and centres are applied to the scores as in the other
@@ -37,52 +37,35 @@ struct Raw {
 template <int D>
 constexpr int kRuns = kTile * D / 16;
 
-template <int D, int WAVES, int N>
-__device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, TableRow table, int head, int k0, int end, int thread) {
-    const int shift = c.page_shift, p = 1 << shift, lane = thread & 63;
-    const auto block_of = [&](int key) {
-        int page = table[key >> shift];
-        if ((uint32_t)page >= (uint32_t)c.pages) page = 0;
-        return c.data + (int64_t)page * c.page_bytes + (int64_t)(head * (p * (D + 8)));
-    };
-    if (shift >= 6) {                             // a tile lies in one page
-        const uint8_t* block = block_of(k0);
-        const int at = k0 & (p - 1);
-        const uint8_t *k = block + at * (D / 2), *v = block + (p + at) * (D / 2), *w = block + p * D + at * 4;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t run = (uint32_t)(thread + 64 * WAVES * i) * 8;
-            if (kRuns<D> % (64 * WAVES) == 0 || run < kRuns<D> * 8) {
-                t.k[i] = *reinterpret_cast<const u32x2*>(k + run);
-                t.v[i] = *reinterpret_cast<const u32x2*>(v + run);
-            }
-        }
-        t.kp = *reinterpret_cast<const uint32_t*>(w + (uint32_t)(lane * 4));
-        t.vp = *reinterpret_cast<const uint32_t*>(w + 4 * p + (uint32_t)(lane * 4));
-    } else {
-        const uint8_t* of[4];                     // of each 16 keys
+// The tile from k0 on, number n of `pages`.
+template <int D, int WAVES, int N, bool PAGED>
+__device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, int pages, int n, int head_at, int k0, int end, int thread) {
+    const int p = 1 << c.page_shift, lane = thread & 63;
+    const uint8_t* w;
+    if constexpr (PAGED) {
+        const int mine = lane >> 4;
+        const uint8_t* block = nullptr;
+        int at = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            int key = k0 + 16 * i;
-            if (key >= end) key = (end - 1) & ~15;                   // (those keys are masked)
-            const int at = key & (p - 1);
-            of[i] = block_of(key) + at * 4;       // + p * D: parameters; codes at 4 * at * (D / 8 - 1) further
-            if ((lane >> 4) == i) {
-                const uint8_t* w = of[i] + p * D + (lane & 15) * 4;
-                t.kp = *reinterpret_cast<const uint32_t*>(w);
-                t.vp = *reinterpret_cast<const uint32_t*>(w + 4 * p);
-            }
-            of[i] += at * (D / 2 - 4);
+            block = mine == i ? block_of<PAGED>(c, pages, n, i, head_at) : block;
+            at = mine == i ? place_of<PAGED>(c, k0, i, end) : at;
         }
+        w = block + (uint32_t)(p * D + 4 * (at + (lane & 15)));
+    } else {
+        w = block_of<PAGED>(c, pages, n, 0, head_at) + (p * D + 4 * place_of<PAGED>(c, k0, 0, end)) + (uint32_t)(lane * 4);
+    }
+    t.kp = *reinterpret_cast<const uint32_t*>(w);
+    t.vp = *reinterpret_cast<const uint32_t*>(w + 4 * p);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int run = thread + 64 * WAVES * i, q = run / (kRuns<D> / 4), in = run % (kRuns<D> / 4) * 8;
-            if (run < kRuns<D>) {
-                const uint8_t* x = q == 0 ? of[0] : q == 1 ? of[1] : q == 2 ? of[2] : of[3];
-                t.k[i] = *reinterpret_cast<const u32x2*>(x + in);
-                t.v[i] = *reinterpret_cast<const u32x2*>(x + p * (D / 2) + in);
-            }
-        }
+    for (int i = 0; i < N; ++i) {
+        const int run = thread + 64 * WAVES * i;
+        if (kRuns<D> % (64 * WAVES) != 0 && run >= kRuns<D>) break;
+        // (a wave's 64 runs lie in one quarter)
+        const int q = PAGED ? __builtin_amdgcn_readfirstlane(run / (kRuns<D> / 4)) : 0;
+        const uint8_t* x = block_of<PAGED>(c, pages, n, q, head_at) + place_of<PAGED>(c, k0, q, end) * (D / 2) + (uint32_t)((PAGED ? run % (kRuns<D> / 4) : run) * 8);
+        t.k[i] = *reinterpret_cast<const u32x2*>(x);
+        t.v[i] = *reinterpret_cast<const u32x2*>(x + p * (D / 2));
     }
 }
 
@@ -91,39 +74,37 @@ __device__ __forceinline__ uint32_t as_bits(f16x2 x) { return __builtin_bit_cast
 
 // c - 7.5 of nibble J of both halves of a dword, exact: 64 + c less 71.5.
 template <int J>
-__device__ __forceinline__ f16x2 code_pair(uint32_t w) {
+__device__ __forceinline__ f16x2 code_pair(uint32_t w, const CodeBits& bits) {
     const uint32_t x = J == 0 ? w << 4 : w >> (4 * J - 4);
-    return as_f16(and_or(x, 0x00f000f0u, 0x54005400u)) + f16x2{(_Float16)-71.5f, (_Float16)-71.5f};
+    return as_f16(bits.high(x)) + f16x2{(_Float16)-71.5f, (_Float16)-71.5f};
 }
 
 // The powers of two in the operands: what has been seen so far is below `limit`.
 struct Range {
     float limit;
-    float by;                                     // 2^UP / limit
+    int up;                                       // log2 of the factor, 2^UP / limit
 };
-// True where the range grew; `grew` is the old factor's inverse times the new one.  UP: 15 for elements, whose fp16 then has
-// full precision down to 2^-29 of the largest; 7 for steps, which meet factors of up to 2^8.
+// By how much the factor's log2 changed.  UP: 15 for elements, whose fp16 then has full precision down to 2^-29 of the largest; 7
+// for steps, which meet factors of up to 2^8.
 template <int UP>
-__device__ __forceinline__ bool widen(Range& r, float x, float& grew) {
-    if (!__any(x > r.limit)) return false;
+__device__ __forceinline__ int widen(Range& r, float x) {
+    if (!__any(x > r.limit)) return 0;
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) x = fmaxf(x, __shfl_xor(x, w));
     int e = (int)(__float_as_uint(x) >> 23) - 126;                   // x < 2^e
-    e = e < -60 ? -60 : e > 126 ? 126 : e;
+    e = __builtin_amdgcn_readfirstlane(e < -60 ? -60 : e > 126 ? 126 : e);
     const float limit = __uint_as_float((uint32_t)(e + 127) << 23);
-    if (!(limit > r.limit)) return false;
-    const float by = __uint_as_float((uint32_t)(127 + UP - e) << 23);
-    grew = by / r.by;
+    if (!(limit > r.limit)) return 0;
+    const int by = UP - e - r.up;
     r.limit = limit;
-    r.by = by;
-    return true;
+    r.up = UP - e;
+    return by;
 }
 
 template <int D, bool EXACT>
 struct Sums {
-    float m, l, w;                                // maximum (log2), sums over the lane's keys
-    typedef float f32x16 __attribute__((ext_vector_type(16)));
-    f32x16 o[D / 32];
+    float m, l, w;                                // maximum (log2), sums over the lane's keys of p and, EXACT, p * mid
+    float __attribute__((ext_vector_type(16))) o[D / 32];
 };
 template <int D, bool EXACT>
 __device__ __forceinline__ void scale_sums(Sums<D, EXACT>& r, float by) {
@@ -133,118 +114,192 @@ __device__ __forceinline__ void scale_sums(Sums<D, EXACT>& r, float by) {
         for (int e = 0; e < 16; ++e) r.o[j][e] *= by;
 }
 
-// Unpacks a thread's runs into LDS.  `key_range` and `value_range` widen to hold the tile.
+// What a thread needs of a tile's parameters to unpack its runs.
+template <int N>
+struct Factors {
+    f16x2 key[N], value[N][4];                    // step and centre
+};
+// The parameters of a tile's keys, a key a lane: ranges widen to hold them, and the lanes get those of their runs.
 template <int D, int WAVES, int N, bool EXACT>
-__device__ __forceinline__ void unpack(Tile<D, EXACT>& to, const Raw<N>& t, int k0, int end, int thread, const Range& key_range, const Range& value_range) {
+__device__ __forceinline__ void take_parameters(Factors<N>& f, Tile<D, EXACT>& to, const Raw<N>& t, bool there, int thread, Range& keys, Range& values, int& grew) {
     const int lane = thread & 63;
-    uint32_t kw = 0, vw = 0;                      // parameters of key `lane`, as fp16 pairs of a step and a centre
-    {
-        const bool there = k0 + lane < end;
-        const uint32_t kp = there ? t.kp : 0u, vp = there ? t.vp : 0u;
-        float ks = __uint_as_float(kp << 16), km = __uint_as_float(kp & 0xffff0000u);
-        float vs = __uint_as_float(vp << 16), vm = __uint_as_float(vp & 0xffff0000u);
-        if constexpr (EXACT) {
-            // (a wave an array: all of them hold the parameters)
-            if (thread >> 6 == 0) to.scale[0][lane] = ks;
-            if (thread >> 6 == 1) to.scale[1][lane] = km;
-            if (thread >> 6 == 2) to.scale[2][lane] = vs;
-            if (thread >> 6 == 3) to.scale[3][lane] = vm;
-        } else {
-            if (!finite(vs) || !finite(vm)) {
-                vs = vm = 0.0f;
-                ks = __builtin_nanf("");
-            }
-            kw = pack_f16(ks * key_range.by, km * key_range.by);
-            vw = pack_f16(vs * value_range.by, vm * value_range.by);
+    const uint32_t kp = there ? t.kp : 0u, vp = there ? t.vp : 0u;
+    float ks = __uint_as_float(kp << 16), km = __uint_as_float(kp & 0xffff0000u);
+    float vs = __uint_as_float(vp << 16), vm = __uint_as_float(vp & 0xffff0000u);
+    if (!finite(vs) || !finite(vm)) {
+        vs = vm = 0.0f;
+        ks = __builtin_nanf("");
+    }
+    const float kx = fmaf(8.0f, ks, fabsf(km)), vx = EXACT ? vs : fmaf(8.0f, vs, fabsf(vm));
+    grew = widen<EXACT ? 7 : 15>(values, vx < 0x1p126f ? vx : 0.0f);
+    if constexpr (EXACT) {
+        // (a wave an array: all of them hold the parameters)
+        if (thread >> 6 == 0) to.scale[0][lane] = ks;
+        if (thread >> 6 == 1) to.scale[1][lane] = km;
+        if (thread >> 6 == 2) to.scale[2][lane] = vs;
+        if (thread >> 6 == 3) to.scale[3][lane] = vm;
+    } else {
+        widen<15>(keys, kx < 0x1p126f ? kx : 0.0f);
+        const int kw = (int)pack_f16(__builtin_amdgcn_ldexpf(ks, keys.up), __builtin_amdgcn_ldexpf(km, keys.up));
+        const int vw = (int)pack_f16(__builtin_amdgcn_ldexpf(vs, values.up), __builtin_amdgcn_ldexpf(vm, values.up));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int run = thread + 64 * WAVES * i;
+            f.key[i] = as_f16((uint32_t)__shfl(kw, run / (D / 16) & 63));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.value[i][e] = as_f16((uint32_t)__shfl(vw, (4 * (run / (D / 4)) + e) & 63));
         }
     }
+}
+
+// A thread's runs on their way into LDS, in four pieces of alike length that stand beside matrix products.
+template <int N>
+struct Unpacked {
+    f16x2 k[N][2][4], v[N][4][2];
+};
+template <int PIECE, int D, int WAVES, int N, bool EXACT>
+__device__ __forceinline__ void unpack(Unpacked<N>& x, Tile<D, EXACT>& to, const Raw<N>& t, const Factors<N>& f, int thread, const CodeBits& bits) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int run = thread + 64 * WAVES * i;
         if (kRuns<D> % (64 * WAVES) != 0 && run >= kRuns<D>) break;
-        {   // keys: a run is 16 elements of one key
-            const int key = run / (D / 16), at = run % (D / 16) * 16;
-            f16x2 step, mid;
-            if constexpr (!EXACT) {
-                const f16x2 sm = as_f16((uint32_t)__shfl((int)kw, key & 63));
-                step = f16x2{sm[0], sm[0]};
-                mid = f16x2{sm[1], sm[1]};
-            }
+        const int key = run / (D / 16), at = run % (D / 16) * 16;    // keys: a run is 16 elements of one key
+        const int four = run / (D / 4), x4 = run % (D / 4);          // values: four elements of four tokens
+        // keys 16 s + 4 q + 0 .. 3 go to places 16 s + 8 (q % 2) + 4 (q / 2) + 0 .. 3
+        const int place = (four & ~3) * 4 + 8 * (four & 1) + 4 * (four >> 1 & 1);
+        if constexpr (PIECE == 0) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f16x2 x[4] = {code_pair<0>(t.k[i][h]), code_pair<1>(t.k[i][h]), code_pair<2>(t.k[i][h]), code_pair<3>(t.k[i][h])};
-                if constexpr (!EXACT)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = __builtin_elementwise_fma(x[e], step, mid);
-                *reinterpret_cast<u32x4*>(&to.k[key][at + 8 * h]) = u32x4{as_bits(x[0]), as_bits(x[1]), as_bits(x[2]), as_bits(x[3])};
+                x.k[i][h][0] = code_pair<0>(t.k[i][h], bits);
+                x.k[i][h][1] = code_pair<1>(t.k[i][h], bits);
+                x.k[i][h][2] = code_pair<2>(t.k[i][h], bits);
+                x.k[i][h][3] = code_pair<3>(t.k[i][h], bits);
             }
         }
-        {   // values: a run is four elements of four tokens
-            const int four = run / (D / 4), x4 = run % (D / 4);
-            f16x2 step[2], mid[2];
-            if constexpr (!EXACT)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f16x2 a = as_f16((uint32_t)__shfl((int)vw, 4 * four + 2 * h)), b = as_f16((uint32_t)__shfl((int)vw, 4 * four + 2 * h + 1));
-                    step[h] = f16x2{a[0], b[0]};
-                    mid[h] = f16x2{a[1], b[1]};
-                }
-            f16x2 x[4][2];
+        if constexpr (PIECE == 1) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                x[0][h] = code_pair<0>(t.v[i][h]);
-                x[1][h] = code_pair<1>(t.v[i][h]);
-                x[2][h] = code_pair<2>(t.v[i][h]);
-                x[3][h] = code_pair<3>(t.v[i][h]);
+                if constexpr (!EXACT)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x.k[i][h][e] = __builtin_elementwise_fma(x.k[i][h][e], f16x2{f.key[i][0], f.key[i][0]}, f16x2{f.key[i][1], f.key[i][1]});
+                *reinterpret_cast<u32x4*>(&to.k[key][at + 8 * h]) = u32x4{as_bits(x.k[i][h][0]), as_bits(x.k[i][h][1]), as_bits(x.k[i][h][2]), as_bits(x.k[i][h][3])};
             }
-            // keys 16 s + 4 q + 0 .. 3 go to places 16 s + 8 (q % 2) + 4 (q / 2) + 0 .. 3
-            const int place = (four & ~3) * 4 + 8 * (four & 1) + 4 * (four >> 1 & 1);
+        }
+        if constexpr (PIECE == 1 || PIECE == 2) {
+            constexpr int h = PIECE - 1;
+            x.v[i][0][h] = code_pair<0>(t.v[i][h], bits);
+            x.v[i][1][h] = code_pair<1>(t.v[i][h], bits);
+            x.v[i][2][h] = code_pair<2>(t.v[i][h], bits);
+            x.v[i][3][h] = code_pair<3>(t.v[i][h], bits);
+        }
+        if constexpr (PIECE == 3) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if constexpr (!EXACT)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) x[e][h] = __builtin_elementwise_fma(x[e][h], step[h], mid[h]);
-                *reinterpret_cast<u32x2*>(&to.v[e * (D / 4) + x4][place]) = u32x2{as_bits(x[e][0]), as_bits(x[e][1])};
+                    for (int h = 0; h < 2; ++h)
+                        x.v[i][e][h] = __builtin_elementwise_fma(x.v[i][e][h], f16x2{f.value[i][2 * h][0], f.value[i][2 * h + 1][0]},
+                                                                 f16x2{f.value[i][2 * h][1], f.value[i][2 * h + 1][1]});
+                *reinterpret_cast<u32x2*>(&to.v[e * (D / 4) + x4][place]) = u32x2{as_bits(x.v[i][e][0]), as_bits(x.v[i][e][1])};
             }
         }
     }
 }
 
-template <int D, bool EXACT, bool MASKED>
-__device__ __forceinline__ void take_tile(Sums<D, EXACT>& r, const Query<D, 32>& q, const Tile<D, EXACT>& t, float f, float up, int k0, int lo, int hi, int lane) {
-    typedef float f32x16 __attribute__((ext_vector_type(16)));
-    const int n = lane & 31, h = lane >> 5;
-    f32x16 s[2];
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Operands come from LDS a group of products ahead of their use.  The compiler would rather read each right before its product, in
+// few registers, and wait for LDS every time: nothing moves over RQ_FENCE, and in a group the reads come first, then products
+// with vector instructions between them.
+constexpr int kValu = 0x2, kMfma = 0x8, kLdsRead = 0x100;
+#define RQ_FENCE() __builtin_amdgcn_sched_barrier(0)
+#define RQ_NEXT(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
+
+// Scores of a tile: products of 32 keys each with the wave's queries, before steps and centres; beside them the next tile is unpacked.
+template <int D, int WAVES, int N, bool EXACT>
+__device__ __forceinline__ void take_keys(f32x16 (&s)[2], const Query<D, 32>& q, const Tile<D, EXACT>& t, Tile<D, EXACT>& to, const Raw<N>& raw,
+                                          const Factors<N>& f, int thread, const CodeBits& bits) {
+    const int n = thread & 31, h = thread >> 5 & 1;
+    constexpr int G = D / 32;                     // groups: of two steps of 16 elements, two blocks of 32 keys
+    f16x8 a[2][2][2];
+    Unpacked<N> x;
+    const auto read = [&](int g) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        s[i] = f32x16{};
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-            const f16x8 a = *reinterpret_cast<const f16x8*>(&t.k[32 * i + n][h * (D / 2) + 8 * j]);
-            s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q.hi[j], s[i], 0, 0, 0);
-            if constexpr (EXACT) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q.lo[j], s[i], 0, 0, 0);
+            for (int i = 0; i < 2; ++i) a[g % 2][j][i] = *reinterpret_cast<const f16x8*>(&t.k[32 * i + n][h * (D / 2) + 8 * (2 * g + j)]);
+    };
+    read(0);
+    s[0] = s[1] = f32x16{};
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        RQ_FENCE();
+        if (g + 1 < G) read(g + 1);
+        if (g == 0) {
+            unpack<0, D, WAVES>(x, to, raw, f, thread, bits);
+            if (G == 2) unpack<1, D, WAVES>(x, to, raw, f, thread, bits);
+        } else if (g == 1) {
+            unpack<G == 2 ? 2 : 1, D, WAVES>(x, to, raw, f, thread, bits);
+            if (G == 2) unpack<3, D, WAVES>(x, to, raw, f, thread, bits);
+        } else if (g == 2) {
+            unpack<2, D, WAVES>(x, to, raw, f, thread, bits);
+        } else {
+            unpack<3, D, WAVES>(x, to, raw, f, thread, bits);
         }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g % 2][j][i], q.hi[2 * g + j], s[i], 0, 0, 0);
+                if constexpr (EXACT) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g % 2][j][i], q.lo[2 * g + j], s[i], 0, 0, 0);
+            }
+        RQ_NEXT(kLdsRead, 4);
+#pragma unroll
+        for (int i = 0; i < (EXACT ? 8 : 4); ++i) {
+            RQ_NEXT(kMfma, 1);
+            RQ_NEXT(kValu, 6);
+        }
+    }
+    RQ_FENCE();
+}
+
+// Scores to probabilities, and their products with the values.
+template <int D, bool EXACT>
+__device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], const Query<D, 32>& q, const Tile<D, EXACT>& t, float f, float up, int k0,
+                                            bool whole, int lo, int seen, int lane) {
+    const int n = lane & 31, h = lane >> 5;
+    constexpr int J = D / 32;
+    f16x8 a[2][J];
+    const auto read = [&](int g) {                // values of 16 keys
+#pragma unroll
+        for (int j = 0; j < J; ++j) a[g % 2][j] = *reinterpret_cast<const f16x8*>(&t.v[32 * j + n][16 * g + 8 * h]);
+    };
+    read(0);
+    RQ_FENCE();
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int key = 32 * i + 2 * e + 4 * h;
+                const f32x4 step = *reinterpret_cast<const f32x4*>(&t.scale[0][key]), mid = *reinterpret_cast<const f32x4*>(&t.scale[1][key]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) s[i][e + u] = fmaf(step[u], s[i][e + u], mid[u] * (q.even + q.odd));
+            }
+    }
+    if (!whole) {
+        const int from = k0 + 4 * h - lo;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[i][e] = (uint32_t)(from + 32 * i + 8 * (e / 4) + e % 4) < (uint32_t)seen ? s[i][e] : -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const int key = 32 * i + 2 * e + 4 * h;
-            f32x4 step, mid;
-            if constexpr (EXACT) {
-                step = *reinterpret_cast<const f32x4*>(&t.scale[0][key]);
-                mid = *reinterpret_cast<const f32x4*>(&t.scale[1][key]);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float x = s[i][e + u];
-                if constexpr (EXACT) x = fmaf(step[u], x, mid[u] * (q.even + q.odd));
-                if constexpr (MASKED) x = k0 + key + u >= lo && k0 + key + u < hi ? x : -INFINITY;
-                s[i][e + u] = x;
-                mx = fmaxf(mx, x);
-            }
-        }
+        for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[i][e]), s[i][e + 1]);
     mx = f * column_max<32>(mx);
     // p may grow to 2^8 before the sums are scaled to a new maximum
     if (__any(mx - r.m > 8.0f)) {
@@ -255,12 +310,12 @@ __device__ __forceinline__ void take_tile(Sums<D, EXACT>& r, const Query<D, 32>&
         r.m = to;
     }
     const float off = (r.m == -INFINITY ? 0.0f : r.m) - up;
-    uint32_t p[2][8];
+    // sixteen keys at a time, the next ones' probabilities beside the products of these
+    uint32_t p[2][4];
+    const auto weigh = [&](int g) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const int key = 32 * i + 2 * e + 4 * h;
+        for (int v = 0; v < 2; ++v) {
+            const int at = 8 * (g % 2) + 4 * v, key = 32 * (g / 2) + 2 * at + 4 * h;
             f32x4 step, mid;
             if constexpr (EXACT) {
                 step = *reinterpret_cast<const f32x4*>(&t.scale[2][key]);
@@ -269,32 +324,43 @@ __device__ __forceinline__ void take_tile(Sums<D, EXACT>& r, const Query<D, 32>&
             float x[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float y = __builtin_amdgcn_exp2f(fmaf(f, s[i][e + u], -off));
-                r.l += y;
-                x[u] = y;
+                x[u] = __builtin_amdgcn_exp2f(fmaf(f, s[g / 2][at + u], -off));
                 if constexpr (EXACT) {
-                    if constexpr (MASKED) {       // a masked key's parameters may be infinite or NaN
-                        const bool seen = s[i][e + u] != -INFINITY;
-                        x[u] = seen ? y * step[u] : 0.0f;
-                        r.w += seen ? y * mid[u] : 0.0f;
-                    } else {
-                        x[u] = y * step[u];
-                        r.w = fmaf(y, mid[u], r.w);
-                    }
+                    r.l += x[u];
+                    r.w = fmaf(x[u], mid[u], r.w);
+                    x[u] *= step[u];
                 }
             }
-            p[i][e / 2] = pack_f16(x[0], x[1]);
-            p[i][e / 2 + 1] = pack_f16(x[2], x[3]);
+            p[g % 2][2 * v] = pack_f16(x[0], x[1]);
+            p[g % 2][2 * v + 1] = pack_f16(x[2], x[3]);
+            if constexpr (!EXACT) {               // (of what the products see: two an instruction)
+                const f16x2 one{(_Float16)1.0f, (_Float16)1.0f};
+                r.l = __builtin_amdgcn_fdot2(as_f16(p[g % 2][2 * v]), one, r.l, false);
+                r.l = __builtin_amdgcn_fdot2(as_f16(p[g % 2][2 * v + 1]), one, r.l, false);
+            }
         }
+    };
+    weigh(0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f16x8 b = __builtin_bit_cast(f16x8, u32x4{p[i / 2][4 * (i % 2)], p[i / 2][4 * (i % 2) + 1], p[i / 2][4 * (i % 2) + 2], p[i / 2][4 * (i % 2) + 3]});
+    for (int g = 0; g < 4; ++g) {
+        RQ_FENCE();
+        if (g < 3) {
+            read(g + 1);
+            weigh(g + 1);
+        }
+        const f16x8 b = __builtin_bit_cast(f16x8, u32x4{p[g % 2][0], p[g % 2][1], p[g % 2][2], p[g % 2][3]});
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-            const f16x8 a = *reinterpret_cast<const f16x8*>(&t.v[32 * j + n][16 * i + 8 * h]);
-            r.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, r.o[j], 0, 0, 0);
+        for (int j = 0; j < J; ++j) r.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[g % 2][j], b, r.o[j], 0, 0, 0);
+        if (g < 3) {
+            RQ_NEXT(kLdsRead, EXACT ? J + 4 : J);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                RQ_NEXT(kMfma, 1);
+                RQ_NEXT(kValu, (EXACT ? 44 : 24) / J);
+            }
         }
     }
+    RQ_FENCE();
 }
 
 // A barrier for what lies in LDS: loads from memory stay under way.
@@ -304,18 +370,20 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int D, int WAVES, bool F16>
+template <int D, int WAVES, bool F16, bool PAGED>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     constexpr bool EXACT = F16;
     constexpr int BM = 32 * WAVES, N = (kRuns<D> + 64 * WAVES - 1) / (64 * WAVES);
-    __shared__ __attribute__((aligned(16))) Tile<D, EXACT> tiles[2];
+    // Eight waves are two groups, four SIMDs each, half a step apart: one has products of keys and unpacks while the other has
+    // exponentials.  Three tiles then, since the one group still reads values of the last while the other unpacks the next.
+    constexpr bool TWO = WAVES == 8;
+    constexpr int TILES = TWO ? 3 : 2;
+    __shared__ __attribute__((aligned(16))) Tile<D, EXACT> tiles[TILES];
     const Kv4Attention& a = job.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = group_index();
-    const int kv = job.cache.kv_heads;
-    const int64_t tc = item / kv;
-    const int head = (int)(item - tc * kv);
-    const int tile_no = (int)(tc / job.chunks), chunk = (int)(tc - (int64_t)tile_no * job.chunks);
+    const int head = blockIdx.x, item = item_number();
+    const int tile_no = job.chunks == 1 ? item : item / job.chunks, chunk = item - tile_no * job.chunks;
+    const CodeBits bits;
     Place at;
     // the last rows of a causal prompt see most: they begin first
     if (tile_no >= job.tiles || !find_rows<BM>(job, job.tiles - 1 - tile_no, at)) return;
@@ -333,13 +401,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
         all_lo = a.window ? p1 - a.window + 1 : 0;
         all_hi = a.causal && p0 + 1 < to ? p0 + 1 : to;
     }
-    const TableRow table = (TableRow)(uintptr_t)(a.table + (int64_t)at.b * a.width);
+    const int32_t* table = a.table + (int64_t)at.b * a.width;
     const int mine = row + (lane & 31);
     const bool there = mine < rows;
     const int token = there ? token_of(job, at, mine) : 0, of = there ? mine - token * job.group : 0;
     const RawQuery<D, 32> raw_q = load_query<D, 32>(job, there, at.q0 + token, head * job.group + of, lane);
-    Raw<N> raw;
-    if (from < to) load_tile<D, WAVES, N>(raw, job.cache, table, head, from, to, threadIdx.x);
+    const int head_at = head * ((D + 8) << job.cache.page_shift);
+    int pages = 0, page_no = 2;                   // page_no: number among those of `pages` of the tile that is asked for next
+    Raw<N> raw, later;                            // the next tile, the one after it
+    if (from < to) {
+        pages = load_pages<PAGED>(job.cache, table, from, kTile, to, lane);
+        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, from, to, threadIdx.x);
+        if (from + kTile < to) load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, 1, head_at, from + kTile, to, threadIdx.x);
+    }
     Query<D, 32> q;
     take_query<D, 32, F16, F16>(q, job, raw_q, lane);
     const int pos = at.len - at.nq + token;
@@ -353,52 +427,60 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) r.o[j][e] = 0.0f;
 
-    Range key_range{0.0f, 1.0f}, value_range{0.0f, 1.0f};
-    // EXACT: p * step; else the elements themselves
-    const auto prepare = [&](int k0, int half, float& key_grew, float& value_grew) {
-        const bool there_k = k0 + lane < to;
-        const float ks = __uint_as_float(raw.kp << 16), km = __uint_as_float(raw.kp & 0xffff0000u);
-        const float vs = __uint_as_float(raw.vp << 16), vm = __uint_as_float(raw.vp & 0xffff0000u);
-        const float kx = fmaf(8.0f, ks, fabsf(km)), vx = EXACT ? vs : fmaf(8.0f, vs, fabsf(vm));
-        if constexpr (!EXACT) widen<15>(key_range, there_k && kx < 0x1p126f ? kx : 0.0f, key_grew);
-        widen<EXACT ? 7 : 15>(value_range, there_k && vx < 0x1p126f ? vx : 0.0f, value_grew);
-        unpack<D, WAVES, N, EXACT>(tiles[half], raw, k0, to, threadIdx.x, key_range, value_range);
-    };
-    float key_grew = 1.0f, value_grew = 1.0f;
-    int half = 0;
-    if (from < to) {
-        prepare(from, 0, key_grew, value_grew);
-        if (from + kTile < to) load_tile<D, WAVES, N>(raw, job.cache, table, head, from + kTile, to, threadIdx.x);
-    }
-    lds_barrier();
-    for (int k0 = from; k0 < to; k0 += kTile) {
+    const int seen = hi > lo ? hi - lo : 0;
+
+    Range keys{0.0f, 0}, values{0.0f, 0};
+    int at_tile = TILES - 1;                      // the tile in hand
+    if (TWO && wave >= 4) lds_barrier();
+    // a step unpacks the next tile and takes this one; the first has none to take
+    for (int k0 = from - kTile; k0 < to; k0 += kTile) {
+        Tile<D, EXACT>& now = tiles[at_tile];
+        at_tile = at_tile == TILES - 1 ? 0 : at_tile + 1;
+        Tile<D, EXACT>& then = tiles[at_tile];
+        const bool mine_too = k0 >= from && k0 < any_hi && k0 + kTile > any_lo;
+        const int next = k0 + kTile;
         // (the tile's own ranges: the next one may widen them)
-        const float f = EXACT ? q.f : q.f / key_range.by;
-        const float up = EXACT ? (value_range.limit > 0.0f ? __builtin_amdgcn_logf(value_range.by) : 0.0f) : 0.0f;
-        value_grew = 1.0f;
-        if (k0 + kTile < to) {
-            prepare(k0 + kTile, half ^ 1, key_grew, value_grew);
-            if (k0 + 2 * kTile < to) load_tile<D, WAVES, N>(raw, job.cache, table, head, k0 + 2 * kTile, to, threadIdx.x);
+        const float f = EXACT ? q.f : __builtin_amdgcn_ldexpf(q.f, -keys.up), up = EXACT ? (float)values.up : 0.0f;
+        int grew = 0;
+        Factors<N> factors{};
+        if (next < to) take_parameters<D, WAVES, N, EXACT>(factors, then, raw, next + lane < to, threadIdx.x, keys, values, grew);
+        f32x16 s[2];
+        if (mine_too) {
+            take_keys<D, WAVES, N, EXACT>(s, q, now, then, raw, factors, threadIdx.x, bits);         // (where there is no next tile, `then` is not read)
+        } else {
+            Unpacked<N> x;
+            unpack<0, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
+            unpack<1, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
+            unpack<2, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
+            unpack<3, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
         }
-        if (k0 < any_hi && k0 + kTile > any_lo) {
-            if (k0 >= all_lo && k0 + kTile <= all_hi) take_tile<D, EXACT, false>(r, q, tiles[half], f, up, k0, lo, hi, lane);
-            else take_tile<D, EXACT, true>(r, q, tiles[half], f, up, k0, lo, hi, lane);
+        raw = later;
+        if (const int ask = next + 2 * kTile; ask < to) {
+            if (page_no == kPagesOf<PAGED>) {
+                pages = load_pages<PAGED>(job.cache, table, ask, kTile, to, lane);
+                page_no = 0;
+            }
+            load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, ask, to, threadIdx.x);
+            ++page_no;
         }
-        if (value_grew != 1.0f) {                 // sums go on in the next tile's range
-            scale_sums(r, value_grew);
+        if constexpr (TWO) lds_barrier();
+        if (mine_too) take_scores<D, EXACT>(r, s, q, now, f, up, k0, k0 >= all_lo && k0 + kTile <= all_hi, lo, seen, lane);
+        if (grew != 0) {                          // sums go on in the next tile's range
+            const float by = __builtin_amdgcn_ldexpf(1.0f, grew);
+            scale_sums(r, by);
             if constexpr (EXACT) {
-                r.l *= value_grew;
-                r.w *= value_grew;
+                r.l *= by;
+                r.w *= by;
             }
         }
-        half ^= 1;
         lds_barrier();
     }
+    if (TWO && wave < 4) lds_barrier();
     if (!there) return;                           // (both lanes of the row)
     const float l = column_sum<32>(r.l), w = EXACT ? column_sum<32>(r.w) : 0.0f;
-    const float by = (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) * (EXACT ? 1.0f : 1.0f / value_range.by);
+    const float by = (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) * (EXACT ? 1.0f : __builtin_amdgcn_ldexpf(1.0f, -values.up));
     float lse = l == 0.0f ? -INFINITY : r.m + __builtin_amdgcn_logf(l);
-    if constexpr (EXACT) lse -= value_range.limit > 0.0f ? __builtin_amdgcn_logf(value_range.by) : 0.0f;
+    if constexpr (EXACT) lse -= (float)values.up;
     const int t_row = at.q0 + token, h_row = head * job.group + of;
     const int64_t part_row = ((int64_t)chunk * a.tokens + t_row) * a.heads + h_row;
     float* part = job.part + part_row * D;
@@ -421,9 +503,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
 
 template <int D, int WAVES>
 void launch(const KvJob& job, hipStream_t s) {
-    const dim3 grid = group_grid((int64_t)job.tiles * job.cache.kv_heads * job.chunks, 64 * WAVES), block(64 * WAVES);
-    if (job.a.dtype == RQ_F16) launch_kernel(k_kv4_prompt<D, WAVES, true>, grid, block, 0, s, job);
-    else launch_kernel(k_kv4_prompt<D, WAVES, false>, grid, block, 0, s, job);
+    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.tiles * job.chunks), block(64 * WAVES);
+    const bool paged = job.cache.page_shift < 6;
+    if (job.a.dtype == RQ_F16 && paged) launch_kernel(k_kv4_prompt<D, WAVES, true, true>, grid, block, 0, s, job);
+    else if (job.a.dtype == RQ_F16) launch_kernel(k_kv4_prompt<D, WAVES, true, false>, grid, block, 0, s, job);
+    else if (paged) launch_kernel(k_kv4_prompt<D, WAVES, false, true>, grid, block, 0, s, job);
+    else launch_kernel(k_kv4_prompt<D, WAVES, false, false>, grid, block, 0, s, job);
 }
 
 }  // namespace

@@ -30,7 +30,21 @@ __device__ __forceinline__ uint32_t pack16(float x, float y) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (x & mask) | bits; }
+
+// What makes codes fp16 numbers: x & even | e1024, x & odd | e64.  Held in registers of whose values the compiler knows nothing: with
+// literals, of which a three-operand instruction takes none, it makes two instructions of each.
+struct CodeBits {
+    uint32_t even, odd, e1024, e64;
+    __device__ __forceinline__ CodeBits() {
+        asm("s_mov_b32 %0, 0x000f000f" : "=s"(even));
+        asm("s_mov_b32 %0, 0x00f000f0" : "=s"(odd));
+        asm("v_mov_b32 %0, 0x64006400" : "=v"(e1024));
+        asm("v_mov_b32 %0, 0x54005400" : "=v"(e64));
+    }
+    // codes in bits 0 .. 3 (1024 + c), 4 .. 7 (64 + c) of both halves
+    __device__ __forceinline__ uint32_t low(uint32_t x) const { return (x & even) | e1024; }
+    __device__ __forceinline__ uint32_t high(uint32_t x) const { return (x & odd) | e64; }
+};
 
 // Sums and maxima over the lanes of a column: of 16 columns lanes n, n + 16, n + 32, n + 48, of 32 columns lanes n, n + 32.
 __device__ __forceinline__ void other_rows(float x, bool far, float& a, float& b) {
@@ -120,7 +134,7 @@ __device__ __forceinline__ void take_query(Query<D, COLUMNS>& r, const KvJob& jo
             for (int e = 0; e < E; ++e) {
                 float y, z;
                 other_rows(q[e], w == 32, y, z);
-                q[e] = lane & w ? y - z : y + z;
+                q[e] = fmaf(lane & w ? -1.0f : 1.0f, z, y);
             }
     }
     // log2(e) and the scale of the scores are in the row, so that f is a power of two and f * (s - m) exact, however large
@@ -187,8 +201,30 @@ __device__ __forceinline__ void store_row(uint16_t* o, const float (&y)[N], bool
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-// Page numbers through the scalar cache: they are the same for all lanes, and a wait for them must not be one for the codes.
-typedef const int32_t __attribute__((address_space(4)))* TableRow;
+// The pages of tiles of 64 keys, read 64 at once, so that no step waits for the table before it can ask for codes.  PAGED: pages of
+// 16 or 32 tokens, the 16 keys of each quarter of a tile in a place of their own, four lanes a tile; else a tile lies in one page,
+// a lane a tile.
+template <bool PAGED>
+constexpr int kPagesOf = PAGED ? 16 : 64;         // tiles
+// The tiles that begin at k0, k0 + stride ...  Keys from `end` on are masked; theirs is the last one's page.
+template <bool PAGED>
+__device__ __forceinline__ int load_pages(const Kv4& c, const int32_t* table, int k0, int stride, int end, int lane) {
+    const int64_t k = PAGED ? k0 + (int64_t)(lane >> 2) * stride + 16 * (lane & 3) : k0 + (int64_t)lane * stride;
+    const int page = table[(k < end ? (int)k : end - 1) >> c.page_shift];
+    return (uint32_t)page < (uint32_t)c.pages ? page : 0;
+}
+// The head's block of the page of quarter `quarter` of tile number n, and its first key's place in the page.  (`head_at`: of the kv
+// head's block in a page)
+template <bool PAGED>
+__device__ __forceinline__ const uint8_t* block_of(const Kv4& c, int pages, int n, int quarter, int head_at) {
+    return c.data + (int64_t)__builtin_amdgcn_readlane(pages, PAGED ? 4 * n + quarter : n) * c.page_bytes + head_at;
+}
+template <bool PAGED>
+__device__ __forceinline__ int place_of(const Kv4& c, int k0, int quarter, int end) {
+    int key = k0 + 16 * quarter;
+    if (PAGED && key >= end) key = (end - 1) & ~15;
+    return key & ((1 << c.page_shift) - 1);
+}
 
 // A tile of BM rows: where they lie, and the positions that they see.
 struct Place {
@@ -198,6 +234,13 @@ struct Place {
 };
 // Row r of a tile's sequence: its token.
 __device__ __forceinline__ int token_of(const KvJob& job, const Place& p, int r) { return p.nq == 1 ? 0 : r / job.group; }
+
+// Grid of `items` workgroups for each kv head, and a workgroup's number in it.
+inline dim3 item_grid(int kv_heads, int64_t items) {
+    const int64_t y = items < 65535 ? items : 65535;
+    return dim3((unsigned)kv_heads, (unsigned)y, (unsigned)((items + y - 1) / y));
+}
+__device__ __forceinline__ int item_number() { return (int)(blockIdx.z * gridDim.y + blockIdx.y); }
 
 // Row tile `tile`: a sequence's tiles begin at floor(q_start * group / BM) + its number.  False where there is none.
 template <int BM>
