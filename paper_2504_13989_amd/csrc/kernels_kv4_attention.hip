@@ -25,12 +25,13 @@
 // two a unit take 109).  The waves take a workgroup's tiles in turn.  A tile's codes are read into the registers of the one before
 // as soon as those are used up, keys during the softmax, values during the next keys' products.
 #include "kv4_attention.h"
-#include <cstdlib>
+
+#include <type_traits>
 
 namespace rq {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kMostWaves = 8;         // of a workgroup; of one that has a row tile to itself while the chip is not full
 
 // Eight key codes as fp16: elements (0, 4), (1, 5), (2, 6), (3, 7) of the dword, 1024 + c in the even ones, 64 + c in the odd ones.
 __device__ __forceinline__ f16x8 key_operand(uint32_t w, const CodeBits& bits) {
@@ -57,12 +58,12 @@ struct Source {
     int at[PAGED ? 4 : 1];
 };
 template <bool PAGED>
-__device__ __forceinline__ Source<PAGED> find_tile(const Kv4& c, int pages, int n, int head_at, int k0, int end) {
+__device__ __forceinline__ Source<PAGED> find_tile(const Kv4& c, int pages, int n, int head_at, int k0) {
     Source<PAGED> s;
 #pragma unroll
     for (int i = 0; i < (PAGED ? 4 : 1); ++i) {
         s.block[i] = block_of<PAGED>(c, pages, n, i, head_at);
-        s.at[i] = place_of<PAGED>(c, k0, i, end);
+        s.at[i] = place_of(c, k0, i);
     }
     return s;
 }
@@ -242,14 +243,15 @@ __device__ __forceinline__ void take_values(Columns<D>& r, const Codes<D>& t, co
     }
 }
 
-// Shares of the row tiles' keys.  Row tile t has tiles of 64 keys numbers begin[t] .. begin[t + 1] - 1; worker i of a kv head takes those
-// from i * each on (a row tile that sees nothing has one, too: its results are zeros).  A share of row tile t that worker i has is number i + t of the partial results: no two shares have one number.
+// Shares of the row tiles' keys.  Row tile t has units begin[t] .. begin[t + 1] - 1: kStart for what a row tile costs besides its keys, then
+// one for each 64 keys (and one where there are none: its results are zeros).  Worker i of a kv head takes units i * each on.  Its
+// share of row tile t is number i + t of the partial results: no two shares have one number.
 constexpr int kMostTiles = 1024;                  // row tiles that are shared out
 struct Shares {
-    int begin[kMostTiles + 1];
+    int begin[kMostTiles + 1], len[kMostTiles];
     int wave_sum[kWaves];
 };
-constexpr int kLeast = 2 * kWaves;                // tiles of 64 keys that a worker takes, if there are as many
+constexpr int kStart = 2 * kWaves, kLeast = kStart + 2 * kWaves;     // kLeast: units of a worker, if there are as many
 
 template <int C>
 __device__ __forceinline__ int share_out(const KvJob& job, Shares& s) {
@@ -260,7 +262,12 @@ __device__ __forceinline__ int share_out(const KvJob& job, Shares& s) {
     for (int i = 0; i < kMostTiles / threads; ++i) {
         const int t = (int)threadIdx.x * each + i;
         Place p;
-        count[i] = i < each && t < job.tiles && find_rows<C>(job, t, p) ? (p.to > p.from ? (p.to - p.from + kTile - 1) / kTile : 1) : 0;
+        count[i] = 0;
+        if (i < each && t < job.tiles && find_rows<C>(job, t, p)) {
+            find_keys<C>(job, p, job.a.kv_lens[p.b]);
+            count[i] = kStart + (p.to > p.from ? (p.to - p.from + kTile - 1) / kTile : 1);
+            s.len[t] = p.len;
+        }
         sum += count[i];
     }
     int before = sum;
@@ -294,13 +301,14 @@ __device__ __forceinline__ int* part_workers(const KvJob& job) {
     return reinterpret_cast<int*>(part_sums<D, C>(job) + (int64_t)(job.workers + job.tiles) * job.cache.kv_heads * C);
 }
 
-template <int D, int F, bool F16, bool PAGED>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
+// SHARED: workers share the keys out, else a workgroup takes a row tile.
+template <int D, int F, bool F16, bool PAGED, int W, bool SHARED>
+__global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
     constexpr int C = 16 / F, E = D / 4;          // rows of the workgroup; elements of a row in a lane
-    __shared__ __attribute__((aligned(16))) float lds_params[kWaves][4 * kTile];
-    __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][D + 4];
-    __shared__ float lds_l[kWaves][16];
-    __shared__ Shares shares;
+    __shared__ __attribute__((aligned(16))) float lds_params[W][4 * kTile];
+    __shared__ __attribute__((aligned(16))) float lds_o[W][16][D + 4];
+    __shared__ float lds_l[W][16];
+    __shared__ std::conditional_t<SHARED, Shares, int> shares;
     const Kv4Attention& a = job.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int copy = (lane & 15) / C, g = lane >> 4;
@@ -308,16 +316,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
     const int head_at = head * ((D + 8) << job.cache.page_shift);    // of the kv head's block in a page
     const CodeBits bits;
     float* lds = lds_params[wave];
-    int tile = number, share = 0, share_end = 1;  // the workgroup's tiles of 64 keys, all row tiles counted
-    if (job.workers) {
+    int tile = number, share = 0, share_end = 1;  // SHARED: the workgroup's units
+    if constexpr (SHARED) {
         const int each = share_out<C>(job, shares);
         share = number * each;
         share_end = share + each < shares.begin[job.tiles] ? share + each : shares.begin[job.tiles];
         if (number == 0 && head == 0)
-            for (int t = threadIdx.x; t < job.tiles; t += 64 * kWaves) {
+            for (int t = threadIdx.x; t < job.tiles; t += 64 * W) {
+                const int begin = shares.begin[t], end = shares.begin[t + 1];
                 int* w = part_workers<D, C>(job) + 2 * t;
-                w[0] = shares.begin[t] / each;
-                w[1] = shares.begin[t + 1] > shares.begin[t] ? (shares.begin[t + 1] - 1) / each : w[0];
+                w[0] = end > begin ? (begin + kStart) / each : 0;
+                w[1] = end > begin ? (end - 1) / each : 0;
             }
         if (share >= share_end) return;           // (also of workers that only fill the grid)
         int lo = 0, hi = job.tiles - 1;           // the last row tile that begins at or before the share
@@ -326,44 +335,46 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
             if (shares.begin[at] <= share) lo = at; else hi = at - 1;
         }
         tile = lo;
-    } else if (tile >= job.tiles) {
-        return;
     }
-    // row tile by row tile; without workers just the one
+    // row tile by row tile; not SHARED: just the one
     for (; tile < job.tiles; ++tile) {
         Place at;
-        int first = 0, count = 0;                 // of the row tile's tiles: those of this workgroup
+        int first = 0, count = 0;                 // of the row tile's tiles of 64 keys: those of this workgroup
         bool all = true;                          // it has all of them
         tile = __builtin_amdgcn_readfirstlane(tile);
-        if (job.workers) {
-            const int begin = shares.begin[tile], end = shares.begin[tile + 1];
+        if constexpr (SHARED) {
+            const int begin = shares.begin[tile], end = shares.begin[tile + 1], keys = begin + kStart;
             if (begin >= share_end) break;
-            first = share > begin ? share - begin : 0;
-            count = (share_end < end ? share_end : end) - begin - first;
-            all = count == end - begin;
+            if (end == begin || share_end <= keys) continue;         // none of its keys
+            first = share > keys ? share - keys : 0;
+            count = (share_end < end ? share_end : end) - keys - first;
+            all = count == end - keys;
         }
-        if (!find_rows<C>(job, tile, at)) {
-            if (!job.workers) return;
-            continue;
-        }
-        const int rows = at.nq * job.group;
-        int from = at.from, to = at.to;
-        if (job.workers) {
-            from += first * kTile;
-            if (to > from + count * kTile) to = from + count * kTile;
-        }
-        const int n = at.base + (lane & 15) % C;
+        if (!find_rows<C>(job, tile, at)) return; // (SHARED: such a tile has no units)
+        const int rows = at.nq * job.group, n = at.base + (lane & 15) % C;
         const bool there = n < rows;
         const int token = there ? token_of(job, at, n) : 0;
+        // everything that does not depend on the length is asked for before it is known
+        int len;
+        if constexpr (SHARED) len = shares.len[tile];
+        else len = a.kv_lens[at.b];
         const RawQuery<D, 16> raw = load_query<D, 16>(job, there, at.q0 + token, head * job.group + (there ? n - token * job.group : 0), lane);
         const int32_t* table = a.table + (int64_t)at.b * a.width;
         const int shift = job.cache.page_shift;
-        constexpr int stride = kWaves * kTile;
-        int k0 = from + wave * kTile, number_of = 0, pages = 0;      // the tile in hand, its number among those of `pages`
+        constexpr int stride = W * kTile;
+        int pages = 0, number_of = 0;             // of the tile in hand: number among those of `pages`
+        if (a.window == 0 && a.width > 0) pages = load_pages<PAGED>(job, table, (first + wave) * kTile, stride, lane);
+        find_keys<C>(job, at, len);
+        int from = at.from, to = at.to;
+        if constexpr (SHARED) {
+            from += first * kTile;
+            if (to > from + count * kTile) to = from + count * kTile;
+        }
+        int k0 = from + wave * kTile;             // the tile in hand
         Codes<D> t;
         if (k0 < to) {
-            pages = load_pages<PAGED>(job.cache, table, k0, stride, to, lane);
-            const Source<PAGED> s = find_tile<PAGED>(job.cache, pages, 0, head_at, k0, to);
+            if (a.window) pages = load_pages<PAGED>(job, table, k0, stride, lane);
+            const Source<PAGED> s = find_tile<PAGED>(job.cache, pages, 0, head_at, k0);
             load_keys<D>(t, s, shift, lane);
             load_values<D>(t, s, shift, lane);
         }
@@ -389,11 +400,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
         while (k0 < to) {
             const int next = k0 + stride;
             if (++number_of == kPagesOf<PAGED> && next < to) {
-                pages = load_pages<PAGED>(job.cache, table, next, stride, to, lane);
+                pages = load_pages<PAGED>(job, table, next, stride, lane);
                 number_of = 0;
             }
             Source<PAGED> s;
-            if (next < to) s = find_tile<PAGED>(job.cache, pages, number_of, head_at, next, to);
+            if (next < to) s = find_tile<PAGED>(job.cache, pages, number_of, head_at, next);
             take_parameters<D>(r, t, lds, k0 + lane < to, lane);
             f32x4 x[4 / F];
             take_keys<D, F, F16>(x, r, t, bits, copy);
@@ -419,16 +430,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
         }
         // the waves' columns, and the copies among them, join in LDS
         __syncthreads();
-        constexpr int per = C * D / (64 * kWaves);                   // results of a thread
+        constexpr int per = C * D / (64 * W) > 0 ? C * D / (64 * W) : 1;  // results of a thread
         const int mine = threadIdx.x * per / D, d = threadIdx.x * per % D;
-        if (at.base + mine < rows) {
+        if (mine < C && at.base + mine < rows) {
             float top = -INFINITY, sum = 0.0f, z[per] = {};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
+            for (int w = 0; w < W; ++w)
 #pragma unroll
                 for (int f = 0; f < F; ++f) top = fmaxf(top, lds_l[w][f * C + mine]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
+            for (int w = 0; w < W; ++w)
 #pragma unroll
                 for (int f = 0; f < F; ++f) {
                     const float l = lds_l[w][f * C + mine];
@@ -437,10 +448,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
 #pragma unroll
                     for (int e = 0; e < per; ++e) z[e] = fmaf(by, lds_o[w][f * C + mine][d + e], z[e]);
                 }
+            const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-            for (int e = 0; e < per; ++e) z[e] = sum == 0.0f ? 0.0f : z[e] / sum;
+            for (int e = 0; e < per; ++e) z[e] *= by;
             const float total = top + __builtin_amdgcn_logf(sum);
-            if (!all) {
+            if (SHARED && !all) {
                 const int64_t slot = ((int64_t)(number + tile) * kv + head) * C + mine;
                 float* o = job.part + slot * D + d;
 #pragma unroll
@@ -452,7 +464,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_attention(KvJob job) {
                 if (d == 0 && a.lse) a.lse[(int64_t)(at.q0 + token_m) * a.heads + h] = total * kLn2;
             }
         }
-        if (!job.workers) return;
+        if constexpr (!SHARED) return;
         __syncthreads();                          // (LDS is written again)
     }
 }
@@ -559,8 +571,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
 
 // How a call is launched.
 struct Plan {
-    int copies;                                   // of the rows among the columns; 0: the kernel for many rows,
-    int waves;                                    // with that many waves
+    int copies;                                   // of the rows among the columns; 0: the kernel for many rows
+    int waves;                                    // of a workgroup
     int tiles, workers, chunk, chunks;
     size_t bytes;                                 // workspace
 };
@@ -572,7 +584,7 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     p.chunks = 1;
     p.chunk = 1 << 30;
     p.copies = mean > 32 ? 0 : mean <= 4 ? 4 : mean <= 8 ? 2 : 1;
-    p.waves = getenv("RQ_PW") ? atoi(getenv("RQ_PW")) : mean <= 512 ? 4 : 8;
+    p.waves = mean <= 512 ? 4 : 8;
     const int bm = p.copies ? 16 / p.copies : 32 * p.waves;
     const int64_t tiles = a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm);
     p.tiles = (int)tiles;
@@ -582,11 +594,14 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
         if (seen < range) range = seen;
     }
     if (p.copies) {
-        // two workgroups a compute unit share the keys out, unless the sequences are short or there are very many of them
-        if (tiles <= kMostTiles && range > kLeast * kTile && tiles * (range / kTile + 1) < INT32_MAX) {
-            p.workers = (int)(((getenv("RQ_W") ? atoi(getenv("RQ_W")) : 2) * num_cu + c.kv_heads - 1) / c.kv_heads);
+        // Two workgroups a compute unit share the keys out.  Not so where sequences are short: joining the shares is a launch more, 4 us,
+        // in which eight waves of one workgroup take 24 tiles of keys.  Nor where there are very many.
+        const bool few = tiles * c.kv_heads <= num_cu;
+        if (tiles <= kMostTiles && range > (few ? 2560 : 1024) && tiles * (range / kTile + kLeast) < INT32_MAX) {
+            p.workers = (int)((2 * num_cu + c.kv_heads - 1) / c.kv_heads);
             p.bytes = ((size_t)(p.workers + p.tiles) * c.kv_heads * (16 / p.copies) * (c.head_dim + 1) + 2 * (size_t)p.tiles) * sizeof(float);
         }
+        p.waves = !p.workers && few ? kMostWaves : kWaves;
         return p;
     }
     // Keys in chunks where the rows alone do not fill the chip, of eight tiles at least.
@@ -603,20 +618,30 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     return p;
 }
 
+template <int D, int F, bool F16, bool PAGED>
+void launch_few(const KvJob& job, const Plan& p, hipStream_t s) {
+    const dim3 grid = item_grid(job.cache.kv_heads, job.workers ? job.workers : job.tiles), block(64 * p.waves);
+    if (job.workers) {
+        launch_kernel(k_kv4_attention<D, F, F16, PAGED, kWaves, true>, grid, block, 0, s, job);
+        launch_kernel(k_kv4_join_shares<D, F, F16>, item_grid(job.cache.kv_heads, job.tiles), dim3(64 * kWaves), 0, s, job);
+    } else if (p.waves == kMostWaves) {
+        launch_kernel(k_kv4_attention<D, F, F16, PAGED, kMostWaves, false>, grid, block, 0, s, job);
+    } else {
+        launch_kernel(k_kv4_attention<D, F, F16, PAGED, kWaves, false>, grid, block, 0, s, job);
+    }
+}
 template <int D, int F, bool F16>
-void launch_few(const KvJob& job, hipStream_t s) {
-    const dim3 block(64 * kWaves), grid = item_grid(job.cache.kv_heads, job.workers ? job.workers : job.tiles);
-    if (job.cache.page_shift >= 6) launch_kernel(k_kv4_attention<D, F, F16, false>, grid, block, 0, s, job);
-    else launch_kernel(k_kv4_attention<D, F, F16, true>, grid, block, 0, s, job);
-    if (job.workers) launch_kernel(k_kv4_join_shares<D, F, F16>, item_grid(job.cache.kv_heads, job.tiles), block, 0, s, job);
+void launch_few(const KvJob& job, const Plan& p, hipStream_t s) {
+    if (job.cache.page_shift < 6) launch_few<D, F, F16, true>(job, p, s);
+    else launch_few<D, F, F16, false>(job, p, s);
 }
 
 template <int D, bool F16>
 int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
     switch (p.copies) {
-        case 4: launch_few<D, 4, F16>(job, s); break;
-        case 2: launch_few<D, 2, F16>(job, s); break;
-        case 1: launch_few<D, 1, F16>(job, s); break;
+        case 4: launch_few<D, 4, F16>(job, p, s); break;
+        case 2: launch_few<D, 2, F16>(job, p, s); break;
+        case 1: launch_few<D, 1, F16>(job, p, s); break;
         default:
             launch_prompt(job, p.waves, s);
             if (p.chunks > 1)

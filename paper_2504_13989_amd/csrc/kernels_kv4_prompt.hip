@@ -39,7 +39,7 @@ constexpr int kRuns = kTile * D / 16;
 
 // The tile from k0 on, number n of `pages`.
 template <int D, int WAVES, int N, bool PAGED>
-__device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, int pages, int n, int head_at, int k0, int end, int thread) {
+__device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, int pages, int n, int head_at, int k0, int thread) {
     const int p = 1 << c.page_shift, lane = thread & 63;
     const uint8_t* w;
     if constexpr (PAGED) {
@@ -49,11 +49,11 @@ __device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, int pages, in
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             block = mine == i ? block_of<PAGED>(c, pages, n, i, head_at) : block;
-            at = mine == i ? place_of<PAGED>(c, k0, i, end) : at;
+            at = mine == i ? place_of(c, k0, i) : at;
         }
         w = block + (uint32_t)(p * D + 4 * (at + (lane & 15)));
     } else {
-        w = block_of<PAGED>(c, pages, n, 0, head_at) + (p * D + 4 * place_of<PAGED>(c, k0, 0, end)) + (uint32_t)(lane * 4);
+        w = block_of<PAGED>(c, pages, n, 0, head_at) + (p * D + 4 * place_of(c, k0, 0)) + (uint32_t)(lane * 4);
     }
     t.kp = *reinterpret_cast<const uint32_t*>(w);
     t.vp = *reinterpret_cast<const uint32_t*>(w + 4 * p);
@@ -63,7 +63,7 @@ __device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, int pages, in
         if (kRuns<D> % (64 * WAVES) != 0 && run >= kRuns<D>) break;
         // (a wave's 64 runs lie in one quarter)
         const int q = PAGED ? __builtin_amdgcn_readfirstlane(run / (kRuns<D> / 4)) : 0;
-        const uint8_t* x = block_of<PAGED>(c, pages, n, q, head_at) + place_of<PAGED>(c, k0, q, end) * (D / 2) + (uint32_t)((PAGED ? run % (kRuns<D> / 4) : run) * 8);
+        const uint8_t* x = block_of<PAGED>(c, pages, n, q, head_at) + place_of(c, k0, q) * (D / 2) + (uint32_t)((PAGED ? run % (kRuns<D> / 4) : run) * 8);
         t.k[i] = *reinterpret_cast<const u32x2*>(x);
         t.v[i] = *reinterpret_cast<const u32x2*>(x + p * (D / 2));
     }
@@ -387,6 +387,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     Place at;
     // the last rows of a causal prompt see most: they begin first
     if (tile_no >= job.tiles || !find_rows<BM>(job, job.tiles - 1 - tile_no, at)) return;
+    find_keys<BM>(job, at, a.kv_lens[at.b]);
     const int rows = at.nq * job.group, row = at.base + 32 * wave;
 
     // the chunk's share of the keys that the workgroup's rows see
@@ -410,9 +411,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     int pages = 0, page_no = 2;                   // page_no: number among those of `pages` of the tile that is asked for next
     Raw<N> raw, later;                            // the next tile, the one after it
     if (from < to) {
-        pages = load_pages<PAGED>(job.cache, table, from, kTile, to, lane);
-        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, from, to, threadIdx.x);
-        if (from + kTile < to) load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, 1, head_at, from + kTile, to, threadIdx.x);
+        pages = load_pages<PAGED>(job, table, from, kTile, lane);
+        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, from, threadIdx.x);
+        if (from + kTile < to) load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, 1, head_at, from + kTile, threadIdx.x);
     }
     Query<D, 32> q;
     take_query<D, 32, F16, F16>(q, job, raw_q, lane);
@@ -457,10 +458,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
         raw = later;
         if (const int ask = next + 2 * kTile; ask < to) {
             if (page_no == kPagesOf<PAGED>) {
-                pages = load_pages<PAGED>(job.cache, table, ask, kTile, to, lane);
+                pages = load_pages<PAGED>(job, table, ask, kTile, lane);
                 page_no = 0;
             }
-            load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, ask, to, threadIdx.x);
+            load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, ask, threadIdx.x);
             ++page_no;
         }
         if constexpr (TWO) lds_barrier();

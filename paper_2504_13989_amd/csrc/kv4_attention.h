@@ -84,7 +84,8 @@ struct Query {
     float f;                                      // log2 of e^(scale q.k) for a unit of hi.k, a power of two
 };
 
-// A lane's part of a row as it is stored; zeros where there is none.
+// What a lane loads of a row.  Rows that are to be rotated are operands of products with H: lane g of a column has elements
+// 8 L s + 8 g + 0 .. 7 (L lanes a column) for s = 0, 1 ...; others lie as Query wants them.  Zeros where there is no row.
 template <int D, int COLUMNS>
 struct RawQuery {
     u32x4 w[D * COLUMNS / 512];
@@ -92,19 +93,64 @@ struct RawQuery {
 template <int D, int COLUMNS>
 __device__ __forceinline__ RawQuery<D, COLUMNS> load_query(const KvJob& job, bool there, int token, int head, int lane) {
     const Kv4Attention& a = job.a;
-    constexpr int E = Query<D, COLUMNS>::E;
+    constexpr int E = Query<D, COLUMNS>::E, L = 64 / COLUMNS;
     RawQuery<D, COLUMNS> raw{};
-    const uint16_t* x = static_cast<const uint16_t*>(a.q) + (int64_t)token * a.q_token + (int64_t)head * a.q_head + E * (lane / COLUMNS);
+    const int g = lane / COLUMNS, first = a.rotate ? 8 * g : E * g, step = a.rotate ? 8 * L : 8;
+    const uint16_t* x = static_cast<const uint16_t*>(a.q) + (int64_t)token * a.q_token + (int64_t)head * a.q_head + first;
     if (there) {
         if (job.wide_q) {
 #pragma unroll
-            for (int e = 0; e < E / 8; ++e) raw.w[e] = reinterpret_cast<const u32x4*>(x)[e];
+            for (int e = 0; e < E / 8; ++e) raw.w[e] = *reinterpret_cast<const u32x4*>(x + e * step);
         } else {
 #pragma unroll
-            for (int e = 0; e < E; e += 2) raw.w[e / 8][e / 2 % 4] = (uint32_t)x[e] | ((uint32_t)x[e + 1] << 16);
+            for (int e = 0; e < E; e += 2) raw.w[e / 8][e / 2 % 4] = (uint32_t)x[e / 8 * step + e % 8] | ((uint32_t)x[e / 8 * step + e % 8 + 1] << 16);
         }
     }
     return raw;
+}
+
+// H x (fp32) of the columns' rows on the matrix cores, laid out as Query wants them.  H[i, j] = (-1)^popcount(i & j); an operand's signs
+// are those of its eight elements' low bits times one sign for the rest of the index, which is a product of a part that
+// depends on the step and one that depends on the tile.
+template <int D, int COLUMNS, bool F16>
+__device__ __forceinline__ void rotate_query(float (&q)[D * COLUMNS / 64], const RawQuery<D, COLUMNS>& raw, int lane) {
+    constexpr int R = COLUMNS == 16 ? 4 : 16, T = D * COLUMNS / 64 / R;   // results of a lane in a tile, tiles
+    constexpr int S = D * COLUMNS / 512, K = D / S;                  // steps, elements of a step
+    constexpr uint32_t minus = 0x80008000u, one = F16 ? 0x3c003c00u : 0x3f803f80u;
+    asm volatile("" : "+v"(lane));                // (in a loop over row tiles the signs are not to be kept in registers)
+    const int m = lane % COLUMNS, g = lane / COLUMNS;
+    // row m of tile t is element `mine` + R' t of the rotated row: what lane m / 4 (mod lanes of a column) is to hold
+    constexpr int lanes = 64 / COLUMNS;
+    const int mine = (m >> 2) % lanes * (D / lanes) + (COLUMNS == 16 ? 0 : (m >> 3) * 4) + (m & 3);
+    const auto sign = [](int x) { return __builtin_popcount((unsigned)x) & 1 ? minus : 0u; };
+    uint32_t by_step[S], by_tile[T];
+#pragma unroll
+    for (int s = 0; s < S; ++s) by_step[s] = sign(mine & (K * s));
+#pragma unroll
+    for (int t = 0; t < T; ++t) by_tile[t] = sign((mine + R * t) & (8 * g));
+    const uint32_t low = one ^ (m & 1 ? 0x80000000u : 0u);
+    const uint32_t high = one ^ (m & 2 ? 0x8000u : 0u) ^ (((m >> 1) ^ m) & 1 ? 0x80000000u : 0u);
+    const uint32_t four = COLUMNS == 16 ? 0u : (m & 8 ? minus : 0u);
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        float __attribute__((ext_vector_type(R))) y = {};
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            uint32_t x = by_step[s] ^ by_tile[t];
+            if (__builtin_popcount((unsigned)((R * t) & (K * s))) & 1) x ^= minus;
+            const uint32_t other = COLUMNS == 16 ? (t & 1 ? x ^ minus : x) : x ^ four;
+            const u32x4 a{low ^ x, high ^ x, low ^ other, high ^ other};
+            if constexpr (COLUMNS == 16) {
+                if constexpr (F16) y = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, raw.w[s]), y, 0, 0, 0);
+                else y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, raw.w[s]), y, 0, 0, 0);
+            } else {
+                if constexpr (F16) y = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, raw.w[s]), y, 0, 0, 0);
+                else y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, raw.w[s]), y, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < R; ++e) q[R * t + e] = y[e];
+    }
 }
 
 // Rotates a row, scales it by a power of two and rounds it.
@@ -113,29 +159,14 @@ __device__ __forceinline__ void take_query(Query<D, COLUMNS>& r, const KvJob& jo
     const Kv4Attention& a = job.a;
     constexpr int E = Query<D, COLUMNS>::E;
     float q[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const uint32_t u = raw.w[e / 8][e / 2 % 4];
-        q[e] = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(e % 2 ? u >> 16 : u)) : __uint_as_float(e % 2 ? u & 0xffff0000u : u << 16);
-    }
     if (a.rotate) {
+        rotate_query<D, COLUMNS, F16>(q, raw, lane);
+    } else {
 #pragma unroll
-        for (int w = 1; w < E; w *= 2)
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (!(e & w)) {
-                    const float y = q[e], z = q[e + w];
-                    q[e] = y + z;
-                    q[e + w] = y - z;
-                }
-#pragma unroll
-        for (int w = COLUMNS; w < 64; w *= 2)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float y, z;
-                other_rows(q[e], w == 32, y, z);
-                q[e] = fmaf(lane & w ? -1.0f : 1.0f, z, y);
-            }
+        for (int e = 0; e < E; ++e) {
+            const uint32_t u = raw.w[e / 8][e / 2 % 4];
+            q[e] = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(e % 2 ? u >> 16 : u)) : __uint_as_float(e % 2 ? u & 0xffff0000u : u << 16);
+        }
     }
     // log2(e) and the scale of the scores are in the row, so that f is a power of two and f * (s - m) exact, however large
     const float unit = a.scale * kLog2e * (a.rotate ? (D == 128 ? 0.08838834764831845f : 0.125f) : 1.0f);
@@ -206,12 +237,14 @@ __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0
 // a lane a tile.
 template <bool PAGED>
 constexpr int kPagesOf = PAGED ? 16 : 64;         // tiles
-// The tiles that begin at k0, k0 + stride ...  Keys from `end` on are masked; theirs is the last one's page.
+// The tiles that begin at k0, k0 + stride ...  Keys behind the sequence's last one are masked: whatever the table has for them is
+// a page or, as numbers that are none, stands for page 0.
 template <bool PAGED>
-__device__ __forceinline__ int load_pages(const Kv4& c, const int32_t* table, int k0, int stride, int end, int lane) {
+__device__ __forceinline__ int load_pages(const KvJob& job, const int32_t* table, int k0, int stride, int lane) {
     const int64_t k = PAGED ? k0 + (int64_t)(lane >> 2) * stride + 16 * (lane & 3) : k0 + (int64_t)lane * stride;
-    const int page = table[(k < end ? (int)k : end - 1) >> c.page_shift];
-    return (uint32_t)page < (uint32_t)c.pages ? page : 0;
+    const int64_t at = k >> job.cache.page_shift;
+    const int page = table[at < job.a.width ? at : job.a.width - 1];
+    return (uint32_t)page < (uint32_t)job.cache.pages ? page : 0;
 }
 // The head's block of the page of quarter `quarter` of tile number n, and its first key's place in the page.  (`head_at`: of the kv
 // head's block in a page)
@@ -219,14 +252,9 @@ template <bool PAGED>
 __device__ __forceinline__ const uint8_t* block_of(const Kv4& c, int pages, int n, int quarter, int head_at) {
     return c.data + (int64_t)__builtin_amdgcn_readlane(pages, PAGED ? 4 * n + quarter : n) * c.page_bytes + head_at;
 }
-template <bool PAGED>
-__device__ __forceinline__ int place_of(const Kv4& c, int k0, int quarter, int end) {
-    int key = k0 + 16 * quarter;
-    if (PAGED && key >= end) key = (end - 1) & ~15;
-    return key & ((1 << c.page_shift) - 1);
-}
+__device__ __forceinline__ int place_of(const Kv4& c, int k0, int quarter) { return (k0 + 16 * quarter) & ((1 << c.page_shift) - 1); }
 
-// A tile of BM rows: where they lie, and the positions that they see.
+// A tile of BM rows: where they lie, and (once find_keys has been asked) the positions that they see.
 struct Place {
     int b, q0, nq, base;                          // sequence, its first token, its tokens, the tile's first row
     int len;                                      // positions of the sequence
@@ -267,16 +295,19 @@ __device__ __forceinline__ bool find_rows(const KvJob& job, int tile, Place& p) 
         first = p.b * each;
     }
     p.base = (tile - first) * BM;
+    return p.base >= 0 && p.base < p.nq * job.group;
+}
+// len: kv_lens of the sequence
+template <int BM>
+__device__ __forceinline__ void find_keys(const KvJob& job, Place& p, int len) {
+    const Kv4Attention& a = job.a;
     const int rows = p.nq * job.group;
-    if (p.base < 0 || p.base >= rows) return false;
-    const int len = a.kv_lens[p.b];
     p.len = len < 0 ? 0 : len > a.max_len ? (int)a.max_len : len;          // (max_len <= width * page size)
     const int last = (p.base + BM < rows ? p.base + BM : rows) - 1;
     const int p0 = p.len - p.nq + token_of(job, p, p.base), p1 = p.len - p.nq + token_of(job, p, last);
     const int from = a.window ? p0 - a.window + 1 : 0;
     p.from = (from < 0 ? 0 : from) & ~(kTile - 1);
     p.to = a.causal && p1 + 1 < p.len ? p1 + 1 : p.len;
-    return true;
 }
 
 }  // namespace
