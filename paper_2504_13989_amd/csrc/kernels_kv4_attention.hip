@@ -526,15 +526,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join_shares(KvJob job) {
     }
 }
 
-// Joins the chunks of a row of the kernel for many: a workgroup a row, the waves take the chunks in turn.  Partial results:
-// [chunks][tokens][heads], D values each, and behind them log2 of the sums.
+// Joins the chunks of a row of the kernel for many: a wave a row.  Partial results: [chunks][tokens][heads], D values each, and
+// behind them log2 of the sums.
 template <int D, bool F16>
 __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
     constexpr int per = D / 64;
-    __shared__ float lds_o[kWaves][D], lds_l[kWaves];
     const Kv4Attention& a = job.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = group_index(), rows = (int64_t)a.tokens * a.heads;
+    const int lane = threadIdx.x & 63;
+    const int64_t row = group_index() * kWaves + (threadIdx.x >> 6), rows = (int64_t)a.tokens * a.heads;
     if (row >= rows) return;
     const float* sums = job.part + (int64_t)job.chunks * rows * D + row;
     float top = -INFINITY;
@@ -543,7 +542,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
     for (int w = 1; w < 64; w *= 2) top = fmaxf(top, __shfl_xor(top, w));
     float all = 0.0f, y[per] = {};
 #pragma unroll 4
-    for (int c = wave; c < job.chunks; c += kWaves) {
+    for (int c = 0; c < job.chunks; ++c) {
         const float l = sums[c * rows];
         const float by = l == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(l - top);
         const float* o = job.part + (c * rows + row) * D + lane * per;
@@ -551,22 +550,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
 #pragma unroll
         for (int e = 0; e < per; ++e) y[e] = fmaf(by, o[e], y[e]);
     }
-#pragma unroll
-    for (int e = 0; e < per; ++e) lds_o[wave][lane * per + e] = y[e];
-    if (lane == 0) lds_l[wave] = all;
-    __syncthreads();
-    all = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) all += lds_l[w];
     const int64_t token = row / a.heads;
     const int h = (int)(row - token * a.heads);
-    if (threadIdx.x < D) {
-        float z = 0.0f;
+    const float by = all == 0.0f ? 0.0f : 1.0f / all;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) z += lds_o[w][threadIdx.x];
-        static_cast<uint16_t*>(a.o)[token * a.o_token + (int64_t)h * a.o_head + threadIdx.x] = (uint16_t)pack16<F16>(all == 0.0f ? 0.0f : z / all, 0.0f);
-    }
-    if (threadIdx.x == 0 && a.lse) a.lse[row] = (top + __builtin_amdgcn_logf(all)) * kLn2;
+    for (int e = 0; e < per; ++e) y[e] *= by;
+    store_row<per, F16>(static_cast<uint16_t*>(a.o) + token * a.o_token + (int64_t)h * a.o_head + lane * per, y, job.wide_o);
+    if (lane == 0 && a.lse) a.lse[row] = (top + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
 // How a call is launched.
@@ -584,9 +574,13 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     p.chunks = 1;
     p.chunk = 1 << 30;
     p.copies = mean > 32 ? 0 : mean <= 4 ? 4 : mean <= 8 ? 2 : 1;
-    p.waves = mean <= 512 ? 4 : 8;
+    // many rows: eight waves a workgroup unpack a key for twice as many rows, four leave a compute unit with two workgroups
+    // that do not wait for each other: better until there are three rounds of the others (2048 x 2048, 32 heads of their own:
+    // 69 us and not 80)
+    const auto tiles_of = [&](int bm) { return a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm); };
+    p.waves = tiles_of(256) * c.kv_heads >= 3 * num_cu ? 8 : 4;
     const int bm = p.copies ? 16 / p.copies : 32 * p.waves;
-    const int64_t tiles = a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm);
+    const int64_t tiles = tiles_of(bm);
     p.tiles = (int)tiles;
     int64_t range = a.max_len;                    // keys of a row tile at most
     if (a.window) {
@@ -604,16 +598,12 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
         p.waves = !p.workers && few ? kMostWaves : kWaves;
         return p;
     }
-    // Keys in chunks where the rows alone do not fill the chip, of eight tiles at least.
-    const int64_t groups = tiles * c.kv_heads, want = (2 * num_cu + groups - 1) / groups;
-    int64_t chunk = (range + want - 1) / want;
-    chunk = chunk < 8 * kTile ? 8 * kTile : chunk;
-    chunk = (chunk + kTile - 1) / kTile * kTile;
-    const int64_t chunks = (range + chunk - 1) / chunk;
+    // Keys in chunks where the rows alone do not fill the chip, of sixteen tiles at least (joining them is a launch more).
+    const int64_t want = 2 * num_cu / (tiles * c.kv_heads), most = range / (16 * kTile), chunks = want < most ? want : most;
     if (chunks > 1) {
-        p.chunk = (int)chunk;
-        p.chunks = (int)chunks;
-        p.bytes = (size_t)chunks * a.tokens * a.heads * (c.head_dim + 1) * sizeof(float);
+        p.chunk = (int)((range + chunks * kTile - 1) / (chunks * kTile) * kTile);
+        p.chunks = (int)((range + p.chunk - 1) / p.chunk);
+        p.bytes = (size_t)p.chunks * a.tokens * a.heads * (c.head_dim + 1) * sizeof(float);
     }
     return p;
 }
@@ -645,7 +635,7 @@ int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
         default:
             launch_prompt(job, p.waves, s);
             if (p.chunks > 1)
-                launch_kernel(k_kv4_join<D, F16>, group_grid((int64_t)job.a.tokens * job.a.heads, 64 * kWaves), dim3(64 * kWaves), 0, s, job);
+                launch_kernel(k_kv4_join<D, F16>, group_grid(((int64_t)job.a.tokens * job.a.heads + kWaves - 1) / kWaves, 64 * kWaves), dim3(64 * kWaves), 0, s, job);
     }
     return launch_rc();
 }
