@@ -514,15 +514,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join_shares(KvJob job) {
         }
         const int token = token_of(job, at, n), h = head * job.group + n - token * job.group;
         static_cast<uint16_t*>(a.o)[(int64_t)(at.q0 + token) * a.o_token + (int64_t)h * a.o_head + x % D] = (uint16_t)pack16<F16>(all == 0.0f ? 0.0f : y / all, 0.0f);
-        // (every lane of the row's first wave has its maximum; the others take it from LDS)
-        if (x % D == 0 && a.lse) lds_l[0][row] = all;
     }
-    if (a.lse) {
-        __syncthreads();
-        if (wave == 0 && d == 0 && at.base + mine < rows) {
-            const int n = at.base + mine, token = token_of(job, at, n), h = head * job.group + n - token * job.group;
-            a.lse[(int64_t)(at.q0 + token) * a.heads + h] = (top + __builtin_amdgcn_logf(lds_l[0][mine])) * kLn2;
-        }
+    if (a.lse && wave == 0 && d == 0 && at.base + mine < rows) {        // (a lane that begins a row has its maximum)
+        const int n = at.base + mine, token = token_of(job, at, n), h = head * job.group + n - token * job.group;
+        float all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += lds_l[w][mine];
+        a.lse[(int64_t)(at.q0 + token) * a.heads + h] = (top + __builtin_amdgcn_logf(all)) * kLn2;
     }
 }
 
