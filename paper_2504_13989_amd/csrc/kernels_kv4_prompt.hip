@@ -84,11 +84,10 @@ struct Range {
     float limit;
     int up;                                       // log2 of the factor, 2^UP / limit
 };
-// By how much the factor's log2 changed.  UP: 15 for elements, whose fp16 then has full precision down to 2^-29 of the largest; 7
-// for steps, which meet factors of up to 2^8.
+// Widens to hold the wave's `x`; by how much the factor's log2 changed.  UP: 15 for elements, whose fp16 then has full precision down
+// to 2^-29 of the largest; 7 for steps, which meet factors of up to 2^8.
 template <int UP>
 __device__ __forceinline__ int widen(Range& r, float x) {
-    if (!__any(x > r.limit)) return 0;
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) x = fmaxf(x, __shfl_xor(x, w));
     int e = (int)(__float_as_uint(x) >> 23) - 126;                   // x < 2^e
@@ -114,42 +113,57 @@ __device__ __forceinline__ void scale_sums(Sums<D, EXACT>& r, float by) {
         for (int e = 0; e < 16; ++e) r.o[j][e] *= by;
 }
 
-// What a thread needs of a tile's parameters to unpack its runs.
+// A tile's parameters, a key a lane: steps and centres.
+struct Parameters {
+    float ks, km, vs, vm;
+};
+// Ranges widen to hold them.
+template <int D, bool EXACT>
+__device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32_t kp, uint32_t vp, int thread, Range& keys, Range& values, int& grew) {
+    Parameters p{__uint_as_float(kp << 16), __uint_as_float(kp & 0xffff0000u), __uint_as_float(vp << 16), __uint_as_float(vp & 0xffff0000u)};
+    if (!finite(p.vs) || !finite(p.vm)) {
+        p.vs = p.vm = 0.0f;
+        p.ks = __builtin_nanf("");
+    }
+    float kx = EXACT ? 0.0f : fmaf(8.0f, p.ks, fabsf(p.km)), vx = EXACT ? p.vs : fmaf(8.0f, p.vs, fabsf(p.vm));
+    kx = kx < 0x1p126f ? kx : 0.0f;
+    vx = vx < 0x1p126f ? vx : 0.0f;
+    grew = 0;
+    if (__any(kx > keys.limit || vx > values.limit)) {
+        if (!EXACT) widen<15>(keys, kx);
+        grew = widen<EXACT ? 7 : 15>(values, vx);
+    }
+    if constexpr (EXACT) {
+        // (a wave an array: all of them hold the parameters)
+        const int lane = thread & 63;
+        if (thread >> 6 == 0) to.scale[0][lane] = p.ks;
+        if (thread >> 6 == 1) to.scale[1][lane] = p.km;
+        if (thread >> 6 == 2) to.scale[2][lane] = p.vs;
+        if (thread >> 6 == 3) to.scale[3][lane] = p.vm;
+    }
+    return p;
+}
+
+// What a thread needs of them to unpack its runs.
 template <int N>
 struct Factors {
     f16x2 key[N], value[N][4];                    // step and centre
 };
-// The parameters of a tile's keys, a key a lane: ranges widen to hold them, and the lanes get those of their runs.
 template <int D, int WAVES, int N, bool EXACT>
-__device__ __forceinline__ void take_parameters(Factors<N>& f, Tile<D, EXACT>& to, const Raw<N>& t, bool there, int thread, Range& keys, Range& values, int& grew) {
-    const int lane = thread & 63;
-    const uint32_t kp = there ? t.kp : 0u, vp = there ? t.vp : 0u;
-    float ks = __uint_as_float(kp << 16), km = __uint_as_float(kp & 0xffff0000u);
-    float vs = __uint_as_float(vp << 16), vm = __uint_as_float(vp & 0xffff0000u);
-    if (!finite(vs) || !finite(vm)) {
-        vs = vm = 0.0f;
-        ks = __builtin_nanf("");
-    }
-    const float kx = fmaf(8.0f, ks, fabsf(km)), vx = EXACT ? vs : fmaf(8.0f, vs, fabsf(vm));
-    grew = widen<EXACT ? 7 : 15>(values, vx < 0x1p126f ? vx : 0.0f);
-    if constexpr (EXACT) {
-        // (a wave an array: all of them hold the parameters)
-        if (thread >> 6 == 0) to.scale[0][lane] = ks;
-        if (thread >> 6 == 1) to.scale[1][lane] = km;
-        if (thread >> 6 == 2) to.scale[2][lane] = vs;
-        if (thread >> 6 == 3) to.scale[3][lane] = vm;
-    } else {
-        widen<15>(keys, kx < 0x1p126f ? kx : 0.0f);
-        const int kw = (int)pack_f16(__builtin_amdgcn_ldexpf(ks, keys.up), __builtin_amdgcn_ldexpf(km, keys.up));
-        const int vw = (int)pack_f16(__builtin_amdgcn_ldexpf(vs, values.up), __builtin_amdgcn_ldexpf(vm, values.up));
+__device__ __forceinline__ Factors<N> factors_of(const Parameters& p, int thread, const Range& keys, const Range& values) {
+    Factors<N> f{};
+    if constexpr (!EXACT) {
+        const int kw = (int)pack_f16(__builtin_amdgcn_ldexpf(p.ks, keys.up), __builtin_amdgcn_ldexpf(p.km, keys.up));
+        const int vw = (int)pack_f16(__builtin_amdgcn_ldexpf(p.vs, values.up), __builtin_amdgcn_ldexpf(p.vm, values.up));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int run = thread + 64 * WAVES * i;
-            f.key[i] = as_f16((uint32_t)__shfl(kw, run / (D / 16) & 63));
+            f.key[i] = as_f16((uint32_t)__builtin_amdgcn_ds_bpermute(4 * (run / (D / 16) & 63), kw));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f.value[i][e] = as_f16((uint32_t)__shfl(vw, (4 * (run / (D / 4)) + e) & 63));
+            for (int e = 0; e < 4; ++e) f.value[i][e] = as_f16((uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((4 * (run / (D / 4)) + e) & 63), vw));
         }
     }
+    return f;
 }
 
 // A thread's runs on their way into LDS, in four pieces of alike length that stand beside matrix products.
@@ -408,15 +422,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     const int token = there ? token_of(job, at, mine) : 0, of = there ? mine - token * job.group : 0;
     const RawQuery<D, 32> raw_q = load_query<D, 32>(job, there, at.q0 + token, head * job.group + of, lane);
     const int head_at = head * ((D + 8) << job.cache.page_shift);
-    int pages = 0, page_no = 2;                   // page_no: number among those of `pages` of the tile that is asked for next
+    int pages = 0, page_no = 0, asked = from;     // the tile asked for last, its number among those of `pages`
     Raw<N> raw, later;                            // the next tile, the one after it
     if (from < to) {
         pages = load_pages<PAGED>(job, table, from, kTile, lane);
         load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, from, threadIdx.x);
-        if (from + kTile < to) load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, 1, head_at, from + kTile, threadIdx.x);
+        if (from + kTile < to) {
+            asked += kTile;
+            page_no = 1;
+        }
+        load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, asked, threadIdx.x);
     }
     Query<D, 32> q;
     take_query<D, 32, F16, F16>(q, job, raw_q, lane);
+    // all that was asked for is here by now: said once, it is not waited for by name in every step (vmcnt(0); other counts stay)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     const int pos = at.len - at.nq + token;
     const int hi = !there ? 0 : a.causal ? (pos + 1 < at.len ? pos + 1 : at.len) : at.len;
     const int lo = a.window ? (pos - a.window + 1 > 0 ? pos - a.window + 1 : 0) : 0;
@@ -434,7 +454,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     int at_tile = TILES - 1;                      // the tile in hand
     if (TWO && wave >= 4) lds_barrier();
     // a step unpacks the next tile and takes this one; the first has none to take
-    for (int k0 = from - kTile; k0 < to; k0 += kTile) {
+    // (two steps a pass, each with registers of its own for what is under way: copies would wait for it.  A tile is asked for in
+    // every step, the last one again at the end: where a load may be left out, what was loaded before it is waited for with all else.)
+    const auto step = [&](int k0, Raw<N>& raw) {
         Tile<D, EXACT>& now = tiles[at_tile];
         at_tile = at_tile == TILES - 1 ? 0 : at_tile + 1;
         Tile<D, EXACT>& then = tiles[at_tile];
@@ -442,29 +464,33 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
         const int next = k0 + kTile;
         // (the tile's own ranges: the next one may widen them)
         const float f = EXACT ? q.f : __builtin_amdgcn_ldexpf(q.f, -keys.up), up = EXACT ? (float)values.up : 0.0f;
-        int grew = 0;
-        Factors<N> factors{};
-        if (next < to) take_parameters<D, WAVES, N, EXACT>(factors, then, raw, next + lane < to, threadIdx.x, keys, values, grew);
+        const bool there = next + lane < to;
+        int grew;
+        const Parameters of_next = take_parameters<D, EXACT>(then, there ? raw.kp : 0u, there ? raw.vp : 0u, threadIdx.x, keys, values, grew);
         f32x16 s[2];
         if (mine_too) {
+            const Factors<N> factors = factors_of<D, WAVES, N, EXACT>(of_next, threadIdx.x, keys, values);
             take_keys<D, WAVES, N, EXACT>(s, q, now, then, raw, factors, threadIdx.x, bits);         // (where there is no next tile, `then` is not read)
         } else {
+            const Factors<N> factors = factors_of<D, WAVES, N, EXACT>(of_next, threadIdx.x, keys, values);
             Unpacked<N> x;
             unpack<0, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
             unpack<1, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
             unpack<2, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
             unpack<3, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
         }
-        raw = later;
-        if (const int ask = next + 2 * kTile; ask < to) {
-            if (page_no == kPagesOf<PAGED>) {
-                pages = load_pages<PAGED>(job, table, ask, kTile, lane);
+        if (asked + kTile < to) {
+            asked += kTile;
+            if (++page_no == kPagesOf<PAGED>) {
+                pages = load_pages<PAGED>(job, table, asked, kTile, lane);
                 page_no = 0;
             }
-            load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, ask, threadIdx.x);
-            ++page_no;
         }
-        if constexpr (TWO) lds_barrier();
+        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, page_no, head_at, asked, threadIdx.x);
+        if constexpr (TWO) {                      // (products of keys go first where both groups have something to issue: 1 %)
+            lds_barrier();
+            __builtin_amdgcn_s_setprio(0);
+        }
         if (mine_too) take_scores<D, EXACT>(r, s, q, now, f, up, k0, k0 >= all_lo && k0 + kTile <= all_hi, lo, seen, lane);
         if (grew != 0) {                          // sums go on in the next tile's range
             const float by = __builtin_amdgcn_ldexpf(1.0f, grew);
@@ -475,6 +501,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
             }
         }
         lds_barrier();
+        if constexpr (TWO) __builtin_amdgcn_s_setprio(1);
+    };
+    for (int k0 = from - kTile; from < to && k0 < to; k0 += 2 * kTile) {
+        step(k0, raw);
+        step(k0 + kTile, later);                  // (where there is no such tile nothing is taken)
     }
     if (TWO && wave < 4) lds_barrier();
     if (!there) return;                           // (both lanes of the row)
