@@ -3,7 +3,7 @@
 //
 // With k_jd = (c_jd - 7.5) step_j + mid_j the scores are  q_i . k_j = step_j (q_i . c_j - 7.5 sum q_i) + mid_j sum q_i:  the codes
 // themselves are an operand of the matrix cores and a key's step and centre are applied once a score, not once an element.  The
-// values' side is alike: with p'_ij = p_ij step_j,  o_i = sum_j p'_ij (c_jd - 8) + sum_j p_ij (mid_j + step_j / 2).
+// values' side is alike: with p'_ij = p_ij step_j,  o_i = sum_j p'_ij (c_jd - 8 + mid_j / step_j + 1 / 2).
 //   - A code becomes an fp16 number by masking it into the mantissa of 1024 or 64: two codes an instruction.  The constants' share
 //     is known and taken off in fp32: for keys in the accumulator's initial value; for values, whose sums run over all keys and would lose
 //     digits to it, tile by tile, by a second product with the constant.
@@ -11,6 +11,7 @@
 //     where that alone is more than an fp16 result's rounding, as rotated queries', it is two fp16 numbers.
 //   - p' is rounded to fp16 too (bf16 would leave 1.4e-3 of error in outputs that fp16 holds to 2e-4): p carries a power of two that
 //     brings the largest step seen so far to 2^7, so that p' neither overflows nor, down to 2^-21 of the largest, loses digits.
+//     The centres' share is summed in fp32 from p' as it was rounded: what the codes and a centre make together is off by p's rounding.
 //
 // Products are taken transposed, keys x queries and elements x queries, so that a query is a column, column n the lanes n, n + 16,
 // n + 32, n + 48: scores leave the matrix cores in the lanes in which p' enters them again (keys in an order of their own,
@@ -104,14 +105,17 @@ __device__ __forceinline__ void load_values(Codes<D>& t, const Source<PAGED>& s,
     }
 }
 
+constexpr int kParameters = 5;                    // of a key in LDS
+
 // The columns of a wave, and what it has summed up.
 template <int D>
 struct Columns {
     Query<D, 16> q;
     float sum, bias;                              // sum of q, what the accumulator starts from
     int lo, seen;                                 // the first key that the column's query sees, how many it sees
-    float m, l, w;                                // running maximum; sums over the lane's keys of p and p * (mid + step / 2)
+    float m, l, w;                                // running maximum; sums over the lane's keys of p, and of what centres and halves of steps add
     f32x4 o[D / 16];
+    bool far;                                     // some centre of the tile goes with p
     float limit, up;                              // a power of two that no step seen so far exceeds; log2 of the factor in p
 };
 
@@ -126,7 +130,7 @@ __device__ __forceinline__ void scale_sums(Columns<D>& r, float by) {
         for (int e = 0; e < 4; ++e) r.o[j][e] *= by;
 }
 
-// The parameters of a tile to LDS: keys' steps and centres, values' steps and centres + step / 2.  A value row that is not finite
+// The parameters of a tile to LDS: keys' steps and centres, values' steps and what their centres + step / 2 add.  A value row that is not finite
 // becomes zeros and its key NaN: columns that do not see it stay what they are.
 template <int D>
 __device__ __forceinline__ void take_parameters(Columns<D>& r, const Codes<D>& t, float* lds, bool there, int lane) {
@@ -139,7 +143,10 @@ __device__ __forceinline__ void take_parameters(Columns<D>& r, const Codes<D>& t
     lds[lane] = ks;
     lds[64 + lane] = __uint_as_float(kp & 0xffff0000u);
     lds[128 + lane] = step;
-    lds[192 + lane] = fmaf(0.5f, step, mid);
+    const Centre c = split_centre(step, mid);
+    put_centre(lds + 192, lane, c.with_step + 0.5f);
+    lds[256 + lane] = c.with_p;
+    r.far = __any(c.with_p != 0.0f);
     if (__any(step > r.limit)) {
 #pragma unroll
         for (int w = 1; w < 64; w *= 2) step = fmaxf(step, __shfl_xor(step, w));
@@ -202,18 +209,28 @@ __device__ __forceinline__ void take_scores(uint32_t (&p)[4 / F][2], Columns<D>&
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int key = 16 * (u * F + copy) + 4 * g;
-        const f32x4 step = *reinterpret_cast<const f32x4*>(lds + 128 + key), mid = *reinterpret_cast<const f32x4*>(lds + 192 + key);
+        const f32x4 step = *reinterpret_cast<const f32x4*>(lds + 128 + key);
+        const u32x4 with_step = *reinterpret_cast<const u32x4*>(lds + 192 + key);
         float x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float y = __builtin_amdgcn_exp2f(fmaf(r.q.f, s[u][e], -off));
-            r.l += y;
-            x[e] = y * step[e];
-            r.w = fmaf(y, mid[e], r.w);
+            s[u][e] = __builtin_amdgcn_exp2f(fmaf(r.q.f, s[u][e], -off));
+            r.l += s[u][e];
+            x[e] = s[u][e] * step[e];
         }
-        p[u][0] = pack_f16(x[0], x[1]);
-        p[u][1] = pack_f16(x[2], x[3]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            p[u][e] = pack_f16(x[2 * e], x[2 * e + 1]);
+            r.w = add_centre(p[u][e], with_step[e], add_centre(p[u][e], with_step[2 + e], r.w));
+        }
     }
+    if (r.far)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const f32x4 with_p = *reinterpret_cast<const f32x4*>(lds + 256 + 16 * (u * F + copy) + 4 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.w = fmaf(s[u][e], with_p[e], r.w);
+        }
 }
 
 template <int D, int F>
@@ -305,7 +322,7 @@ __device__ __forceinline__ int* part_workers(const KvJob& job) {
 template <int D, int F, bool F16, bool PAGED, int W, bool SHARED>
 __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
     constexpr int C = 16 / F, E = D / 4;          // rows of the workgroup; elements of a row in a lane
-    __shared__ __attribute__((aligned(16))) float lds_params[W][4 * kTile];
+    __shared__ __attribute__((aligned(16))) float lds_params[W][kParameters * kTile];
     __shared__ __attribute__((aligned(16))) float lds_o[W][16][D + 4];
     __shared__ float lds_l[W][16];
     __shared__ std::conditional_t<SHARED, Shares, int> shares;
@@ -560,7 +577,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
 // How a call is launched.
 struct Plan {
     int copies;                                   // of the rows among the columns; 0: the kernel for many rows
-    int waves;                                    // of a workgroup
+    int waves;                                    // of a workgroup; many rows: of a group of them
+    int groups;                                   // many rows: groups of a workgroup, which share its keys out
     int tiles, workers, chunk, chunks;
     size_t bytes;                                 // workspace
 };
@@ -572,11 +590,17 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     p.chunks = 1;
     p.chunk = 1 << 30;
     p.copies = mean > 32 ? 0 : mean <= 4 ? 4 : mean <= 8 ? 2 : 1;
-    // many rows: eight waves a workgroup unpack a key for twice as many rows, four leave a compute unit with two workgroups
-    // that do not wait for each other: better until there are three rounds of the others (2048 x 2048, 32 heads of their own:
-    // 69 us and not 80)
+    // Many rows.  Eight waves that share each tile unpack a key once for 256 rows: best where there are such workgroups for one and a quarter
+    // rounds and more (8192 tokens against themselves, 16 heads to 4 of keys: 308 us; four waves 365; 2048 tokens, 32 to 8: 75, 67).  Below
+    // that four waves; and where these alone would leave every compute unit one or two workgroups, a second four that take every other
+    // tile of the same rows (4096 tokens, 8 heads of 64: 56 us and not 77; 2048 tokens, 32 heads to 8: 65 and not 67).  Fewer workgroups
+    // still: keys in chunks are spread better (512 tokens against 8192, 136 workgroups: 120 us and not 153).  fp16 results of
+    // 128 elements have no registers for a second four (512 x 4096: 80 us and not 42).  Where a window makes workgroups alike, a
+    // second round of them costs as much as the first (276 workgroups: 54 us and not 51).
     const auto tiles_of = [&](int bm) { return a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm); };
-    p.waves = tiles_of(256) * c.kv_heads >= 3 * num_cu ? 8 : 4;
+    p.waves = 4 * tiles_of(256) * c.kv_heads >= 5 * (int64_t)num_cu ? 8 : 4;
+    const int64_t small = tiles_of(128) * c.kv_heads;
+    p.groups = p.waves == 4 && (a.dtype != RQ_F16 || c.head_dim == 64) && 3 * small >= 2 * (int64_t)num_cu && (!a.window || small <= num_cu) ? 2 : 1;
     const int bm = p.copies ? 16 / p.copies : 32 * p.waves;
     const int64_t tiles = tiles_of(bm);
     p.tiles = (int)tiles;
@@ -596,8 +620,9 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
         p.waves = !p.workers && few ? kMostWaves : kWaves;
         return p;
     }
-    // Keys in chunks where the rows alone do not fill the chip, of sixteen tiles at least (joining them is a launch more).
-    const int64_t want = 2 * num_cu / (tiles * c.kv_heads), most = range / (16 * kTile), chunks = want < most ? want : most;
+    // Keys in chunks where the rows alone do not fill the chip, of eight tiles at least (1500 tokens, 4 heads to one: 30 us; sixteen tiles:
+    // 44; joining them is a launch more).
+    const int64_t want = 2 * num_cu / (tiles * c.kv_heads), most = p.groups == 1 ? range / (8 * kTile) : 1, chunks = want < most ? want : most;
     if (chunks > 1) {
         p.chunk = (int)((range + chunks * kTile - 1) / (chunks * kTile) * kTile);
         p.chunks = (int)((range + p.chunk - 1) / p.chunk);
@@ -631,7 +656,7 @@ int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
         case 2: launch_few<D, 2, F16>(job, p, s); break;
         case 1: launch_few<D, 1, F16>(job, p, s); break;
         default:
-            launch_prompt(job, p.waves, s);
+            launch_prompt(job, p.waves, p.groups, s);
             if (p.chunks > 1)
                 launch_kernel(k_kv4_join<D, F16>, group_grid(((int64_t)job.a.tokens * job.a.heads + kWaves - 1) / kWaves, 64 * kWaves), dim3(64 * kWaves), 0, s, job);
     }
@@ -640,7 +665,16 @@ int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
 
 }  // namespace
 
-size_t kv4_attention_workspace(const Kv4& c, const Kv4Attention& a, int num_cu) { return plan(c, a, num_cu).bytes; }
+size_t kv4_attention_workspace(const Kv4& c, const Kv4Attention& a, int num_cu) {
+    Kv4Attention x = a;                           // (the caller's size holds for results of either type)
+    size_t most = 0;
+    for (const int dtype : {RQ_BF16, RQ_F16}) {
+        x.dtype = dtype;
+        const size_t bytes = plan(c, x, num_cu).bytes;
+        most = bytes > most ? bytes : most;
+    }
+    return most;
+}
 
 int kv4_attention(const Kv4& c, const Kv4Attention& a, int num_cu, float* workspace, hipStream_t s) {
     const Plan p = plan(c, a, num_cu);

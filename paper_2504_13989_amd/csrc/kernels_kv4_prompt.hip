@@ -23,7 +23,7 @@ template <int D, bool EXACT>
 struct Tile {
     uint16_t k[kTile][D + kKeyPad];
     uint16_t v[D][kValueRow];                     // element d in row (d % 4) * D / 4 + d / 4
-    float scale[EXACT ? 4 : 1][EXACT ? kTile : 4];  // EXACT: keys' steps and centres, values' steps and centres
+    float scale[EXACT ? 5 : 1][EXACT ? kTile : 4];  // EXACT: keys' steps and centres, values' steps and what their centres add
 };
 
 // What a thread unpacks of a tile: N runs of eight bytes each of keys and of values.
@@ -69,7 +69,6 @@ __device__ __forceinline__ void load_tile(Raw<N>& t, const Kv4& c, int pages, in
     }
 }
 
-__device__ __forceinline__ f16x2 as_f16(uint32_t w) { return __builtin_bit_cast(f16x2, w); }
 __device__ __forceinline__ uint32_t as_bits(f16x2 x) { return __builtin_bit_cast(uint32_t, x); }
 
 // c - 7.5 of nibble J of both halves of a dword, exact: 64 + c less 71.5.
@@ -102,7 +101,7 @@ __device__ __forceinline__ int widen(Range& r, float x) {
 
 template <int D, bool EXACT>
 struct Sums {
-    float m, l, w;                                // maximum (log2), sums over the lane's keys of p and, EXACT, p * mid
+    float m, l, w;                                // maximum (log2), sums over the lane's keys of p and, EXACT, of what centres add
     float __attribute__((ext_vector_type(16))) o[D / 32];
 };
 template <int D, bool EXACT>
@@ -119,7 +118,7 @@ struct Parameters {
 };
 // Ranges widen to hold them.
 template <int D, bool EXACT>
-__device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32_t kp, uint32_t vp, int thread, Range& keys, Range& values, int& grew) {
+__device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32_t kp, uint32_t vp, int thread, Range& keys, Range& values, int& grew, bool& far) {
     Parameters p{__uint_as_float(kp << 16), __uint_as_float(kp & 0xffff0000u), __uint_as_float(vp << 16), __uint_as_float(vp & 0xffff0000u)};
     if (!finite(p.vs) || !finite(p.vm)) {
         p.vs = p.vm = 0.0f;
@@ -139,7 +138,10 @@ __device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32
         if (thread >> 6 == 0) to.scale[0][lane] = p.ks;
         if (thread >> 6 == 1) to.scale[1][lane] = p.km;
         if (thread >> 6 == 2) to.scale[2][lane] = p.vs;
-        if (thread >> 6 == 3) to.scale[3][lane] = p.vm;
+        const Centre c = split_centre(p.vs, p.vm);
+        if (thread >> 6 == 3) put_centre(to.scale[3], lane, c.with_step);
+        if (thread >> 6 == 0) to.scale[4][lane] = c.with_p;
+        far = __any(c.with_p != 0.0f);
     }
     return p;
 }
@@ -280,7 +282,7 @@ __device__ __forceinline__ void take_keys(f32x16 (&s)[2], const Query<D, 32>& q,
 
 // Scores to probabilities, and their products with the values.
 template <int D, bool EXACT>
-__device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], const Query<D, 32>& q, const Tile<D, EXACT>& t, float f, float up, int k0,
+__device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], const Query<D, 32>& q, const Tile<D, EXACT>& t, float f, float up, bool far, int k0,
                                             bool whole, int lo, int seen, int lane) {
     const int n = lane & 31, h = lane >> 5;
     constexpr int J = D / 32;
@@ -316,12 +318,23 @@ __device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], c
         for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[i][e]), s[i][e + 1]);
     mx = f * column_max<32>(mx);
     // p may grow to 2^8 before the sums are scaled to a new maximum
-    if (__any(mx - r.m > 8.0f)) {
+    if (__builtin_expect(__any(mx - r.m > 8.0f) || (EXACT && far), 0)) {
         const float to = fmaxf(r.m, mx), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(r.m - to);
         scale_sums(r, by);
         r.l *= by;
         r.w *= by;
         r.m = to;
+        if (EXACT && far) {                       // (rare: these exponentials are taken again below)
+            const float off = (to == -INFINITY ? 0.0f : to) - up;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 with_p = *reinterpret_cast<const f32x4*>(&t.scale[4][32 * i + 2 * e + 4 * h]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) r.w = fmaf(__builtin_amdgcn_exp2f(fmaf(f, s[i][e + u], -off)), with_p[u], r.w);
+                }
+        }
     }
     const float off = (r.m == -INFINITY ? 0.0f : r.m) - up;
     // sixteen keys at a time, the next ones' probabilities beside the products of these
@@ -330,10 +343,11 @@ __device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], c
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
             const int at = 8 * (g % 2) + 4 * v, key = 32 * (g / 2) + 2 * at + 4 * h;
-            f32x4 step, mid;
+            f32x4 step;
+            u32x4 with_step;
             if constexpr (EXACT) {
                 step = *reinterpret_cast<const f32x4*>(&t.scale[2][key]);
-                mid = *reinterpret_cast<const f32x4*>(&t.scale[3][key]);
+                with_step = *reinterpret_cast<const u32x4*>(&t.scale[3][key]);
             }
             float x[4];
 #pragma unroll
@@ -341,12 +355,14 @@ __device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], c
                 x[u] = __builtin_amdgcn_exp2f(fmaf(f, s[g / 2][at + u], -off));
                 if constexpr (EXACT) {
                     r.l += x[u];
-                    r.w = fmaf(x[u], mid[u], r.w);
                     x[u] *= step[u];
                 }
             }
             p[g % 2][2 * v] = pack_f16(x[0], x[1]);
             p[g % 2][2 * v + 1] = pack_f16(x[2], x[3]);
+            if constexpr (EXACT)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) r.w = add_centre(p[g % 2][2 * v + u % 2], with_step[u], r.w);
             if constexpr (!EXACT) {               // (of what the products see: two an instruction)
                 const f16x2 one{(_Float16)1.0f, (_Float16)1.0f};
                 r.l = __builtin_amdgcn_fdot2(as_f16(p[g % 2][2 * v]), one, r.l, false);
@@ -384,17 +400,29 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int D, int WAVES, bool F16, bool PAGED>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
+// What a wave of the second group hands to its counterpart of the first, a lane's words side by side.
+template <int D>
+struct Handed {
+    float o[D / 2][64], m[64], l[64], w[64];
+    int up[64];
+};
+
+// GROUPS: 2 where a workgroup's rows are few: two groups of WAVES waves have the same rows and take turns at the tiles, each with tiles of
+// its own in LDS, and the second hands its sums to the first at the end.
+template <int D, int WAVES, int GROUPS, bool F16, bool PAGED>
+__global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job) {
     constexpr bool EXACT = F16;
     constexpr int BM = 32 * WAVES, N = (kRuns<D> + 64 * WAVES - 1) / (64 * WAVES);
     // Eight waves are two groups, four SIMDs each, half a step apart: one has products of keys and unpacks while the other has
     // exponentials.  Three tiles then, since the one group still reads values of the last while the other unpacks the next.
     constexpr bool TWO = WAVES == 8;
-    constexpr int TILES = TWO ? 3 : 2;
-    __shared__ __attribute__((aligned(16))) Tile<D, EXACT> tiles[TILES];
+    constexpr int TILES = WAVES == 8 ? 3 : 2;
+    constexpr int kStride = GROUPS * kTile;       // from a group's tile to its next
+    __shared__ __attribute__((aligned(16))) Tile<D, EXACT> all_tiles[GROUPS][TILES];
     const Kv4Attention& a = job.a;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int half = GROUPS == 1 ? 0 : of_all / WAVES, wave = of_all - half * WAVES, thread = GROUPS == 1 ? threadIdx.x : 64 * wave + lane;
+    Tile<D, EXACT>* tiles = all_tiles[half];
     const int head = blockIdx.x, item = item_number();
     const int tile_no = job.chunks == 1 ? item : item / job.chunks, chunk = item - tile_no * job.chunks;
     const CodeBits bits;
@@ -422,16 +450,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     const int token = there ? token_of(job, at, mine) : 0, of = there ? mine - token * job.group : 0;
     const RawQuery<D, 32> raw_q = load_query<D, 32>(job, there, at.q0 + token, head * job.group + of, lane);
     const int head_at = head * ((D + 8) << job.cache.page_shift);
-    int pages = 0, page_no = 0, asked = from;     // the tile asked for last, its number among those of `pages`
+    int pages = 0, page_no = 0, asked = from + half * kTile;   // the tile asked for last, its number among those of `pages`
     Raw<N> raw, later;                            // the next tile, the one after it
     if (from < to) {
-        pages = load_pages<PAGED>(job, table, from, kTile, lane);
-        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, from, threadIdx.x);
-        if (from + kTile < to) {
-            asked += kTile;
+        pages = load_pages<PAGED>(job, table, asked, kStride, lane);
+        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, asked, thread);
+        if (asked + kStride < to) {
+            asked += kStride;
             page_no = 1;
         }
-        load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, asked, threadIdx.x);
+        load_tile<D, WAVES, N, PAGED>(later, job.cache, pages, page_no, head_at, asked, thread);
     }
     Query<D, 32> q;
     take_query<D, 32, F16, F16>(q, job, raw_q, lane);
@@ -452,8 +480,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
 
     Range keys{0.0f, 0}, values{0.0f, 0};
     int at_tile = TILES - 1;                      // the tile in hand
-    if (TWO && wave >= 4) lds_barrier();
+    if (TWO && of_all >= 4) lds_barrier();
     // a step unpacks the next tile and takes this one; the first has none to take
+    bool far = false;                             // EXACT: some centre of the tile in hand goes with p
     // (two steps a pass, each with registers of its own for what is under way: copies would wait for it.  A tile is asked for in
     // every step, the last one again at the end: where a load may be left out, what was loaded before it is waited for with all else.)
     const auto step = [&](int k0, Raw<N>& raw) {
@@ -461,37 +490,39 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
         at_tile = at_tile == TILES - 1 ? 0 : at_tile + 1;
         Tile<D, EXACT>& then = tiles[at_tile];
         const bool mine_too = k0 >= from && k0 < any_hi && k0 + kTile > any_lo;
-        const int next = k0 + kTile;
+        const int next = k0 + kStride;
         // (the tile's own ranges: the next one may widen them)
         const float f = EXACT ? q.f : __builtin_amdgcn_ldexpf(q.f, -keys.up), up = EXACT ? (float)values.up : 0.0f;
         const bool there = next + lane < to;
         int grew;
-        const Parameters of_next = take_parameters<D, EXACT>(then, there ? raw.kp : 0u, there ? raw.vp : 0u, threadIdx.x, keys, values, grew);
+        bool far_next = false;
+        const Parameters of_next = take_parameters<D, EXACT>(then, there ? raw.kp : 0u, there ? raw.vp : 0u, thread, keys, values, grew, far_next);
         f32x16 s[2];
         if (mine_too) {
-            const Factors<N> factors = factors_of<D, WAVES, N, EXACT>(of_next, threadIdx.x, keys, values);
-            take_keys<D, WAVES, N, EXACT>(s, q, now, then, raw, factors, threadIdx.x, bits);         // (where there is no next tile, `then` is not read)
+            const Factors<N> factors = factors_of<D, WAVES, N, EXACT>(of_next, thread, keys, values);
+            take_keys<D, WAVES, N, EXACT>(s, q, now, then, raw, factors, thread, bits);         // (where there is no next tile, `then` is not read)
         } else {
-            const Factors<N> factors = factors_of<D, WAVES, N, EXACT>(of_next, threadIdx.x, keys, values);
+            const Factors<N> factors = factors_of<D, WAVES, N, EXACT>(of_next, thread, keys, values);
             Unpacked<N> x;
-            unpack<0, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
-            unpack<1, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
-            unpack<2, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
-            unpack<3, D, WAVES>(x, then, raw, factors, threadIdx.x, bits);
+            unpack<0, D, WAVES>(x, then, raw, factors, thread, bits);
+            unpack<1, D, WAVES>(x, then, raw, factors, thread, bits);
+            unpack<2, D, WAVES>(x, then, raw, factors, thread, bits);
+            unpack<3, D, WAVES>(x, then, raw, factors, thread, bits);
         }
-        if (asked + kTile < to) {
-            asked += kTile;
+        if (asked + kStride < to) {
+            asked += kStride;
             if (++page_no == kPagesOf<PAGED>) {
-                pages = load_pages<PAGED>(job, table, asked, kTile, lane);
+                pages = load_pages<PAGED>(job, table, asked, kStride, lane);
                 page_no = 0;
             }
         }
-        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, page_no, head_at, asked, threadIdx.x);
+        load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, page_no, head_at, asked, thread);
         if constexpr (TWO) {                      // (products of keys go first where both groups have something to issue: 1 %)
             lds_barrier();
             __builtin_amdgcn_s_setprio(0);
         }
-        if (mine_too) take_scores<D, EXACT>(r, s, q, now, f, up, k0, k0 >= all_lo && k0 + kTile <= all_hi, lo, seen, lane);
+        if (mine_too) take_scores<D, EXACT>(r, s, q, now, f, up, far, k0, k0 >= all_lo && k0 + kTile <= all_hi, lo, seen, lane);
+        far = far_next;
         if (grew != 0) {                          // sums go on in the next tile's range
             const float by = __builtin_amdgcn_ldexpf(1.0f, grew);
             scale_sums(r, by);
@@ -503,11 +534,45 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
         lds_barrier();
         if constexpr (TWO) __builtin_amdgcn_s_setprio(1);
     };
-    for (int k0 = from - kTile; from < to && k0 < to; k0 += 2 * kTile) {
-        step(k0, raw);
-        step(k0 + kTile, later);                  // (where there is no such tile nothing is taken)
+    for (int k0 = from - kStride; from < to && k0 < to; k0 += 2 * kStride) {
+        step(k0 + half * kTile, raw);
+        step(k0 + half * kTile + kStride, later); // (where there is no such tile nothing is taken)
     }
-    if (TWO && wave < 4) lds_barrier();
+    if (TWO && of_all < 4) lds_barrier();
+    if constexpr (GROUPS == 2) {
+        static_assert(sizeof(all_tiles) >= WAVES * sizeof(Handed<D>), "what is handed over takes the tiles' place");
+        Handed<D>& h = reinterpret_cast<Handed<D>*>(all_tiles)[wave];
+        if (half == 1) {
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) h.o[16 * j + e][lane] = r.o[j][e];
+            h.m[lane] = r.m;
+            h.l[lane] = r.l;
+            h.w[lane] = r.w;
+            h.up[lane] = values.up;
+        }
+        lds_barrier();
+        if (half == 1) return;
+        // the smaller of the factors: neither side's sums overflow by it
+        const int theirs = __builtin_amdgcn_readfirstlane(h.up[lane]);
+        const int up = values.up < theirs ? values.up : theirs;
+        const float m = fmaxf(r.m, h.m[lane]);
+        float x = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - m), y = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(h.m[lane] - m);
+        const float xo = x * __builtin_amdgcn_ldexpf(1.0f, up - values.up), yo = y * __builtin_amdgcn_ldexpf(1.0f, up - theirs);
+        if constexpr (EXACT) {
+            x = xo;
+            y = yo;
+        }
+        r.l = fmaf(y, h.l[lane], x * r.l);
+        r.w = fmaf(y, h.w[lane], x * r.w);
+        r.m = m;
+        values.up = up;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r.o[j][e] = fmaf(yo, h.o[16 * j + e][lane], xo * r.o[j][e]);
+    }
     if (!there) return;                           // (both lanes of the row)
     const float l = column_sum<32>(r.l), w = EXACT ? column_sum<32>(r.w) : 0.0f;
     const float by = (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) * (EXACT ? 1.0f : __builtin_amdgcn_ldexpf(1.0f, -values.up));
@@ -533,21 +598,30 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv4_prompt(KvJob job) {
     }
 }
 
-template <int D, int WAVES>
+template <int D, int WAVES, int GROUPS>
 void launch(const KvJob& job, hipStream_t s) {
-    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.tiles * job.chunks), block(64 * WAVES);
+    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.tiles * job.chunks), block(64 * WAVES * GROUPS);
     const bool paged = job.cache.page_shift < 6;
-    if (job.a.dtype == RQ_F16 && paged) launch_kernel(k_kv4_prompt<D, WAVES, true, true>, grid, block, 0, s, job);
-    else if (job.a.dtype == RQ_F16) launch_kernel(k_kv4_prompt<D, WAVES, true, false>, grid, block, 0, s, job);
-    else if (paged) launch_kernel(k_kv4_prompt<D, WAVES, false, true>, grid, block, 0, s, job);
-    else launch_kernel(k_kv4_prompt<D, WAVES, false, false>, grid, block, 0, s, job);
+    if constexpr (D == 64 || GROUPS == 1)
+        if (job.a.dtype == RQ_F16) {
+            launch_kernel(paged ? k_kv4_prompt<D, WAVES, GROUPS, true, true> : k_kv4_prompt<D, WAVES, GROUPS, true, false>, grid, block, 0, s, job);
+            return;
+        }
+    if (paged) launch_kernel(k_kv4_prompt<D, WAVES, GROUPS, false, true>, grid, block, 0, s, job);
+    else launch_kernel(k_kv4_prompt<D, WAVES, GROUPS, false, false>, grid, block, 0, s, job);
+}
+template <int D>
+void launch(const KvJob& job, int waves, int groups, hipStream_t s) {
+    if (waves == 8) launch<D, 8, 1>(job, s);
+    else if (groups == 2) launch<D, 4, 2>(job, s);
+    else launch<D, 4, 1>(job, s);
 }
 
 }  // namespace
 
-void launch_prompt(const KvJob& job, int waves, hipStream_t s) {
-    if (job.cache.head_dim == 128) waves == 8 ? launch<128, 8>(job, s) : launch<128, 4>(job, s);
-    else waves == 8 ? launch<64, 8>(job, s) : launch<64, 4>(job, s);
+void launch_prompt(const KvJob& job, int waves, int groups, hipStream_t s) {
+    if (job.cache.head_dim == 128) launch<128>(job, waves, groups, s);
+    else launch<64>(job, waves, groups, s);
 }
 
 }  // namespace rq

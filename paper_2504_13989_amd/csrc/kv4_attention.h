@@ -250,9 +250,33 @@ __device__ __forceinline__ int load_pages(const KvJob& job, const int32_t* table
 // head's block in a page)
 template <bool PAGED>
 __device__ __forceinline__ const uint8_t* block_of(const Kv4& c, int pages, int n, int quarter, int head_at) {
-    return c.data + (int64_t)__builtin_amdgcn_readlane(pages, PAGED ? 4 * n + quarter : n) * c.page_bytes + head_at;
+    // (a page's bytes fit 32 bits: RQ_KV4_MAX_HEADS * 256 * 136)
+    return c.data + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(pages, PAGED ? 4 * n + quarter : n) * (uint32_t)c.page_bytes + head_at;
 }
 __device__ __forceinline__ int place_of(const Kv4& c, int k0, int quarter) { return (k0 + 16 * quarter) & ((1 << c.page_shift) - 1); }
+
+// What a key's centre adds to the sums, for the two factors it can go with: p, and p * step as it was rounded to fp16.  A centre of the
+// size of the range, which the codes' share may cancel, goes with the latter, so that the rounding stays one of p; a larger one
+// cannot be cancelled, and its quotient might overflow.
+struct Centre {
+    float with_p, with_step;
+};
+__device__ __forceinline__ Centre split_centre(float step, float mid) {
+    const bool near = step >= 0x1p-100f && fabsf(mid) < 16.0f * step;
+    return Centre{near ? 0.0f : mid, near ? mid * __builtin_amdgcn_rcpf(step) : 0.0f};
+}
+
+// with_step of a tile's keys in LDS, as two fp16 numbers each: four keys' high parts, then their low ones.  The sum with p * step then
+// takes two products an instruction, at the rate of others (a product of fp16 and fp32 operands takes twice as long: a prompt's
+// fp16 results 80 us and not 74).
+__device__ __forceinline__ void put_centre(float* lds, int key, float x) {
+    _Float16* w = reinterpret_cast<_Float16*>(lds + (key & ~3)) + (key & 3);
+    const _Float16 high = (_Float16)x;
+    w[0] = high;
+    w[4] = (_Float16)(x - (float)high);
+}
+__device__ __forceinline__ f16x2 as_f16(uint32_t w) { return __builtin_bit_cast(f16x2, w); }
+__device__ __forceinline__ float add_centre(uint32_t p, uint32_t with_step, float sum) { return __builtin_amdgcn_fdot2(as_f16(p), as_f16(with_step), sum, false); }
 
 // A tile of BM rows: where they lie, and (once find_keys has been asked) the positions that they see.
 struct Place {
@@ -312,7 +336,7 @@ __device__ __forceinline__ void find_keys(const KvJob& job, Place& p, int len) {
 
 }  // namespace
 
-// kernels_kv4_prompt.hip: many rows, 32 a wave, a workgroup of 4 or 8 waves
-void launch_prompt(const KvJob& job, int waves, hipStream_t s);
+// kernels_kv4_prompt.hip: many rows, 32 a wave, a workgroup of one or two groups of 4 waves or one of 8
+void launch_prompt(const KvJob& job, int waves, int groups, hipStream_t s);
 
 }  // namespace rq
