@@ -461,8 +461,10 @@ size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int hea
  * q_start[b] .. q_start[b + 1] - 1 and stand at its last positions: query i of n at kv_lens[b] - n + i.  A causal query sees
  * positions up to its own, others all of the sequence; with a window w > 0 only those later than its own minus w.  A query that sees
  * nothing gets zeros (and -infinity in lse).
- * Query head x reads kv head x / (heads / kv_heads).  Queries are rotated as the keys were (h), rounded to fp16 after scaling each
- * row by a power of two, and multiplied with the codes; probabilities are rounded to bf16, all else is fp32.
+ * Query head x reads kv head x / (heads / kv_heads).  Queries are rotated as the keys were (h) and rounded to fp16 after scaling each
+ * row by a power of two (for fp16 results: to two fp16 numbers), probabilities times the steps of the values are rounded to fp16, all
+ * else is fp32 - but that bf16 results of many queries a sequence (over 32 rows of a kv head) come from elements rounded to fp16
+ * and from probabilities rounded to fp16.
  *   Q            [in]  DEVICE, element [token][head][i] at token * q_token_stride + head * q_head_stride + i
  *   dtype        [in]  RQ_BF16 or RQ_F16, of Q and O
  *   tokens       [in]  0 .. 2^24

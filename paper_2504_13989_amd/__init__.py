@@ -8,3 +8,4 @@ from .binding import (Hadamard, KV4Cache, RotqError, dequantize_rotate, expand_l
                       kv4_append, kv4_attention, kv4_cache, kv4_copy_pages, kv4_page_bytes, kv4_read, next_order,
                       quant_error, quant_error_workspace, quantize, quantize_asym, rotate, rotate_quantize,
                       rotate_quantize_asym)
+from .pages import PagePool  # noqa: F401

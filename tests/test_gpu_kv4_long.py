@@ -54,3 +54,17 @@ def test_tiles_of_very_different_size(dtype, first):
         v = torch.randn(n, kv, d, device="cuda") * torch.where(tile, 1.0, 2.0 ** -60)[:, None, None]
         rq.kv4_append(None, b.cache, k, v, torch.tensor(b.slots[0]).cuda())
         b.check(q.half(), [n], rq.kv4_attention(None, b.cache, q.half(), b.dev_table, b.dev_lens, start))
+
+
+def test_example():
+    """The example's branches against the model without a cache.  A row's 16 levels over 2 max |y| (some 5 deviations for 128 elements) are a third
+    of a deviation apart: a rounding of 0.1 deviations, in keys and values; two layers of them, sums of residuals."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "examples", "kv4_generate.py")
+    spec = importlib.util.spec_from_file_location("kv4_generate", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    far, size = example.main()
+    assert size == 2 * 136 and set(far) == {"a", "b", "keys"}
+    assert far["keys"] < 0.13 and far["a"] < 0.2 and far["b"] < 0.2
