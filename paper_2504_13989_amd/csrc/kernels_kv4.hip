@@ -219,7 +219,8 @@ __device__ __forceinline__ uint32_t* params(const Place& at, int p) { return rei
 // A wave takes 8 (or, short heads, 16) consecutive tokens of a head, key and value.  Value codes of two tokens make a dword: where the
 // slots of an even token and the next one are such a pair, the even token's lanes write the dwords of their first eight
 // elements and the odd token's those of the other; else each writes its own halfwords.
-// Bound by vector issue and memory alike: about 500 instructions a wave.  8192 tokens of 32 heads of 128, bf16, rotated.
+// Bound by memory, of which it reaches 4.5 TB/s (a copy: 5.0): 8192 tokens of 32 heads of 128, bf16, rotated, 170 MB: 38 us; vector issue 43 %
+// (with eight elements a lane, twice the lanes and their crossings: 59).
 template <int D, int DT, bool ALIGNED, bool ROTATE>
 __global__ __launch_bounds__(kThreads) void k_kv4_append(Kv4 cache, Kv4Append a, Shape shape) {
     const int lane = threadIdx.x & 63, part = part_of<D>(lane);
@@ -267,6 +268,8 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(Kv4 cache, Kv4Append a,
     }
 }
 
+// Bound by the rows' stores: 65536 rows of 8 heads of 128 to fp16, 340 MB: 51.7 us, 6.6 TB/s (writing alone reaches 6.9); with eight elements a
+// lane 82.
 template <int D, int DT, bool ROTATE>
 __global__ __launch_bounds__(kThreads) void k_kv4_read(Kv4 cache, Kv4Read a, Shape shape) {
     const int lane = threadIdx.x & 63, part = part_of<D>(lane);
