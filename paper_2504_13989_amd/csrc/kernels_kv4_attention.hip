@@ -567,7 +567,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) top = fmaxf(top, __shfl_xor(top, w));
     float all = 0.0f, y[per] = {};
-#pragma unroll 4
+#pragma unroll 16                                 // (that many chunks in one trip to memory)
     for (int c = 0; c < job.chunks; ++c) {
         const float l = sums[c * rows];
         const float by = l == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(l - top);
@@ -597,10 +597,20 @@ struct Plan {
 Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     const int group = a.heads / c.kv_heads;
     const int64_t rows = (int64_t)a.tokens * group, mean = rows / a.batch;
+    const auto tiles_of = [&](int bm) { return a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm); };
+    const auto range_of = [&](int bm) {           // keys of a row tile at most
+        const int64_t seen = a.window ? (int64_t)a.window + bm / group + 2 + kTile : a.max_len;
+        return seen < a.max_len ? seen : a.max_len;
+    };
     Plan p{};
-    p.chunks = 1;
+    p.chunks = p.groups = 1;
     p.chunk = 1 << 30;
-    p.copies = mean > 32 ? 0 : mean <= 4 ? 4 : mean <= 8 ? 2 : 1;
+    // Rows of 16 in workgroups of their own fill the chip sooner and start at once; the kernel for many rows reads a key for 128 or 256 of
+    // them.  By tiles of 16 rows x 64 keys, the former up to 256 a compute unit: 50 tokens against 1000, 8 heads to 4: 11 us and not 24;
+    // 1000 x 1000, 8 heads: 14 and not 31; 500 x 8000 (122 a unit): 39 and 48; 1000 x 1000, 32 heads to 8 (126): 33 and 31; 2000 x 2000,
+    // 32 to 8 (500): 88 and 64.
+    const bool many = mean > 32 && tiles_of(16) * c.kv_heads * (range_of(16) / kTile + 1) > 256 * (int64_t)num_cu;
+    p.copies = many ? 0 : mean <= 4 ? 4 : mean <= 8 ? 2 : 1;
     // Many rows.  Eight waves that share each tile unpack a key once for 256 rows: best where there are such workgroups for one and a quarter
     // rounds and more (8192 tokens against themselves, 16 heads to 4 of keys: 308 us; four waves 365; 2048 tokens, 32 to 8: 75, 67).  Below
     // that four waves; and where these alone would leave every compute unit one or two workgroups, a second four that take every other
@@ -608,23 +618,21 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     // still: keys in chunks are spread better (512 tokens against 8192, 136 workgroups: 120 us and not 153).  fp16 results of
     // 128 elements have no registers for a second four (512 x 4096: 80 us and not 42).  Where a window makes workgroups alike, a
     // second round of them costs as much as the first (276 workgroups: 54 us and not 51).
-    const auto tiles_of = [&](int bm) { return a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm); };
     p.waves = 4 * tiles_of(256) * c.kv_heads >= 5 * (int64_t)num_cu ? 8 : 4;
     const int64_t small = tiles_of(128) * c.kv_heads;
     p.groups = p.waves == 4 && (a.dtype != RQ_F16 || c.head_dim == 64) && 3 * small >= 2 * (int64_t)num_cu && (!a.window || small <= num_cu) ? 2 : 1;
     const int bm = p.copies ? 16 / p.copies : 32 * p.waves;
     const int64_t tiles = tiles_of(bm);
     p.tiles = (int)tiles;
-    int64_t range = a.max_len;                    // keys of a row tile at most
-    if (a.window) {
-        const int64_t seen = (int64_t)a.window + bm / group + 2 + kTile;
-        if (seen < range) range = seen;
-    }
+    const int64_t range = range_of(bm);
     if (p.copies) {
         // Two workgroups a compute unit share the keys out.  Not so where sequences are short: joining the shares is a launch more, 4 us,
         // in which eight waves of one workgroup take 24 tiles of keys.  Nor where there are very many.
+        // Full columns share where that takes most of the time away from few workgroups (66 of 256 tiles of keys: 36 us and not 72).
         const bool few = tiles * c.kv_heads <= num_cu;
-        if (tiles <= kMostTiles && range > (few ? 2560 : 1024) && tiles * (range / kTile + kLeast) < INT32_MAX) {
+        const bool share = mean > 32 || (few && p.copies == 1) ? range / kTile * (num_cu - tiles * c.kv_heads) > 56 * (int64_t)num_cu
+                                                              : range > (few ? 2560 : 1024);
+        if (tiles <= kMostTiles && share && tiles * (range / kTile + kLeast) < INT32_MAX) {
             p.workers = (int)((2 * num_cu + c.kv_heads - 1) / c.kv_heads);
             p.bytes = ((size_t)(p.workers + p.tiles) * c.kv_heads * (16 / p.copies) * (c.head_dim + 1) + 2 * (size_t)p.tiles) * sizeof(float);
         }

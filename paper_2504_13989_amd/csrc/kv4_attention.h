@@ -263,7 +263,9 @@ struct Centre {
 };
 __device__ __forceinline__ Centre split_centre(float step, float mid) {
     const bool near = step >= 0x1p-100f && fabsf(mid) < 16.0f * step;
-    return Centre{near ? 0.0f : mid, near ? mid * __builtin_amdgcn_rcpf(step) : 0.0f};
+    // (a quotient with one correction: what cancels exactly does so here too)
+    const float inv = __builtin_amdgcn_rcpf(step), x = mid * inv;
+    return Centre{near ? 0.0f : mid, near ? fmaf(fmaf(-x, step, mid), inv, x) : 0.0f};
 }
 
 // with_step of a tile's keys in LDS, as two fp16 numbers each: four keys' high parts, then their low ones.  The sum with p * step then
