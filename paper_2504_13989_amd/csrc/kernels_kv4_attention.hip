@@ -416,24 +416,29 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
         r.l = r.w = r.limit = r.up = 0.0f;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) r.o[j] = f32x4{0, 0, 0, 0};
-        while (k0 < to) {
+        // (the last tile by itself: where loads may be left out, all that was loaded before them is waited for)
+        const auto step = [&](auto more) {
             const int next = k0 + stride;
-            if (++number_of == kPagesOf<PAGED> && next < to) {
-                pages = load_pages<PAGED>(job, table, next, stride, lane);
-                number_of = 0;
-            }
             Source<PAGED> s;
-            if (next < to) s = find_tile<PAGED>(job.cache, pages, number_of, head_at, next);
+            if constexpr (more) {
+                if (++number_of == kPagesOf<PAGED>) {
+                    pages = load_pages<PAGED>(job, table, next, stride, lane);
+                    number_of = 0;
+                }
+                s = find_tile<PAGED>(job.cache, pages, number_of, head_at, next);
+            }
             take_parameters<D>(r, t, lds, k0 + lane < to, lane);
             f32x4 x[4 / F];
             take_keys<D, F, F16>(x, r, t, bits, copy);
-            if (next < to) load_keys<D>(t, s, shift, lane);
+            if constexpr (more) load_keys<D>(t, s, shift, lane);
             uint32_t p[4 / F][2];
             take_scores<D, F>(p, r, x, lds, k0, k0 >= all_lo && k0 + kTile <= all_hi, copy, g);
             take_values<D, F>(r, t, p, bits, copy);
-            if (next < to) load_values<D>(t, s, shift, lane);
+            if constexpr (more) load_values<D>(t, s, shift, lane);
             k0 = next;
-        }
+        };
+        while (k0 + stride < to) step(std::true_type{});
+        if (k0 < to) step(std::false_type{});
         // a column's results: normalised, with log2 of the sum of e^(scale q.k)
         {
             const float l = column_sum<16>(r.l), w = column_sum<16>(r.w);
