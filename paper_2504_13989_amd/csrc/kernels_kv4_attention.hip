@@ -25,8 +25,9 @@
 // sequences (a workgroup costs 5 us beside its tiles: when that was settled, eight times as many of an eighth of the work took
 // 141 us where two a unit took 109).  The waves take a workgroup's tiles in turn.  A tile's codes are read into the registers of the one before
 // as soon as those are used up, keys during the softmax, values during the next keys' products.
-// 16 sequences x 32 heads x 8192 positions of 128, bf16: 93 us and 4.6 for the join, 6.1 TB/s of codes and parameters (reading alone
-// reaches 6.9); vector issue 42 %, matrix cores 23 %.  Six sequences of 12 to 65 thousand positions, 64 heads to 8, fp16: 49 us and 5.6.
+// 16 sequences x 32 heads x 8192 positions of 128, bf16: 91 us and 4.7 for the join, 6.3 TB/s of codes and parameters (reading alone
+// reaches 6.9); vector issue 42 %, matrix cores 22 %.  Six sequences of up to 65411 positions, 64 heads to 8, fp16: 46 us and 5.1.
+// Five chunks of prompts, 14 heads of 64 to 2, window 1024, fp16: 44 us, vector issue 61 %.
 #include "kv4_attention.h"
 
 #include <type_traits>
@@ -631,7 +632,7 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     p.tiles = (int)tiles;
     const int64_t range = range_of(bm);
     if (p.copies) {
-        // Two workgroups a compute unit share the keys out.  Not so where sequences are short: joining the shares is a launch more, 4 us,
+        // Two workgroups a compute unit share the keys out (three, which registers and LDS would allow: 98.5 us and not 95).  Not so where sequences are short: joining the shares is a launch more, 4 us,
         // in which eight waves of one workgroup take 24 tiles of keys.  Nor where there are very many.
         // Full columns share where that takes most of the time away from few workgroups (66 of 256 tiles of keys: 36 us and not 72).
         const bool few = tiles * c.kv_heads <= num_cu;
