@@ -35,7 +35,7 @@
 namespace rq {
 namespace {
 
-constexpr int kWaves = 4, kMostWaves = 8;         // of a workgroup; of one that has a row tile to itself while the chip is not full
+constexpr int kWaves = 4, kMostWaves = 8;         // of a workgroup; of one that has a row tile to itself while the chip is not full (or one: plan())
 
 // Eight key codes as fp16: elements (0, 4), (1, 5), (2, 6), (3, 7) of the dword, 1024 + c in the even ones, 64 + c in the odd ones.
 __device__ __forceinline__ f16x8 key_operand(uint32_t w, const CodeBits& bits) {
@@ -642,7 +642,9 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
             p.workers = (int)((2 * num_cu + c.kv_heads - 1) / c.kv_heads);
             p.bytes = ((size_t)(p.workers + p.tiles) * c.kv_heads * (16 / p.copies) * (c.head_dim + 1) + 2 * (size_t)p.tiles) * sizeof(float);
         }
-        p.waves = !p.workers && few ? kMostWaves : kWaves;
+        // A row tile of its own: eight waves while the chip is not full, one where there are more row tiles than workgroups of four have
+        // room and their keys are few (64 sequences x 32 heads x 200: 15 us and not 23, x 1000: 46 and 48; 700 workgroups: 13.5, 9.1).
+        p.waves = p.workers ? kWaves : few ? kMostWaves : tiles * c.kv_heads > 3 * (int64_t)num_cu && range <= 1024 ? 1 : kWaves;
         return p;
     }
     // Keys in chunks where the rows alone do not fill the chip, of eight tiles at least (1500 tokens, 4 heads to one: 30 us; sixteen tiles:
@@ -664,6 +666,8 @@ void launch_few(const KvJob& job, const Plan& p, hipStream_t s) {
         launch_kernel(k_kv4_join_shares<D, F, F16>, item_grid(job.cache.kv_heads, job.tiles), dim3(64 * kWaves), 0, s, job);
     } else if (p.waves == kMostWaves) {
         launch_kernel(k_kv4_attention<D, F, F16, PAGED, kMostWaves, false>, grid, block, 0, s, job);
+    } else if (p.waves == 1) {
+        launch_kernel(k_kv4_attention<D, F, F16, PAGED, 1, false>, grid, block, 0, s, job);
     } else {
         launch_kernel(k_kv4_attention<D, F, F16, PAGED, kWaves, false>, grid, block, 0, s, job);
     }

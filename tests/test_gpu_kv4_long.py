@@ -158,3 +158,15 @@ def test_kernel_for_many_rows_takes_strided_queries():
     out = torch.zeros(300, 7, 66, device="cuda").to(torch.bfloat16)
     rq.kv4_attention(b.h, b.cache, part, b.dev_table, b.dev_lens, start, out=out[:, :6, 1:65])
     assert torch.equal(out[:, :6, 1:65], o) and (out[:, 6] == 0).all() and (out[:, :, 0] == 0).all() and (out[:, :, 65] == 0).all()
+
+
+@pytest.mark.parametrize("d,group,page,dtype,window", [(128, 1, 64, "bf16", 0), (64, 6, 16, "f16", 0), (128, 3, 32, "f16", 40), (64, 13, 64, "bf16", 0)])
+def test_many_short_sequences(d, group, page, dtype, window):
+    """More row tiles than the chip has room for: a wave each, some with no keys, some with a few tiles of them."""
+    lens = np.random.default_rng(3).integers(0, 200, 56).tolist() + [0, 1, 64, 65, 300]
+    b = Batch(lens, 14, d, page, True, seed=12)
+    q, start = b.queries([1] * len(lens), 14 * group, dtype)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    o = rq.kv4_attention(b.h, b.cache, q, b.dev_table, b.dev_lens, window=window, lse=lse)
+    b.check(q, [1] * len(lens), o, lse, window=window)
+    assert torch.equal(o, rq.kv4_attention(b.h, b.cache, q, b.dev_table, b.dev_lens, start, window=window))
