@@ -632,19 +632,23 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     p.tiles = (int)tiles;
     const int64_t range = range_of(bm);
     if (p.copies) {
-        // Two workgroups a compute unit share the keys out (three, which registers and LDS would allow: 98.5 us and not 95).  Not so where sequences are short: joining the shares is a launch more, 4 us,
-        // in which eight waves of one workgroup take 24 tiles of keys.  Nor where there are very many.
-        // Full columns share where that takes most of the time away from few workgroups (66 of 256 tiles of keys: 36 us and not 72).
-        const bool few = tiles * c.kv_heads <= num_cu;
-        const bool share = mean > 32 || (few && p.copies == 1) ? range / kTile * (num_cu - tiles * c.kv_heads) > 56 * (int64_t)num_cu
-                                                              : range > (few ? 2560 : 1024);
+        // Two workgroups a compute unit share the keys out (three, which registers and LDS would allow: 98.5 us and not 95).  Joining the
+        // shares is a launch more, and finding them a scan: 10 us.  So where row tiles leave compute units empty, once that takes more
+        // than that off the time (40 tiles of keys of 8 row tiles: 16 us either way; 79 of 96: 18 and 22; 47 of 64: 19 and 17; 66 row tiles of 256: 36 and
+        // 72).  Else workgroups that end leave their place to others or their bandwidth to longer ones (16 sequences x 32 heads x 8192: 88 us, shared 92;
+        // 64 x 8 x 3000, lengths all over the range: 25 and 31), but for a round and a little more (40 x 8, 64 heads, 8000: 61, shared 43) and for
+        // very long ones.
+        const int64_t wgs = tiles * c.kv_heads, keys = range / kTile;
+        const bool few = wgs <= num_cu;
+        const bool share = few ? keys * (num_cu - wgs) > 44 * (int64_t)num_cu
+                               : mean <= 32 && (2 * wgs < 3 * (int64_t)num_cu ? keys > 56 : wgs < 3 * (int64_t)num_cu && keys > 256);
         if (tiles <= kMostTiles && share && tiles * (range / kTile + kLeast) < INT32_MAX) {
             p.workers = (int)((2 * num_cu + c.kv_heads - 1) / c.kv_heads);
             p.bytes = ((size_t)(p.workers + p.tiles) * c.kv_heads * (16 / p.copies) * (c.head_dim + 1) + 2 * (size_t)p.tiles) * sizeof(float);
         }
         // A row tile of its own: eight waves while the chip is not full, one where there are more row tiles than workgroups of four have
         // room and their keys are few (64 sequences x 32 heads x 200: 15 us and not 23, x 1000: 46 and 48; 700 workgroups: 13.5, 9.1).
-        p.waves = p.workers ? kWaves : few ? kMostWaves : tiles * c.kv_heads > 3 * (int64_t)num_cu && range <= 1024 ? 1 : kWaves;
+        p.waves = p.workers ? kWaves : few ? kMostWaves : wgs > 3 * (int64_t)num_cu && range <= 1024 ? 1 : kWaves;
         return p;
     }
     // Keys in chunks where the rows alone do not fill the chip, of eight tiles at least (1500 tokens, 4 heads to one: 30 us; sixteen tiles:
