@@ -20,13 +20,13 @@
 // every F-th 16 keys: a lane then works on 16 / F scores a tile and not on 16 (the matrix cores, which are idle most of the time,
 // compute the rest for nothing), and the copies are joined at the end as waves are.
 //
-// What is bound here is the stream of codes.  A compute unit holds two workgroups of four waves; there are as many workgroups as
-// that takes, and where sequences are of any length each takes the same number of tiles of 64 keys, which may be parts of several
-// sequences (a workgroup costs 5 us beside its tiles: when that was settled, eight times as many of an eighth of the work took
+// What is bound here is the stream of codes.  A row tile is a workgroup's, of one, four or eight waves as there are many row tiles or
+// few.  Where that leaves compute units empty for long, there are two workgroups of four waves a compute unit, and each takes
+// the same number of tiles of 64 keys, which may be parts of several sequences (a workgroup costs 5 us beside its tiles: when that was settled, eight times as many of an eighth of the work took
 // 141 us where two a unit took 109).  The waves take a workgroup's tiles in turn.  A tile's codes are read into the registers of the one before
 // as soon as those are used up, keys during the softmax, values during the next keys' products.
-// 16 sequences x 32 heads x 8192 positions of 128, bf16: 91 us and 4.7 for the join, 6.3 TB/s of codes and parameters (reading alone
-// reaches 6.9); vector issue 42 %, matrix cores 22 %.  Six sequences of up to 65411 positions, 64 heads to 8, fp16: 46 us and 5.1.
+// 16 sequences x 32 heads x 8192 positions of 128, bf16: 87 .. 90 us, 6.3 to 6.5 TB/s of codes and parameters (reading alone
+// reaches 6.9); vector issue 43 %, matrix cores 24 %.  Six sequences of up to 65411 positions, 64 heads to 8, fp16: 46 us and 5.1.
 // Five chunks of prompts, 14 heads of 64 to 2, window 1024, fp16: 44 us, vector issue 61 %.
 #include "kv4_attention.h"
 

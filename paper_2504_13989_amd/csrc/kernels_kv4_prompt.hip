@@ -13,7 +13,7 @@
 //     kernel; four instructions a score and one product more.  Queries are two fp16 numbers.
 // A value row that is not finite becomes zeros and its key NaN: queries that do not see it stay what they are.
 //
-// 8192 tokens against themselves, 32 heads to 8 of keys, 128 elements: bf16 597 .. 620 us, 890 TFLOP/s of the products that a causal
+// 8192 tokens against themselves, 32 heads to 8 of keys, 128 elements: bf16 600 .. 635 us, 890 TFLOP/s of the products that a causal
 // prompt needs (a large matrix product: 1360); fp16 856.  A step of two waves a SIMD takes 4600 cycles: vector instructions
 // take 4.5 each and exponentials 9.7, some 2600 of them, the issue of 64 products 500; the rest is waiting for each other (counters: vector
 // issue 50 %, matrix cores 40 %, LDS 33 %).  Operands read two groups ahead, unpacking after and not beside the products: no faster.
