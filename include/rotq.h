@@ -488,6 +488,24 @@ int rq_kv4_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* 
                      int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * How rq_kv4_attention lays out such a call (testing / measurement): by these numbers alone, on a device of `compute_units`; 0: the
+ * current device's.  tokens and batch at least 1.
+ */
+typedef struct rq_kv4_plan {
+    int many;          /* 0: the kernel for few queries a sequence, 1: the one for many */
+    int rows;          /* queries x heads of a row tile, all of one sequence and kv head */
+    int waves;         /* of a workgroup; many: of a group of them */
+    int groups;        /* many: groups of a workgroup, which share its keys out */
+    int tiles;         /* row tiles of a kv head at most */
+    int workers;       /* few: workgroups of a kv head that share all keys out; 0: a workgroup a row tile */
+    int chunk, chunks; /* many: a row tile's keys, from the first that one of its rows sees (rounded down to 64), are `chunks` times
+                          `chunk` at most, a workgroup each */
+} rq_kv4_plan_t;
+
+int rq_kv4_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int heads, int batch, int decode, int causal, int window,
+                          int64_t max_len, int compute_units, rq_kv4_plan_t* plan);
+
+/*
  * Select the kernel family for subsequent hot-path calls on this handle (testing /
  * measurement): 0 = automatic (fastest available), 1 = the general LDS kernel; for long
  * power-of-two rows 2 = one wave per row at any row count, 3 / 4 = a row split over 2 / 4 waves

@@ -31,6 +31,11 @@ class RqKv4(C.Structure):
                 ("page_size", C.c_int)]
 
 
+class RqKv4Plan(C.Structure):
+    """rq_kv4_plan_t of include/rotq.h."""
+    _fields_ = [(name, C.c_int) for name in ("many", "rows", "waves", "groups", "tiles", "workers", "chunk", "chunks")]
+
+
 class RotqError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -88,6 +93,7 @@ def lib() -> C.CDLL:
     L.rq_kv4_attention_workspace.restype = C.c_size_t
     L.rq_kv4_attention.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, i32, i32, vp, vp, C.c_float, i32, i32, i64, vp,
                                    i64, i64, vp, vp, C.c_size_t, vp]
+    L.rq_kv4_attention_plan.argtypes = [kv4p, i32, i64, i32, i32, i32, i32, i32, i64, i32, C.POINTER(RqKv4Plan)]
     L.rq_strerror.argtypes = [i32]
     L.rq_strerror.restype = C.c_char_p
     for name in ("rq_hadamard_build", "rq_hadamard_info", "rq_hadamard_dense", "rq_next_order",

@@ -604,8 +604,11 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     const int group = a.heads / c.kv_heads;
     const int64_t rows = (int64_t)a.tokens * group, mean = rows / a.batch;
     const auto tiles_of = [&](int bm) { return a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm); };
-    const auto range_of = [&](int bm) {           // keys of a row tile at most
-        const int64_t seen = a.window ? (int64_t)a.window + bm / group + 2 + kTile : a.max_len;
+    // Keys of a row tile at most.  A causal tile of a window ends with its last token; another goes on to the end of the sequence, which
+    // lies as many tokens behind its first one as the sequence has queries.
+    const auto range_of = [&](int bm) {
+        const int64_t behind = a.causal ? bm / group + 2 : a.q_start ? a.tokens : 1;
+        const int64_t seen = a.window ? (int64_t)a.window + behind + kTile : a.max_len;
         return seen < a.max_len ? seen : a.max_len;
     };
     Plan p{};
@@ -699,14 +702,31 @@ int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
 }  // namespace
 
 size_t kv4_attention_workspace(const Kv4& c, const Kv4Attention& a, int num_cu) {
-    Kv4Attention x = a;                           // (the caller's size holds for results of either type)
+    Kv4Attention x = a;                           // (the caller's size holds for results of either type, causal or not)
     size_t most = 0;
-    for (const int dtype : {RQ_BF16, RQ_F16}) {
-        x.dtype = dtype;
-        const size_t bytes = plan(c, x, num_cu).bytes;
-        most = bytes > most ? bytes : most;
-    }
+    for (const int dtype : {RQ_BF16, RQ_F16})
+        for (const bool causal : {true, false}) {
+            if (!causal && !a.window) continue;   // (without a window the plan is the same)
+            x.dtype = dtype;
+            x.causal = causal;
+            const size_t bytes = plan(c, x, num_cu).bytes;
+            most = bytes > most ? bytes : most;
+        }
     return most;
+}
+
+rq_kv4_plan_t kv4_attention_plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
+    const Plan p = plan(c, a, num_cu);
+    rq_kv4_plan_t r{};
+    r.many = p.copies == 0;
+    r.rows = p.copies ? 16 / p.copies : 32 * p.waves;
+    r.waves = p.waves;
+    r.groups = p.copies ? 1 : p.groups;
+    r.tiles = p.tiles;
+    r.workers = p.workers;
+    r.chunk = p.chunk;
+    r.chunks = p.chunks;
+    return r;
 }
 
 int kv4_attention(const Kv4& c, const Kv4Attention& a, int num_cu, float* workspace, hipStream_t s) {

@@ -43,6 +43,8 @@ int num_cu() {
     return n;
 }
 
+const int32_t kRagged = 0;                        // q_start of a call that is only planned: asked for being there
+
 // The checks that rq_kv4_attention and its workspace share.
 int shape_ok(const rq::Kv4& c, int64_t tokens, int heads, int batch, int window, int64_t max_len) {
     if (tokens < 0 || tokens > (1 << 24) || heads < 1 || heads % c.kv_heads != 0 || heads / c.kv_heads > 256) return RQ_ERR_ARG;
@@ -110,9 +112,31 @@ size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int hea
     a.batch = batch;
     a.window = window;
     a.max_len = max_len;
-    static const int32_t ragged = 0;              // (asked for being there only)
-    a.q_start = decode ? nullptr : &ragged;
+    a.q_start = decode ? nullptr : &kRagged;
     return rq::kv4_attention_workspace(c, a, cu);
+}
+
+int rq_kv4_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int heads, int batch, int decode, int causal, int window,
+                          int64_t max_len, int compute_units, rq_kv4_plan_t* plan) {
+    rq::Kv4 c;
+    int rc = cache_of(cache, &c);
+    if (rc != RQ_OK) return rc;
+    if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
+    if (!plan || (dtype != RQ_BF16 && dtype != RQ_F16) || (causal != 0 && causal != 1) || compute_units < 0) return RQ_ERR_ARG;
+    if (tokens == 0 || batch == 0 || (decode && tokens != batch)) return RQ_ERR_ARG;
+    const int cu = compute_units ? compute_units : num_cu();
+    if (cu <= 0) return RQ_ERR_HIP;
+    rq::Kv4Attention a{};
+    a.dtype = dtype;
+    a.tokens = (int)tokens;
+    a.heads = heads;
+    a.batch = batch;
+    a.causal = causal != 0;
+    a.window = window;
+    a.max_len = max_len;
+    a.q_start = decode ? nullptr : &kRagged;
+    *plan = rq::kv4_attention_plan(c, a, cu);
+    return RQ_OK;
 }
 
 int rq_kv4_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* Q, int dtype, int64_t tokens, int heads,

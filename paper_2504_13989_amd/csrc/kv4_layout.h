@@ -61,6 +61,7 @@ struct Kv4Attention {
     int64_t max_len;                              // no sequence is longer
 };
 size_t kv4_attention_workspace(const Kv4& c, const Kv4Attention& a, int num_cu);
+rq_kv4_plan_t kv4_attention_plan(const Kv4& c, const Kv4Attention& a, int num_cu);
 int kv4_attention(const Kv4& c, const Kv4Attention& a, int num_cu, float* workspace, hipStream_t s);
 
 }  // namespace rq

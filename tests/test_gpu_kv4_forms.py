@@ -1,0 +1,163 @@
+"""GPU: attention over the 4-bit cache in each form that a call can take (rq_kv4_attention_plan says which), in ways that show a tile of
+64 keys left out or taken twice."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import kv4_reference as ref
+
+torch = pytest.importorskip("torch")
+import paper_2504_13989_amd as rq  # noqa: E402
+from paper_2504_13989_amd import binding  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+CODE = {"bf16": binding.RQ_BF16, "f16": binding.RQ_F16}
+U_OUT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+class Filled:
+    """Sequences in a cache of their own, shuffled pages; keys and values f(sequence's positions) [n, kv heads, d]."""
+
+    def __init__(self, lens, kv, d, page, rotate, keys, values):
+        rng = np.random.default_rng(1)
+        need = [-(-n // page) for n in lens]
+        self.lens, self.kv, self.d, self.page = lens, kv, d, page
+        self.h = rq.hadamard_build(d) if rotate else None
+        self.cache = rq.kv4_cache(sum(need) + 1, kv, d, page)
+        self.cache.data.fill_(0xFF)                      # slots that nothing is appended to: NaN parameters
+        order, at = rng.permutation(sum(need) + 1), 0
+        table, self.slots = np.full((len(lens), max(need)), -1, np.int32), []
+        for i, (n, m) in enumerate(zip(lens, need)):
+            table[i, :m] = order[at:at + m]
+            at += m
+            pos = np.arange(n)
+            self.slots.append(torch.tensor(table[i, pos // page].astype(np.int64) * page + pos % page).cuda())
+            t = torch.arange(n, device="cuda")
+            rq.kv4_append(self.h, self.cache, keys(t), values(t), self.slots[-1])
+        self.table, self.kv_lens = torch.tensor(table).cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+
+    def stored(self, i):
+        """(keys, values) of sequence i as they are stored, float64 [n, kv heads, d]"""
+        return [x.double() for x in rq.kv4_read(None, self.cache, self.slots[i], out_dtype=torch.float32)]
+
+    def steps(self, i):
+        """steps of its keys, float64 [n, kv heads]"""
+        p, block = self.page, self.page * (self.d + 8)
+        data = self.cache.data.view(-1, self.kv, block)[..., p * self.d:p * (self.d + 4)].unflatten(-1, (p, 4))
+        s = self.slots[i]
+        return data[s // p, :, s % p, :2].contiguous().view(torch.bfloat16)[..., 0].double()
+
+    def run(self, q, counts, causal, window, form=None):
+        """(o, lse), after a look at the form that the call takes"""
+        start = torch.tensor(np.concatenate(([0], np.cumsum(counts))), dtype=torch.int32).cuda()
+        decode = set(counts) == {1}
+        if form is not None:
+            p = plan(self, q, counts, causal, window)
+            got = dict(many=p.many, waves=p.waves, groups=p.groups, shared=p.workers > 0, chunked=p.chunks > 1)
+            assert got == {**got, **form}, got
+        lse = torch.full(q.shape[:2], float("nan"), device="cuda")
+        o = rq.kv4_attention(self.h, self.cache, q, self.table, self.kv_lens, None if decode else start, causal=causal, window=window,
+                             max_len=max(self.lens), lse=lse)
+        return o, lse
+
+
+def plan(f, q, counts, causal, window):
+    c, p = f.cache, binding.RqKv4Plan()
+    cache = binding.RqKv4(c.data.data_ptr(), c.pages, c.kv_heads, c.head_dim, c.page_size)
+    code = {v: CODE[k] for k, v in DT.items()}[q.dtype]
+    assert binding.lib().rq_kv4_attention_plan(C.byref(cache), code, q.shape[0], q.shape[1], len(counts), int(set(counts) == {1}), int(causal),
+                                               window, max(f.lens), 0, C.byref(p)) == binding.RQ_OK
+    return p
+
+
+def ranges(n, m, causal, window):
+    """[lo, hi) of the positions that each of m queries at the end of n positions sees"""
+    pos = torch.arange(m, device="cuda") + (n - m)
+    hi = (pos + 1).clamp(min=0) if causal else torch.full_like(pos, n)
+    lo = (pos - window + 1).clamp(min=0) if window else torch.zeros_like(pos)
+    return lo, torch.maximum(hi, lo)
+
+
+def check_coverage(lens, counts, kv, group, d, page, causal, window, dtype, form):
+    """Queries of 2^-20: all keys weigh the same, to expm1(2 e), e the largest score that |q| |k| allows.  Tile t's values are 1 in one element and 0
+    in the others, so each row's result is the number of its tiles' keys, and the log-sum the number of all.  Values and weights are
+    rounded to fp16 (2^-11 each), sums are fp32: a lane adds a 32nd of the keys, to sums below their number."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def values(t):
+        at = (t // 64)[:, None] + 5 * torch.arange(kv, device="cuda")
+        return torch.nn.functional.one_hot(at % d, d).float()
+
+    f = Filled(lens, kv, d, page, True, lambda t: torch.randn(len(t), kv, d, generator=gen, device="cuda"), values)
+    q = (torch.randn(sum(counts), kv * group, d, generator=gen, device="cuda") * 2.0 ** -20).to(DT[dtype])
+    o, lse = f.run(q, counts, causal, window, form)
+    at = 0
+    for i, (n, m) in enumerate(zip(lens, counts)):
+        k, v = f.stored(i)
+        lo, hi = ranges(n, m, causal, window)
+        count = (hi - lo).double()[:, None, None]
+        sums = [torch.cat((torch.zeros_like(x[:1]), x.cumsum(0))) for x in (v, v.abs())]
+        want, size = [((s[hi] - s[lo]) / count.clamp(min=1)).repeat_interleave(group, 1) for s in sums]
+        e = float(q.double().norm(dim=-1).max() * k.norm(dim=-1).max()) / math.sqrt(d)
+        tol = (math.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT[dtype] * want.abs() + n / 32 * 2.0 ** -24
+        assert (tol < 16 / count.clamp(min=1)).all()      # a quarter of what one tile of one row adds
+        off = (o[at:at + m].double() - want).abs()
+        assert (off <= tol).all(), (i, float((off / tol).max()))
+        none = (hi == lo)
+        assert torch.equal(torch.isinf(lse[at:at + m]), none[:, None].expand(-1, kv * group)) and (o[at:at + m][none] == 0).all()
+        off = (lse[at:at + m].double() - count[..., 0].clamp(min=1).log())[~none].abs()
+        assert (off <= 2 * e + 1e-5).all(), (i, float(off.max()))
+        at += m
+
+
+def check_values(lens, counts, kv, group, d, page, causal, window, dtype, form):
+    """Some rows against 64 bits.  A score is off by the rounding of q and of k to fp16 (2^-11 each) and by sums of codes that carry 1024 in
+    fp32 (16 roundings, see kv4_reference.attention): e at most; p and v are rounded to fp16 once each, sums are fp32."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    rows = lambda t: torch.randn(len(t), kv, d, generator=gen, device="cuda")  # noqa: E731
+    f = Filled(lens, kv, d, page, True, rows, rows)
+    q = torch.randn(sum(counts), kv * group, d, generator=gen, device="cuda").to(DT[dtype])
+    o, lse = f.run(q, counts, causal, window, form)
+    hd, at, rng = torch.tensor(ref.sylvester(d)).cuda(), 0, np.random.default_rng(5)
+    for i, (n, m) in enumerate(zip(lens, counts)):
+        k, v = f.stored(i)
+        step, (lo, hi) = f.steps(i), ranges(n, m, causal, window)
+        for t in sorted({0, m - 1, *rng.integers(0, m, 12).tolist()}):
+            a, b = int(lo[t]), int(hi[t])
+            for j in range(kv):
+                heads = slice(j * group, (j + 1) * group)
+                x = q[at + t, heads].double() @ hd
+                s = x @ k[a:b, j].t() / math.sqrt(d)
+                e = ((2.0 ** -10 * (x.abs() @ k[a:b, j].abs().t()) + 2.0 ** -10 * step[a:b, j] * x.abs().sum(-1, keepdim=True)) / math.sqrt(d)).amax(-1)
+                p, total = torch.softmax(s, -1), torch.logsumexp(s, -1)
+                want, size = p @ v[a:b, j], p @ v[a:b, j].abs()
+                tol = (torch.expm1(2 * e)[:, None] + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT[dtype] * want.abs()
+                off = (o[at + t, heads].double() - want).abs()
+                assert (off <= tol).all(), (i, t, j, float((off / tol).max()))
+                assert ((lse[at + t, heads].double() - total).abs() <= e + 2.0 ** -11 + 2.0 ** -16 + 2.0 ** -20 * total.abs()).all(), (i, t, j)
+        at += m
+
+
+def form(many, waves, groups=1, shared=False, chunked=False):
+    return dict(many=many, waves=waves, groups=groups, shared=shared, chunked=chunked)
+
+
+# lens, counts, kv heads, group, head_dim, page, causal, window, form
+CHUNKS = form(1, 4, chunked=True)
+BEHIND = [
+    ([8192], [1024], 4, 4, 128, 64, False, 4096, CHUNKS),
+    ([8000, 3230], [1500, 900], 2, 4, 128, 16, False, 4096, CHUNKS),
+    ([8100], [4814], 2, 2, 64, 128, False, 2000, CHUNKS),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", range(len(BEHIND)))
+def test_windows_of_queries_that_are_not_causal(case, dtype):
+    """With many queries and keys in chunks: all positions from the window's first to the end of the sequence count."""
+    check_coverage(*BEHIND[case][:-1], dtype, BEHIND[case][-1])
+    check_values(*BEHIND[case][:-1], dtype, BEHIND[case][-1])
