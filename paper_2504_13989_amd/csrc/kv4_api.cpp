@@ -54,6 +54,10 @@ int shape_ok(const rq::Kv4& c, int64_t tokens, int heads, int batch, int window,
     return RQ_OK;
 }
 
+// A window that reaches back over the longest sequence hides nothing: 0, as without one.  Others are below 2^30, so that a position (above
+// -2^24 where there are more queries than positions) less a window fits 32 bits.
+int window_of(int window, int64_t max_len) { return window < max_len ? window : 0; }
+
 }  // namespace
 
 extern "C" {
@@ -110,7 +114,7 @@ size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int hea
     a.tokens = (int)tokens;
     a.heads = heads;
     a.batch = batch;
-    a.window = window;
+    a.window = window_of(window, max_len);
     a.max_len = max_len;
     a.q_start = decode ? nullptr : &kRagged;
     return rq::kv4_attention_workspace(c, a, cu);
@@ -132,7 +136,7 @@ int rq_kv4_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int 
     a.heads = heads;
     a.batch = batch;
     a.causal = causal != 0;
-    a.window = window;
+    a.window = window_of(window, max_len);
     a.max_len = max_len;
     a.q_start = decode ? nullptr : &kRagged;
     *plan = rq::kv4_attention_plan(c, a, cu);
@@ -156,7 +160,7 @@ int rq_kv4_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* 
     if (!aligned(Q, 2) || !aligned(O, 2) || !aligned(table, 4) || !aligned(kv_lens, 4) || !aligned(q_start, 4) || !aligned(lse, 4)) return RQ_ERR_ARG;
     if (max_len > (int64_t)width << c.page_shift) return RQ_ERR_ARG;
     const rq::Kv4Attention a{Q, O, lse, dtype, (int)tokens, heads, batch, width, q_token_stride, q_head_stride, o_token_stride, o_head_stride,
-                             table, kv_lens, q_start, scale, causal != 0, h != nullptr, window, max_len};
+                             table, kv_lens, q_start, scale, causal != 0, h != nullptr, window_of(window, max_len), max_len};
     const int cu = num_cu();
     if (cu <= 0) return RQ_ERR_HIP;
     const size_t need = rq::kv4_attention_workspace(c, a, cu);

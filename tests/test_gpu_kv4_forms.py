@@ -161,3 +161,19 @@ def test_windows_of_queries_that_are_not_causal(case, dtype):
     """With many queries and keys in chunks: all positions from the window's first to the end of the sequence count."""
     check_coverage(*BEHIND[case][:-1], dtype, BEHIND[case][-1])
     check_values(*BEHIND[case][:-1], dtype, BEHIND[case][-1])
+
+
+@pytest.mark.parametrize("kv,many", [(1, 0), (32, 1)])
+def test_windows_of_any_size(kv, many):
+    """A window over all positions is none, however large, also where there are more queries than positions."""
+    lens, counts = [700, 40], [1400, 900]
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    rows = lambda t: torch.randn(len(t), kv, 64, generator=gen, device="cuda")  # noqa: E731
+    f = Filled(lens, kv, 64, 16, True, rows, rows)
+    q = torch.randn(sum(counts), kv * 2, 64, generator=gen, device="cuda").bfloat16()
+    for causal in (True, False):
+        want, sums = f.run(q, counts, causal, 0, dict(many=many))
+        assert torch.isfinite(want).all() and (want != 0).any()
+        for window in (700, 1 << 30, (1 << 31) - 1500, (1 << 31) - 1):
+            o, lse = f.run(q, counts, causal, window)
+            assert torch.equal(o, want) and torch.equal(lse, sums), window

@@ -79,3 +79,10 @@ def test_plan_refuses(L):
                 dict(causal=2), dict(window=-1), dict(max_len=-1), dict(units=-1)):
         assert ask(**bad) == binding.RQ_ERR_ARG, bad
     assert L.rq_kv4_attention_plan(C.byref(cache), *ok.values(), None) == binding.RQ_ERR_ARG
+
+
+@pytest.mark.parametrize("window", [4096, 4097, 1 << 30, (1 << 31) - 1])
+def test_a_window_over_all_positions_is_none(L, window):
+    """as the plan shows, which takes two groups of waves without a window and one with"""
+    plans = [plan_of(L, [4096], [4096], 8, 8, 64, binding.RQ_BF16, True, w) for w in (0, window, 4095)]
+    assert bytes(plans[0]) == bytes(plans[1]) and plans[0].groups == 2 and plans[2].groups == 1
