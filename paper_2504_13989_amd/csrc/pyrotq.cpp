@@ -421,6 +421,9 @@ struct Scratch {
     Scratch(PyObject* o, size_t need, c10::Device device) {
         if (o != Py_None) {
             const at::Tensor& t = tensor(o);
+            // (elements that share memory, as an expanded tensor's do, would count for more bytes than there are)
+            if (!t.is_cuda() || t.device() != device || !t.is_non_overlapping_and_dense())
+                raise(PyExc_ValueError, "workspace must be a dense tensor on the device of the inputs");
             data = t.data_ptr();
             bytes = (size_t)t.numel() * t.element_size();
         } else {
