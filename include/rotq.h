@@ -476,7 +476,8 @@ size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int hea
  *   scale        [in]  of the scores, finite, > 0
  *   causal       [in]  0 or 1;  window [in]  0: none
  *   max_len      [in]  no sequence is longer; at most width * page_size and 2^30.  It bounds the work that is laid out.
- *   O            [out] as Q with its own strides; must not overlap Q
+ *   O            [out] as Q with its own strides, which are head_dim at least where there are two tokens, two heads; rows must not overlap
+ *                      each other nor Q
  *   lse          [out] DEVICE, tokens x heads floats, log of the sum of exp(scale * q . k_j), or NULL
  *   workspace    [in]  DEVICE, >= rq_kv4_attention_workspace(...) bytes, 16-byte aligned, scratch; NULL where that is 0
  * Long sequences are split over workgroups and joined in a fixed order: the same call gives the same bits.

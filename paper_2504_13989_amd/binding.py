@@ -374,6 +374,6 @@ def kv4_attention(h: Optional[Hadamard], cache: KV4Cache, q, table, kv_lens, q_s
     """rq_kv4_attention: attention of q [tokens, heads, head_dim] (bfloat16 or float16) over the cached sequences of a batch, table
     int32 [batch, width] of page numbers, kv_lens int32 [batch].  Queries of sequence b are tokens q_start[b] .. q_start[b + 1] - 1
     (int32 [batch + 1]; None: one token a sequence) and stand at its last positions.  scale: 1 / sqrt(head_dim).  `lse` (float32
-    [tokens, heads]) receives the logarithms of the softmax sums."""
+    [tokens, heads]) receives the logarithms of the softmax sums.  `out` must not overlap q, nor its rows each other."""
     return (_nat or _native()).kv4_attention(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q,
                                              table, kv_lens, q_start, scale, causal, window, max_len, out, lse, workspace, stream)

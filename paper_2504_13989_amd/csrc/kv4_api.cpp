@@ -154,6 +154,8 @@ int rq_kv4_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* 
     if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
     if (width < 0 || (causal != 0 && causal != 1) || !(scale > 0.0f) || !std::isfinite(scale)) return RQ_ERR_ARG;
     if (q_token_stride < 0 || q_head_stride < 0 || o_token_stride < 0 || o_head_stride < 0) return RQ_ERR_ARG;
+    // (rows of results that share elements would be written over each other)
+    if ((tokens > 1 && o_token_stride < c.head_dim) || (heads > 1 && o_head_stride < c.head_dim)) return RQ_ERR_ARG;
     if (!q_start && tokens != batch) return RQ_ERR_ARG;                    // a token a sequence
     if (tokens == 0) return RQ_OK;
     if (batch == 0 || !Q || !O || !kv_lens || (width > 0 && (!table || c.pages == 0))) return RQ_ERR_ARG;

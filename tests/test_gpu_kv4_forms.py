@@ -177,3 +177,18 @@ def test_windows_of_any_size(kv, many):
         for window in (700, 1 << 30, (1 << 31) - 1500, (1 << 31) - 1):
             o, lse = f.run(q, counts, causal, window)
             assert torch.equal(o, want) and torch.equal(lse, sums), window
+
+
+def test_results_that_overlap_are_refused():
+    rows = lambda t: torch.randn(len(t), 2, 64, device="cuda")  # noqa: E731
+    f = Filled([40, 30], 2, 64, 16, True, rows, rows)
+    q = torch.randn(2, 4, 64, device="cuda").half()
+    call = lambda q, out: rq.kv4_attention(f.h, f.cache, q, f.table[:len(q)], f.kv_lens[:len(q)], out=out)  # noqa: E731
+    want = call(q, None)
+    for out in (torch.empty_like(q[:1]).expand(2, 4, 64), torch.empty_like(q[:, :1]).expand(2, 4, 64), torch.empty_like(q).view(-1).as_strided((2, 4, 64), (256, 32, 1))):
+        with pytest.raises(rq.RotqError):
+            call(q, out)
+    turned = torch.empty(4, 2, 64, dtype=torch.float16, device="cuda").transpose(0, 1)           # heads further apart than tokens
+    assert torch.equal(call(q, turned), want)
+    one = torch.empty(256, dtype=torch.float16, device="cuda").as_strided((1, 4, 64), (0, 64, 1))  # (one token: its stride is never used)
+    assert torch.equal(call(q[:1], one), want[:1])

@@ -249,3 +249,8 @@ def test_pool_against_a_model():
             t = pool.table(s)
             assert pool.length(s) == len(rows) and len(t) == -(-len(rows) // P)
             assert [mem[t[i // P] * P + i % P] for i in range(len(rows))] == rows
+
+
+@pytest.mark.parametrize("o", [(0, 128), (512, 0), (512, 127), (100, 128), (0, 0)])
+def test_attention_refuses_results_that_overlap(L, o):
+    assert L.rq_kv4_attention(None, cache(), 64, 0, 3, 4, 512, 128, 64, 3, 2, 64, None, 0.1, 1, 0, 32, 4096, *o, None, None, 0, None) == ARG
