@@ -104,6 +104,10 @@ __device__ __forceinline__ int widen(Range& r, float x) {
     return by;
 }
 
+// log2 of the factor in the probabilities of bf16 results, which are rounded to fp16: at most 2^15 of them where one has grown to 2^8, and
+// down to 2^-21 of the largest in full precision (without the factor keys 2^-25 below it, of which long sequences have many, were lost).
+constexpr float kUp = 7.0f;
+
 template <int D, bool EXACT>
 struct Sums {
     float m, l, w;                                // maximum (log2), sums over the lane's keys of p and, EXACT, of what centres add
@@ -497,7 +501,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         const bool mine_too = k0 >= from && k0 < any_hi && k0 + kTile > any_lo;
         const int next = k0 + kStride;
         // (the tile's own ranges: the next one may widen them)
-        const float f = EXACT ? q.f : __builtin_amdgcn_ldexpf(q.f, -keys.up), up = EXACT ? (float)values.up : 0.0f;
+        const float f = EXACT ? q.f : __builtin_amdgcn_ldexpf(q.f, -keys.up), up = EXACT ? (float)values.up : kUp;
         const bool there = next + lane < to;
         int grew;
         bool far_next = false;
@@ -582,7 +586,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
     const float l = column_sum<32>(r.l), w = EXACT ? column_sum<32>(r.w) : 0.0f;
     const float by = (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) * (EXACT ? 1.0f : __builtin_amdgcn_ldexpf(1.0f, -values.up));
     float lse = l == 0.0f ? -INFINITY : r.m + __builtin_amdgcn_logf(l);
-    if constexpr (EXACT) lse -= (float)values.up;
+    lse -= EXACT ? (float)values.up : kUp;
     const int t_row = at.q0 + token, h_row = head * job.group + of;
     const int64_t part_row = ((int64_t)chunk * a.tokens + t_row) * a.heads + h_row;
     float* part = job.part + part_row * D;

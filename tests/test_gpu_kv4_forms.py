@@ -192,3 +192,28 @@ def test_results_that_overlap_are_refused():
     assert torch.equal(call(q, turned), want)
     one = torch.empty(256, dtype=torch.float16, device="cuda").as_strided((1, 4, 64), (0, 64, 1))  # (one token: its stride is never used)
     assert torch.equal(call(q[:1], one), want[:1])
+
+
+def column(n, at, row, rest):
+    """[n, d] rows `rest`, row `at` of them `row`"""
+    x = rest.clone()
+    x[at] = row
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("at", [0, 8191])
+def test_many_small_weights_add_up(at, dtype):
+    """One key 17.6 above 8191 others, whose weights of 2^-25.4 make 2^-12 together, all of them a workgroup's.  All numbers but q * scale * log2(e), rounded to fp16, are
+    powers of two or exact in fp16; a weight of 2^-18.4 (the largest is 2^7) is rounded to 2^-24."""
+    n, d, kv = 8192, 64, 32
+    rest = torch.zeros(n, d, device="cuda")
+    keys, values = column(n, at, 2.0, rest), column(n, at, 0.0, rest + 1)
+    f = Filled([n], kv, d, 64, False, *(lambda t, x=x: x[t][:, None].repeat(1, kv, 1) for x in (keys, values)))
+    q = torch.full((1200, 2 * kv, d), 1.1015625, device="cuda").to(DT[dtype])
+    o, lse = f.run(q, [1200], False, 0, form(1, 8))
+    score = 64 * 2 * 1.1015625 / 8
+    want = (n - 1) / (n - 1 + math.exp(score))
+    off = math.expm1(score * 2.0 ** -11) + 2.0 ** -25 / 2.0 ** (7 - score / math.log(2)) + U_OUT[dtype]
+    assert ((o.double() - want).abs() <= off * want).all(), float(o.double().mean() / want)
+    assert ((lse.double() - math.log(n - 1 + math.exp(score))).abs() <= score * 2.0 ** -11 + 1e-4).all()
