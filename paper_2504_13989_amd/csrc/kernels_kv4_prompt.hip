@@ -83,24 +83,24 @@ __device__ __forceinline__ f16x2 code_pair(uint32_t w, const CodeBits& bits) {
     return as_f16(bits.high(x)) + f16x2{(_Float16)-71.5f, (_Float16)-71.5f};
 }
 
-// The powers of two in the operands: what has been seen so far is below `limit`.
+// The powers of two in the operands: what has been seen so far is below 16 * `limit`.  (Sixteenths: those of all finite elements are finite.)
 struct Range {
     float limit;
-    int up;                                       // log2 of the factor, 2^UP / limit
+    int up;                                       // log2 of the factor, 2^UP / (16 * limit)
 };
-// Widens to hold the wave's `x`; by how much the factor's log2 changed.  UP: 15 for elements, whose fp16 then has full precision down
+// Widens to hold 16 times the wave's `x`; by how much the factor's log2 changed.  UP: 15 for elements, whose fp16 then has full precision down
 // to 2^-29 of the largest; 7 for steps, which meet factors of up to 2^8.
 template <int UP>
 __device__ __forceinline__ int widen(Range& r, float x) {
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) x = fmaxf(x, __shfl_xor(x, w));
     int e = (int)(__float_as_uint(x) >> 23) - 126;                   // x < 2^e
-    e = __builtin_amdgcn_readfirstlane(e < -60 ? -60 : e > 126 ? 126 : e);
+    e = __builtin_amdgcn_readfirstlane(e < -64 ? -64 : e);
     const float limit = __uint_as_float((uint32_t)(e + 127) << 23);
     if (!(limit > r.limit)) return 0;
-    const int by = UP - e - r.up;
+    const int up = UP - 4 - e, by = up - r.up;
     r.limit = limit;
-    r.up = UP - e;
+    r.up = up;
     return by;
 }
 
@@ -133,9 +133,9 @@ __device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32
         p.vs = p.vm = 0.0f;
         p.ks = __builtin_nanf("");
     }
-    float kx = EXACT ? 0.0f : fmaf(8.0f, p.ks, fabsf(p.km)), vx = EXACT ? p.vs : fmaf(8.0f, p.vs, fabsf(p.vm));
-    kx = kx < 0x1p126f ? kx : 0.0f;
-    vx = vx < 0x1p126f ? vx : 0.0f;
+    // sixteenths of the largest element that a row could have, EXACT: of the step
+    float kx = EXACT ? 0.0f : fmaf(0.5f, p.ks, 0.0625f * fabsf(p.km)), vx = EXACT ? 0.0625f * p.vs : fmaf(0.5f, p.vs, 0.0625f * fabsf(p.vm));
+    kx = kx < INFINITY ? kx : 0.0f;               // (keys may be infinite or NaN)
     grew = 0;
     if (__any(kx > keys.limit || vx > values.limit)) {
         if (!EXACT) widen<15>(keys, kx);
@@ -500,8 +500,8 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         Tile<D, EXACT>& then = tiles[at_tile];
         const bool mine_too = k0 >= from && k0 < any_hi && k0 + kTile > any_lo;
         const int next = k0 + kStride;
-        // (the tile's own ranges: the next one may widen them)
-        const float f = EXACT ? q.f : __builtin_amdgcn_ldexpf(q.f, -keys.up), up = EXACT ? (float)values.up : kUp;
+        // (the tile's own ranges: the next one may widen them; finite, so that a score of 0 stays 0 beside a key of 2^127)
+        const float f = EXACT ? q.f : fminf(__builtin_amdgcn_ldexpf(q.f, -keys.up), 0x1p127f), up = EXACT ? (float)values.up : kUp;
         const bool there = next + lane < to;
         int grew;
         bool far_next = false;

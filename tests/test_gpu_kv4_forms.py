@@ -217,3 +217,67 @@ def test_many_small_weights_add_up(at, dtype):
     off = math.expm1(score * 2.0 ** -11) + 2.0 ** -25 / 2.0 ** (7 - score / math.log(2)) + U_OUT[dtype]
     assert ((o.double() - want).abs() <= off * want).all(), float(o.double().mean() / want)
     assert ((lse.double() - math.log(n - 1 + math.exp(score))).abs() <= score * 2.0 ** -11 + 1e-4).all()
+
+
+def reference(f, q, causal, scale=None):
+    """(o, log of the sums, sum of p |v|, largest |score|) of a batch of one sequence whose queries are all its last positions, float64"""
+    k, v = f.stored(0)
+    n, m, group = k.shape[0], q.shape[0], q.shape[1] // f.kv
+    seen = ranges(n, m, causal, 0)[1]
+    hidden = torch.arange(n, device="cuda")[None] >= seen[:, None]
+    x = q.double() @ torch.tensor(ref.sylvester(f.d)).cuda() if f.h else q.double()
+    out = []
+    for h in range(q.shape[1]):
+        s = (x[:, h] @ k[:, h // group].t() / math.sqrt(f.d)).masked_fill(hidden, -math.inf)
+        p = torch.softmax(s, -1)
+        out.append((p @ v[:, h // group], torch.logsumexp(s, -1), p @ v[:, h // group].abs(), s.masked_fill(hidden, 0).abs().amax(-1)))
+    return [torch.stack(y, 1) for y in zip(*out)]
+
+
+LARGE = {"step": (-1e38, 1e38), "centre": (1.6e38, 1.6e38)}       # (rows whose least + largest element overflows are stored as not finite)
+
+
+@pytest.mark.parametrize("what", LARGE)
+def test_values_up_to_the_end_of_the_range(what):
+    """A value row that is finite, however large, makes no result NaN.  What is 2^-40 of it and less is lost beside it (fp16's least number is 2^-24, its largest
+    2^16), also for rows that do not see it where it is in a tile that their workgroup comes to."""
+    n, kv, d, at = 1300, 32, 64, 700
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    rows = lambda t: torch.randn(len(t), kv, d, generator=gen, device="cuda")  # noqa: E731
+    values = rows(torch.arange(n))
+    values[at] = torch.linspace(*LARGE[what], d, device="cuda")
+    f = Filled([n], kv, d, 64, False, rows, lambda t: values[t])
+    q = torch.randn(n, 2 * kv, d, generator=gen, device="cuda").bfloat16()
+    o, lse = f.run(q, [n], True, 0, form(1, 8))
+    want, sums, size, most = reference(f, q, True)
+    assert torch.isfinite(o).all()
+    k, step = f.stored(0)[0].abs().amax(0).repeat_interleave(2, 0), f.steps(0).max()
+    e = float(((2.0 ** -10 * (q.double().abs() * k).sum(-1) + 2.0 ** -10 * step * q.double().abs().sum(-1)) / math.sqrt(d)).max())
+    tol = (math.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT["bf16"] * want.abs()
+    near = torch.arange(n, device="cuda") >= at // 64 * 64            # (rows whose tiles of keys end with the large one's or go on)
+    tol = tol + 2.0 ** (128 - 40) * near[:, None, None]
+    assert ((o.double() - want).abs() <= tol).all()
+    assert ((lse.double() - sums).abs() <= e + 2.0 ** -11 + 2.0 ** -16 + 2.0 ** -20 * sums.abs()).all()
+
+
+def test_keys_up_to_the_end_of_the_range():
+    """A key of 1e38 takes all weight of rows that see it or none (queries of 2^-12: its scores are beyond 1e30, the others' below 0.01); the other
+    keys' scores, lost beside it or not, weigh them alike to expm1(2 s), s the largest of them."""
+    n, kv, d, at = 1300, 32, 64, 700
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    rows = lambda t: torch.randn(len(t), kv, d, generator=gen, device="cuda")  # noqa: E731
+    keys = rows(torch.arange(n))
+    keys[at] = torch.linspace(-1e38, 1e38, d, device="cuda")
+    f = Filled([n], kv, d, 64, False, lambda t: keys[t], rows)
+    sign = 2.0 * (torch.rand(n, 2 * kv, 1, generator=gen, device="cuda") < 0.5) - 1
+    q = sign * torch.linspace(-1, 1, d, device="cuda") + 0.25 * torch.randn(n, 2 * kv, d, generator=gen, device="cuda")
+    q = (q * 2.0 ** -12).bfloat16()
+    o, lse = f.run(q, [n], True, 0, form(1, 8))
+    want, sums, size, _ = reference(f, q, True)
+    k = f.stored(0)[0].repeat_interleave(2, 1)
+    assert ((q.double() * k[at]).sum(-1).abs() / math.sqrt(d) > 1e30).all()
+    k[at] = 0
+    s = float(q.double().norm(dim=-1).max() * k.norm(dim=-1).max()) / math.sqrt(d)
+    assert s < 0.01
+    assert ((o.double() - want).abs() <= (math.expm1(2 * s) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT["bf16"] * want.abs()).all()
+    assert ((lse.double() - sums).abs()[:at] <= s + 2.0 ** -11 + 2.0 ** -16 + 1e-5).all()
