@@ -9,8 +9,9 @@
 //     digits to it, tile by tile, by a second product with the constant.
 //   - The query row is scaled by a power of two to at most 1 and rounded to fp16 (2^-12; bf16 would move a score of 10 by 0.02);
 //     where that alone is more than an fp16 result's rounding, as rotated queries', it is two fp16 numbers.
-//   - p' is rounded to fp16 too (bf16 would leave 1.4e-3 of error in outputs that fp16 holds to 2e-4): p carries a power of two that
-//     brings the largest step seen so far to 2^7, so that p' neither overflows nor, down to 2^-21 of the largest, loses digits.
+//   - p' is rounded to fp16 too (bf16 would leave 1.4e-3 of error in outputs that fp16 holds to 2e-4): steps carry a power of two that
+//     brings the largest seen so far to 2^7, so that p' neither overflows nor, down to 2^-21 of the largest, loses digits.  (They, and
+//     not p: the sum of p is then the same however large or small values are.)
 //     The centres' share is summed in fp32 from p' as it was rounded: what the codes and a centre make together is off by p's rounding.
 //
 // Products are taken transposed, keys x queries and elements x queries, so that a query is a column, column n the lanes n, n + 16,
@@ -119,13 +120,13 @@ struct Columns {
     float m, l, w;                                // running maximum; sums over the lane's keys of p, and of what centres and halves of steps add
     f32x4 o[D / 16];
     bool far;                                     // some centre of the tile goes with p
-    float limit, up;                              // a power of two that no step seen so far exceeds; log2 of the factor in p
+    float limit;                                  // a power of two that no step seen so far exceeds, nor 2^-64 of a centre that goes with p
+    float factor;                                 // 2^7 / limit: in steps and in sums of values
 };
 
-// All sums times a factor of the column.
+// Sums of values times a factor of the column.
 template <int D>
 __device__ __forceinline__ void scale_sums(Columns<D>& r, float by) {
-    r.l *= by;
     r.w *= by;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
@@ -143,23 +144,28 @@ __device__ __forceinline__ void take_parameters(Columns<D>& r, const Codes<D>& t
         step = mid = 0.0f;
         ks = __builtin_nanf("");
     }
+    const Centre c = split_centre(step, mid);
+    const auto put = [&] {
+        lds[128 + lane] = step * r.factor;
+        lds[256 + lane] = c.with_p * r.factor;
+    };
     lds[lane] = ks;
     lds[64 + lane] = __uint_as_float(kp & 0xffff0000u);
-    lds[128 + lane] = step;
-    const Centre c = split_centre(step, mid);
     put_centre(lds + 192, lane, c.with_step + 0.5f);
-    lds[256 + lane] = c.with_p;
+    put();
     r.far = __any(c.with_p != 0.0f);
-    if (__any(step > r.limit)) {
+    float size = fmaxf(step, fabsf(c.with_p) * 0x1p-64f);
+    if (__any(size > r.limit)) {
 #pragma unroll
-        for (int w = 1; w < 64; w *= 2) step = fmaxf(step, __shfl_xor(step, w));
-        const int x = (int)(__float_as_uint(step) >> 23) - 126;      // step < 2^x
+        for (int w = 1; w < 64; w *= 2) size = fmaxf(size, __shfl_xor(size, w));
+        const int x = (int)(__float_as_uint(size) >> 23) - 126;      // size < 2^x
         const float limit = __uint_as_float((uint32_t)((x < -60 ? -60 : x > 127 ? 127 : x) + 127) << 23);
         if (limit > r.limit) {
-            const int up = 134 - (int)(__float_as_uint(limit) >> 23);
-            scale_sums(r, __builtin_amdgcn_ldexpf(1.0f, up - (int)r.up));
+            const float factor = 0x1p7f / limit;
+            scale_sums(r, factor / r.factor);     // (0 where sums of values are lost beside the new ones)
             r.limit = limit;
-            r.up = (float)up;
+            r.factor = factor;
+            put();
         }
     }
 }
@@ -205,10 +211,12 @@ __device__ __forceinline__ void take_scores(uint32_t (&p)[4 / F][2], Columns<D>&
     // p may grow to 2^8 before the sums are scaled to a new maximum
     if (__any(r.q.f * (mx - r.m) > 8.0f)) {
         const float to = fmaxf(r.m, mx);
-        scale_sums(r, to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(r.q.f * (r.m - to)));
+        const float by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(r.q.f * (r.m - to));
+        scale_sums(r, by);
+        r.l *= by;
         r.m = to;
     }
-    const float off = (r.m == -INFINITY ? 0.0f : r.q.f * r.m) - r.up;
+    const float off = r.m == -INFINITY ? 0.0f : r.q.f * r.m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int key = 16 * (u * F + copy) + 4 * g;
@@ -414,7 +422,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
             all_hi = a.causal && p0 + 1 < to ? p0 + 1 : to;
         }
         r.m = -INFINITY;
-        r.l = r.w = r.limit = r.up = 0.0f;
+        r.l = r.w = r.limit = 0.0f;
+        r.factor = 1.0f;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) r.o[j] = f32x4{0, 0, 0, 0};
         // (the last tile by itself: where loads may be left out, all that was loaded before them is waited for)
@@ -443,7 +452,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
         // a column's results: normalised, with log2 of the sum of e^(scale q.k)
         {
             const float l = column_sum<16>(r.l), w = column_sum<16>(r.w);
-            const float by = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+            const float by = (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) / r.factor;
             float* o = lds_o[wave][lane & 15] + E * g;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -451,7 +460,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
                 for (int j = 0; j < D / 16; j += 4)
                     *reinterpret_cast<f32x4*>(o + e * (D / 16) + j) =
                         f32x4{(r.o[j][e] + w) * by, (r.o[j + 1][e] + w) * by, (r.o[j + 2][e] + w) * by, (r.o[j + 3][e] + w) * by};
-            if (lane < 16) lds_l[wave][lane] = l == 0.0f ? -INFINITY : fmaf(r.q.f, r.m, __builtin_amdgcn_logf(l)) - r.up;
+            if (lane < 16) lds_l[wave][lane] = l == 0.0f ? -INFINITY : fmaf(r.q.f, r.m, __builtin_amdgcn_logf(l));
         }
         // the waves' columns, and the copies among them, join in LDS
         __syncthreads();

@@ -133,8 +133,10 @@ __device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32
         p.vs = p.vm = 0.0f;
         p.ks = __builtin_nanf("");
     }
-    // sixteenths of the largest element that a row could have, EXACT: of the step
-    float kx = EXACT ? 0.0f : fmaf(0.5f, p.ks, 0.0625f * fabsf(p.km)), vx = EXACT ? 0.0625f * p.vs : fmaf(0.5f, p.vs, 0.0625f * fabsf(p.vm));
+    // sixteenths of the largest element that a row could have, EXACT: of the step, and 2^-64 of a centre that goes with p
+    const Centre c = EXACT ? split_centre(p.vs, p.vm) : Centre{0.0f, 0.0f};
+    float kx = EXACT ? 0.0f : fmaf(0.5f, p.ks, 0.0625f * fabsf(p.km));
+    const float vx = EXACT ? 0.0625f * fmaxf(p.vs, 0x1p-64f * fabsf(c.with_p)) : fmaf(0.5f, p.vs, 0.0625f * fabsf(p.vm));
     kx = kx < INFINITY ? kx : 0.0f;               // (keys may be infinite or NaN)
     grew = 0;
     if (__any(kx > keys.limit || vx > values.limit)) {
@@ -146,10 +148,9 @@ __device__ __forceinline__ Parameters take_parameters(Tile<D, EXACT>& to, uint32
         const int lane = thread & 63;
         if (thread >> 6 == 0) to.scale[0][lane] = p.ks;
         if (thread >> 6 == 1) to.scale[1][lane] = p.km;
-        if (thread >> 6 == 2) to.scale[2][lane] = p.vs;
-        const Centre c = split_centre(p.vs, p.vm);
+        if (thread >> 6 == 2) to.scale[2][lane] = __builtin_amdgcn_ldexpf(p.vs, values.up);
         if (thread >> 6 == 3) put_centre(to.scale[3], lane, c.with_step);
-        if (thread >> 6 == 0) to.scale[4][lane] = c.with_p;
+        if (thread >> 6 == 0) to.scale[4][lane] = __builtin_amdgcn_ldexpf(c.with_p, values.up);
         far = __any(c.with_p != 0.0f);
     }
     return p;
@@ -291,7 +292,7 @@ __device__ __forceinline__ void take_keys(f32x16 (&s)[2], const Query<D, 32>& q,
 
 // Scores to probabilities, and their products with the values.
 template <int D, bool EXACT>
-__device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], const Query<D, 32>& q, const Tile<D, EXACT>& t, float f, float up, bool far, int k0,
+__device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], const Query<D, 32>& q, const Tile<D, EXACT>& t, float f, bool far, int k0,
                                             bool whole, int lo, int seen, int lane) {
     const int n = lane & 31, h = lane >> 5;
     constexpr int J = D / 32;
@@ -334,7 +335,7 @@ __device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], c
         r.w *= by;
         r.m = to;
         if (EXACT && far) {                       // (rare: these exponentials are taken again below)
-            const float off = (to == -INFINITY ? 0.0f : to) - up;
+            const float off = to == -INFINITY ? 0.0f : to;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -345,7 +346,7 @@ __device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], c
                 }
         }
     }
-    const float off = (r.m == -INFINITY ? 0.0f : r.m) - up;
+    const float off = (r.m == -INFINITY ? 0.0f : r.m) - (EXACT ? 0.0f : kUp);
     // sixteen keys at a time, the next ones' probabilities beside the products of these
     uint32_t p[2][4];
     const auto weigh = [&](int g) {
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         const bool mine_too = k0 >= from && k0 < any_hi && k0 + kTile > any_lo;
         const int next = k0 + kStride;
         // (the tile's own ranges: the next one may widen them; finite, so that a score of 0 stays 0 beside a key of 2^127)
-        const float f = EXACT ? q.f : fminf(__builtin_amdgcn_ldexpf(q.f, -keys.up), 0x1p127f), up = EXACT ? (float)values.up : kUp;
+        const float f = EXACT ? q.f : fminf(__builtin_amdgcn_ldexpf(q.f, -keys.up), 0x1p127f);
         const bool there = next + lane < to;
         int grew;
         bool far_next = false;
@@ -530,15 +531,12 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
             lds_barrier();
             __builtin_amdgcn_s_setprio(0);
         }
-        if (mine_too) take_scores<D, EXACT>(r, s, q, now, f, up, far, k0, k0 >= all_lo && k0 + kTile <= all_hi, lo, seen, lane);
+        if (mine_too) take_scores<D, EXACT>(r, s, q, now, f, far, k0, k0 >= all_lo && k0 + kTile <= all_hi, lo, seen, lane);
         far = far_next;
         if (grew != 0) {                          // sums go on in the next tile's range
             const float by = __builtin_amdgcn_ldexpf(1.0f, grew);
             scale_sums(r, by);
-            if constexpr (EXACT) {
-                r.l *= by;
-                r.w *= by;
-            }
+            if constexpr (EXACT) r.w *= by;
         }
         lds_barrier();
         if constexpr (TWO) __builtin_amdgcn_s_setprio(1);
@@ -567,14 +565,10 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         const int theirs = __builtin_amdgcn_readfirstlane(h.up[lane]);
         const int up = values.up < theirs ? values.up : theirs;
         const float m = fmaxf(r.m, h.m[lane]);
-        float x = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - m), y = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(h.m[lane] - m);
+        const float x = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - m), y = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(h.m[lane] - m);
         const float xo = x * __builtin_amdgcn_ldexpf(1.0f, up - values.up), yo = y * __builtin_amdgcn_ldexpf(1.0f, up - theirs);
-        if constexpr (EXACT) {
-            x = xo;
-            y = yo;
-        }
         r.l = fmaf(y, h.l[lane], x * r.l);
-        r.w = fmaf(y, h.w[lane], x * r.w);
+        r.w = fmaf(yo, h.w[lane], xo * r.w);
         r.m = m;
         values.up = up;
 #pragma unroll
@@ -584,9 +578,9 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
     }
     if (!there) return;                           // (both lanes of the row)
     const float l = column_sum<32>(r.l), w = EXACT ? column_sum<32>(r.w) : 0.0f;
-    const float by = (l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l)) * (EXACT ? 1.0f : __builtin_amdgcn_ldexpf(1.0f, -values.up));
+    const float by = __builtin_amdgcn_ldexpf(l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l), -values.up);
     float lse = l == 0.0f ? -INFINITY : r.m + __builtin_amdgcn_logf(l);
-    lse -= EXACT ? (float)values.up : kUp;
+    if constexpr (!EXACT) lse -= kUp;
     const int t_row = at.q0 + token, h_row = head * job.group + of;
     const int64_t part_row = ((int64_t)chunk * a.tokens + t_row) * a.heads + h_row;
     float* part = job.part + part_row * D;

@@ -281,3 +281,63 @@ def test_keys_up_to_the_end_of_the_range():
     assert s < 0.01
     assert ((o.double() - want).abs() <= (math.expm1(2 * s) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT["bf16"] * want.abs()).all()
     assert ((lse.double() - sums).abs()[:at] <= s + 2.0 ** -11 + 2.0 ** -16 + 1e-5).all()
+
+
+SHARED, EIGHT = form(0, 4, shared=True), form(0, 8)
+
+
+@pytest.mark.parametrize("dtype,n,counts,kv,want_form", [
+    ("bf16", 20000, [1], 1, SHARED), ("f16", 20000, [1], 1, SHARED), ("bf16", 1500, [1], 1, EIGHT), ("f16", 1500, [1], 1, EIGHT),
+    ("bf16", 900, [300], 32, form(0, 1)), ("f16", 3000, [1300], 32, form(1, 8)), ("bf16", 3000, [1300], 32, form(1, 8))])
+def test_sums_do_not_go_by_the_size_of_values(dtype, n, counts, kv, want_form):
+    """One key whose score is 10 among others of 0, values of 1e37: a weight of e^-10 is not lost.  (The score is off by the rounding of q * scale *
+    log2(e) to fp16; results are compared where their type holds them: p and v are rounded to fp16 besides, or p * step.)"""
+    d = 64
+    line = torch.linspace(-1e37, 1e37, d, device="cuda")
+    keys = lambda t: ((t == 7) * 2.0)[:, None, None].repeat(1, kv, d)  # noqa: E731
+    f = Filled([n], kv, d, 64, False, keys, lambda t: torch.where((t == 7)[:, None, None], -line, line).expand(-1, kv, d))
+    q = torch.full((sum(counts), 2 * kv, d), 0.625, device="cuda").to(DT[dtype])
+    o, lse = f.run(q, counts, False, 0, want_form)
+    one, rest = math.exp(10), n - 1
+    assert ((lse.double() - math.log(one + rest)).abs() <= 10 * 2.0 ** -11 + 1e-4).all()
+    if dtype == "bf16":
+        v = f.stored(0)[1]
+        want = (v[7, 0] * one + v[8, 0] * rest) / (one + rest)
+        tol = (math.expm1(2 * 10 * 2.0 ** -11) + 2.0 ** -10 + 2.0 ** -16) * v[8, 0].abs() + U_OUT[dtype] * want.abs()
+        assert ((o.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,n,kv,many", [("bf16", 400, 1, 0), ("f16", 400, 1, 0), ("f16", 1300, 32, 1), ("bf16", 1300, 32, 1)])
+def test_log_sums_beside_a_large_value(dtype, n, kv, many):
+    """Values of 2^-57 and one of 1e37 behind them: the sums are those of the scores, for rows that see it and for rows that do not."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    d, at = 64, n // 2 + 5
+    keys, values = [torch.randn(n, kv, d, generator=gen, device="cuda") for _ in range(2)]
+    values *= 2.0 ** -57
+    values[at] = torch.linspace(-1e37, 1e37, d, device="cuda")
+    f = Filled([n], kv, d, 64, True, lambda t: keys[t], lambda t: values[t])
+    q = torch.randn(n, 2 * kv, d, generator=gen, device="cuda").to(DT[dtype])
+    o, lse = f.run(q, [n], True, 0, dict(many=many))
+    _, sums, _, _ = reference(f, q, True)
+    k, step = f.stored(0)[0].abs().amax(0).repeat_interleave(2, 0), f.steps(0).max()
+    x = (q.double() @ torch.tensor(ref.sylvester(d)).cuda()).abs()
+    e = float(((2.0 ** -10 * (x * k).sum(-1) + 2.0 ** -10 * step * x.sum(-1)) / math.sqrt(d)).max())
+    assert ((lse.double() - sums).abs() <= e + 2.0 ** -11 + 2.0 ** -16 + 2.0 ** -20 * sums.abs()).all()
+    assert not torch.isnan(o).any()
+
+
+def test_a_large_centre_beside_small_steps():
+    """A flat row of 1e25 among values of 2^-48, which set the factor of sums: nothing overflows."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    n, d, at = 300, 64, 9
+    keys, values = [torch.randn(n, 1, d, generator=gen, device="cuda") for _ in range(2)]
+    values *= 2.0 ** -48
+    values[at] = 1e25
+    f = Filled([n], 1, d, 64, False, lambda t: keys[t], lambda t: values[t])
+    q = torch.randn(1, 4, d, generator=gen, device="cuda").bfloat16()
+    o, lse = f.run(q, [1], True, 0, dict(many=0))
+    want, sums, size, _ = reference(f, q, True)
+    k, step = f.stored(0)[0].abs().amax(0), f.steps(0).max()
+    e = float(((2.0 ** -10 * (q.double().abs() * k).sum(-1) + 2.0 ** -10 * step * q.double().abs().sum(-1)) / math.sqrt(d)).max())
+    assert ((o.double() - want).abs() <= (math.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT["bf16"] * want.abs()).all()
+    assert ((lse.double() - sums).abs() <= e + 2.0 ** -16 + 2.0 ** -20 * sums.abs()).all()
