@@ -48,8 +48,9 @@ class PagePool:
 
     def extend(self, seq, tokens: int) -> Tuple[List[int], List[Tuple[int, int]]]:
         """Room for `tokens` more tokens: (their slots, pages to copy first).  A page that other sequences hold too is copied
-        before it is written to: (src, dst) pairs for kv4_copy_pages.  MemoryError where the pool has too few pages; nothing has
-        changed then."""
+        before it is written to: (src, dst) pairs for kv4_copy_pages.  Pairs of consecutive calls of extend may be joined in one
+        copy; they have to be launched before any other call that changes the pool (fork, truncate, free, compact): pages could be
+        handed out again that are still to be read.  MemoryError where the pool has too few pages; nothing has changed then."""
         if tokens < 0:
             raise ValueError("tokens must be >= 0")
         if tokens == 0:

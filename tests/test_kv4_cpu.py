@@ -254,3 +254,49 @@ def test_pool_against_a_model():
 @pytest.mark.parametrize("o", [(0, 128), (512, 0), (512, 127), (100, 128), (0, 0)])
 def test_attention_refuses_results_that_overlap(L, o):
     assert L.rq_kv4_attention(None, cache(), 64, 0, 3, 4, 512, 128, 64, 3, 2, 64, None, 0.1, 1, 0, 32, 4096, *o, None, None, 0, None) == ARG
+
+
+def test_pairs_of_consecutive_extends_make_one_copy():
+    """A server's step: every sequence gets room, then one copy of all pairs, all pages read before any is written, then the tokens.  Pairs name no
+    page in both places, and every sequence keeps its tokens."""
+    rng, P = random.Random(5), 16
+    pool, mem, truth, n = PagePool(80, P), {}, {0: []}, 0
+    pool.add(0)
+    joined = 0
+    for step in range(400):
+        tokens, pairs = [], []
+        for s in rng.sample(sorted(truth), len(truth)):
+            k = rng.choice((0, 1, 1, 1, 7, 20))
+            try:
+                slots, copies = pool.extend(s, k)
+            except MemoryError:
+                continue
+            tokens += [(x, s, (s, len(truth[s]) + i, step)) for i, x in enumerate(slots)]
+            truth[s] = truth[s] + [(s, len(truth[s]) + i, step) for i in range(len(slots))]
+            pairs += copies
+        src, dst = [a for a, _ in pairs], [b for _, b in pairs]
+        assert not set(src) & set(dst) and len(set(dst)) == len(dst)
+        joined = max(joined, len(pairs))
+        old = dict(mem)
+        for a, b in pairs:
+            for i in range(P):
+                if a * P + i in old:
+                    mem[b * P + i] = old[a * P + i]
+        for x, _, value in tokens:
+            mem[x] = value
+        for s, rows in truth.items():
+            t = pool.table(s)
+            assert [mem[t[i // P] * P + i % P] for i in range(len(rows))] == rows
+        s = rng.choice(sorted(truth))
+        if len(truth) < 6:
+            n += 1
+            pool.fork(s, n)
+            truth[n] = list(truth[s])
+        elif rng.random() < 0.5:
+            pool.free(s)
+            del truth[s]
+        else:
+            k = rng.randrange(len(truth[s]) + 1)
+            pool.truncate(s, k)
+            truth[s] = truth[s][:k]
+    assert joined > 1
