@@ -341,3 +341,45 @@ def test_a_large_centre_beside_small_steps():
     e = float(((2.0 ** -10 * (q.double().abs() * k).sum(-1) + 2.0 ** -10 * step * q.double().abs().sum(-1)) / math.sqrt(d)).max())
     assert ((o.double() - want).abs() <= (math.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT["bf16"] * want.abs()).all()
     assert ((lse.double() - sums).abs() <= e + 2.0 ** -16 + 2.0 ** -20 * sums.abs()).all()
+
+
+FORMS = [
+    # few rows: keys shared out, 4, 8 and 16 rows a tile; a row tile a workgroup of eight, four waves and of one
+    ([8192], [1], 2, 4, 128, 64, True, 0, SHARED),
+    ([8000, 100, 3000], [1] * 3, 1, 1, 64, 16, True, 0, SHARED),
+    ([4000, 900], [1] * 2, 2, 8, 64, 32, True, 0, SHARED),
+    ([8000], [1], 2, 16, 128, 256, True, 0, SHARED),
+    ([20000], [8], 1, 2, 64, 64, True, 0, SHARED),
+    ([8192] * 4, [1] * 4, 2, 4, 128, 64, True, 4096, SHARED),
+    ([30000, 700], [1] * 2, 1, 40, 64, 16, False, 5000, SHARED),
+    ([2000] * 3, [1] * 3, 4, 16, 128, 128, True, 0, EIGHT),
+    ([1000, 300, 64], [1] * 3, 4, 4, 64, 16, True, 0, EIGHT),
+    ([3000, 50, 2000], [1, 40, 1], 8, 4, 64, 64, True, 0, EIGHT),
+    ([3000] * 20, [1] * 20, 32, 2, 64, 64, True, 0, form(0, 4)),
+    ([2000, 700], [300, 500], 4, 2, 128, 16, False, 1000, form(0, 4)),
+    ([300, 129, 64, 1, 200] * 8, [1] * 40, 32, 1, 64, 64, True, 0, form(0, 1)),
+    ([300, 129, 64, 1, 200] * 8, [1] * 40, 32, 1, 128, 16, True, 100, form(0, 1)),
+    # many rows: four waves, keys in chunks, two groups of four, eight waves; with windows, causal and not
+    ([4000], [4000], 8, 2, 64, 16, True, 1000, form(1, 4)),
+    ([4000], [3999], 8, 2, 128, 64, False, 1000, form(1, 4)),
+    ([8192], [1024], 4, 4, 128, 64, True, 4096, CHUNKS),
+    ([8192], [700], 4, 4, 128, 32, True, 0, CHUNKS),
+    ([8192], [700], 4, 4, 64, 64, False, 0, CHUNKS),
+    ([3900], [3900], 8, 1, 64, 16, True, 3000, form(1, 4, 2)),
+    ([4096, 3000], [4096, 2000], 1, 4, 64, 64, False, 1000, form(1, 4, 2)),
+    ([4096], [4096], 8, 1, 64, 64, True, 0, form(1, 4, 2)),
+    ([4096], [2048], 8, 4, 128, 64, True, 0, {"bf16": form(1, 4, 2), "f16": form(1, 4)}),
+    ([4096], [4096], 8, 2, 128, 64, True, 1500, {"bf16": form(1, 4), "f16": form(1, 4)}),
+    ([2500], [2500], 32, 2, 128, 64, True, 1000, form(1, 8)),
+    ([2500], [2500], 32, 2, 64, 16, False, 1000, form(1, 8)),
+    ([1300, 900], [1300, 700], 32, 2, 128, 16, True, 0, form(1, 8)),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", range(len(FORMS)))
+def test_every_form_takes_every_key_once(case, dtype):
+    *shape, want_form = FORMS[case]
+    want_form = want_form.get(dtype, want_form)
+    check_coverage(*shape, dtype, want_form)
+    check_values(*shape, dtype, want_form)
