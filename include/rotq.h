@@ -461,16 +461,22 @@ size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int hea
  * q_start[b] .. q_start[b + 1] - 1 and stand at its last positions: query i of n at kv_lens[b] - n + i.  A causal query sees
  * positions up to its own, others all of the sequence; with a window w > 0 only those later than its own minus w.  A query that sees
  * nothing gets zeros (and -infinity in lse).
- * Query head x reads kv head x / (heads / kv_heads).  Queries are rotated as the keys were (h) and rounded to fp16 after scaling each
- * row by a power of two (for fp16 results: to two fp16 numbers), probabilities times the steps of the values are rounded to fp16, all
- * else is fp32 - but that bf16 results of many queries a sequence (over 32 rows of a kv head) come from elements rounded to fp16
- * and from probabilities rounded to fp16.
+ * Query head x reads kv head x / (heads / kv_heads).
+ *
+ * What is rounded: queries are rotated as the keys were (h), multiplied by scale * log2(e) and by a power of two of the row's, in fp32,
+ * and rounded to fp16 (for fp16 results: to two fp16 numbers); probabilities times the steps of the values are rounded to fp16; all else
+ * is fp32.  bf16 results of the kernel for many queries (rq_kv4_attention_plan: many) come from keys, values and
+ * probabilities rounded to fp16 each, weights below 2^-32 of a row's largest count as 0 there.
+ * Steps (there: elements) carry a power of two on their way into fp16, which follows the largest among the keys that a row tile has come
+ * to, whether all of its rows see that key or not.  Beside a value whose step is the largest, values lose digits whose steps are
+ * less than 2^-20 of it, and are lost below 2^-31; there: elements of keys and of values below 2^-28 of the largest, and below 2^-40.
+ * A key or value that is not finite makes the results of rows that see it NaN, and of no others.
  *   Q            [in]  DEVICE, element [token][head][i] at token * q_token_stride + head * q_head_stride + i
  *   dtype        [in]  RQ_BF16 or RQ_F16, of Q and O
  *   tokens       [in]  0 .. 2^24
  *   heads        [in]  a multiple of kv_heads, at most 256 times it
- *   table        [in]  DEVICE, batch x width int32 page numbers; those behind a sequence's last page are not read, a number
- *                      that is not in the cache stands for page 0
+ *   table        [in]  DEVICE, batch x width int32 page numbers; what stands behind a sequence's last page does not matter, and a
+ *                      number that is not in the cache stands for page 0
  *   kv_lens      [in]  DEVICE, batch int32; values are taken to be in 0 .. max_len
  *   q_start      [in]  DEVICE, batch + 1 int32, ascending from 0 to tokens; NULL: one token a sequence (tokens == batch)
  *   scale        [in]  of the scores, finite, > 0

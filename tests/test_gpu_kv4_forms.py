@@ -383,3 +383,35 @@ def test_every_form_takes_every_key_once(case, dtype):
     want_form = want_form.get(dtype, want_form)
     check_coverage(*shape, dtype, want_form)
     check_values(*shape, dtype, want_form)
+
+
+@pytest.mark.parametrize("dtype,n,kv,many,big", [("bf16", 400, 1, 0, 14), ("f16", 400, 1, 0, 14), ("f16", 1300, 32, 1, 14), ("bf16", 1300, 32, 1, 24)])
+def test_rows_beside_a_large_one_that_they_do_not_see(dtype, n, kv, many, big):
+    """A key and value row 2^big times the others.  It sets the range of the row tiles that come to it, and rows of these that do not see it keep
+    their results, but for what the header says is lost: of p * step what is below 2^-25 / 2^6 of the largest step, with elements up to 8 steps;
+    bf16 results of many rows: of elements 2^-40 of twice the largest (8 steps and the centre)."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    d, at = 64, n // 2 + 5
+    keys, values = [torch.randn(n, kv, d, generator=gen, device="cuda") for _ in range(2)]
+    for x in (keys, values):
+        x[at] *= 2.0 ** big
+    f = Filled([n], kv, d, 64, True, lambda t: keys[t], lambda t: values[t])
+    q = torch.randn(n, 2 * kv, d, generator=gen, device="cuda").to(DT[dtype])
+    o, lse = f.run(q, [n], True, 0, dict(many=many))
+    o, lse, q = o[:at], lse[:at], q[:at]
+    k, v = f.stored(0)
+    step, largest = f.steps(0)[:at].max(), max(float(k.abs().max()), float(v.abs().max()))
+    hd = torch.tensor(ref.sylvester(d)).cuda()
+    for h in range(2 * kv):
+        x = q[:, h].double() @ hd
+        s = (x @ k[:at, h // 2].t() / math.sqrt(d)).masked_fill(torch.ones(at, at, dtype=torch.bool, device="cuda").triu(1), -math.inf)
+        p, total = torch.softmax(s, -1), torch.logsumexp(s, -1)
+        lost_k = 2.0 ** -40 * 2 * 2 * largest if many and dtype == "bf16" else 0.0
+        e = ((2.0 ** -10 * (x.abs() @ k[:at, h // 2].abs().amax(0)) + 2.0 ** -10 * step * x.abs().sum(-1) + lost_k * x.abs().sum(-1)) / math.sqrt(d))[:, None]
+        ones = torch.exp(total - s.amax(-1))[:, None]                     # the sum of weights, the largest 1
+        seen = torch.arange(1, at + 1, device="cuda")[:, None]
+        lost_v = lost_k if many and dtype == "bf16" else seen / ones * 8 * 2.0 ** -31 * (2 * largest / 15)
+        want, size = p @ v[:at, h // 2], p @ v[:at, h // 2].abs()
+        tol = (torch.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT[dtype] * want.abs() + lost_v
+        assert ((o[:, h].double() - want).abs() <= tol).all(), h
+        assert ((lse[:, h].double() - total).abs() <= e[:, 0] + 2.0 ** -11 + 2.0 ** -16 + 2.0 ** -20 * total.abs()).all(), h
