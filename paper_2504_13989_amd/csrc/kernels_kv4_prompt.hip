@@ -501,8 +501,9 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         Tile<D, EXACT>& then = tiles[at_tile];
         const bool mine_too = k0 >= from && k0 < any_hi && k0 + kTile > any_lo;
         const int next = k0 + kStride;
-        // (the tile's own ranges: the next one may widen them; finite, so that a score of 0 stays 0 beside a key of 2^127)
-        const float f = EXACT ? q.f : fminf(__builtin_amdgcn_ldexpf(q.f, -keys.up), 0x1p127f);
+        // (the tile's own ranges: the next one may widen them; neither infinite nor 0, so that a score of 0 stays 0 beside a key of 2^127
+        // and one of -infinity what it is where queries and keys are tiny)
+        const float f = EXACT ? q.f : __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(q.f, -keys.up), 0x1p-126f, 0x1p127f);
         const bool there = next + lane < to;
         int grew;
         bool far_next = false;

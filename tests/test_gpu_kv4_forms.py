@@ -415,3 +415,20 @@ def test_rows_beside_a_large_one_that_they_do_not_see(dtype, n, kv, many, big):
         tol = (torch.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -16) * size + U_OUT[dtype] * want.abs() + lost_v
         assert ((o[:, h].double() - want).abs() <= tol).all(), h
         assert ((lse[:, h].double() - total).abs() <= e[:, 0] + 2.0 ** -11 + 2.0 ** -16 + 2.0 ** -20 * total.abs()).all(), h
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,kv,many", [(400, 1, 0), (1300, 32, 1)])
+def test_tiny_queries_and_keys(n, kv, many, dtype):
+    """Queries of 2^-105 against keys of 2^-60 (fp16: of 2^-24 against the same): all scores are 0 next to 1, and hidden keys stay hidden."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    d = 64
+    keys, values = [torch.randn(n, kv, d, generator=gen, device="cuda") for _ in range(2)]
+    f = Filled([n], kv, d, 64, False, lambda t: keys[t] * 2.0 ** -60, lambda t: values[t])
+    q = (torch.randn(n, 2 * kv, d, generator=gen, device="cuda") * 2.0 ** (-105 if dtype == "bf16" else -24)).to(DT[dtype])
+    o, lse = f.run(q, [n], True, 0, dict(many=many))
+    v = f.stored(0)[1]
+    count = torch.arange(1, n + 1, device="cuda", dtype=torch.float64)[:, None, None]
+    want, size = (x.cumsum(0).div(count).repeat_interleave(2, 1) for x in (v, v.abs()))
+    assert ((o.double() - want).abs() <= (2.0 ** -10 + 2.0 ** -16) * size + U_OUT[dtype] * want.abs()).all()
+    assert ((lse.double() - count[..., 0].log()).abs() <= 1e-5).all()
