@@ -470,7 +470,8 @@ size_t rq_kv4_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int hea
  * Steps (there: elements) carry a power of two on their way into fp16, which follows the largest among the keys that a row tile has come
  * to, whether all of its rows see that key or not.  Beside a value whose step is the largest, values lose digits whose steps are
  * less than 2^-20 of it, and are lost below 2^-31; there: elements of keys and of values below 2^-28 of the largest, and below 2^-40.
- * A key or value that is not finite makes the results of rows that see it NaN, and of no others.
+ * A key or value that is not finite makes the results of rows that see it NaN, and of no others.  (So may a finite key whose product
+ * with a query row, scaled to at most 1, leaves fp32: elements of 2^120 and more.)
  *   Q            [in]  DEVICE, element [token][head][i] at token * q_token_stride + head * q_head_stride + i
  *   dtype        [in]  RQ_BF16 or RQ_F16, of Q and O
  *   tokens       [in]  0 .. 2^24

@@ -7,7 +7,7 @@
 //   - A code becomes an fp16 number by masking it into the mantissa of 1024 or 64: two codes an instruction.  The constants' share
 //     is known and taken off in fp32: for keys in the accumulator's initial value; for values, whose sums run over all keys and would lose
 //     digits to it, tile by tile, by a second product with the constant.
-//   - The query row is scaled by a power of two to at most 1 and rounded to fp16 (2^-12; bf16 would move a score of 10 by 0.02);
+//   - The query row is scaled by a power of two to at most 1 and rounded to fp16 (2^-11; bf16 would move a score of 10 by 0.02);
 //     where that alone is more than an fp16 result's rounding, as rotated queries', it is two fp16 numbers.
 //   - p' is rounded to fp16 too (bf16 would leave 1.4e-3 of error in outputs that fp16 holds to 2e-4): steps carry a power of two that
 //     brings the largest seen so far to 2^7, so that p' neither overflows nor, down to 2^-21 of the largest, loses digits.  (They, and
@@ -27,8 +27,8 @@
 // 141 us where two a unit took 109).  The waves take a workgroup's tiles in turn.  A tile's codes are read into the registers of the one before
 // as soon as those are used up, keys during the softmax, values during the next keys' products.
 // 16 sequences x 32 heads x 8192 positions of 128, bf16: 87 .. 90 us, 6.3 to 6.5 TB/s of codes and parameters (reading alone
-// reaches 6.9); vector issue 43 %, matrix cores 24 %.  Six sequences of up to 65411 positions, 64 heads to 8, fp16: 46 us and 5.1.
-// Five chunks of prompts, 14 heads of 64 to 2, window 1024, fp16: 44 us, vector issue 61 %.
+// reaches 6.9); vector issue 44 %, matrix cores 24 %.  Six sequences of up to 65411 positions, 64 heads to 8, fp16: 46 us and 5.2.
+// Five chunks of prompts, 14 heads of 64 to 2, window 1024, fp16: 44 us, vector issue 62 %.
 #include "kv4_attention.h"
 
 #include <type_traits>

@@ -8,15 +8,15 @@
 // the order in which scores leave the matrix cores, so that p enters them again as it is.  The next tile is unpacked into
 // another part of LDS beside the products of keys on this one; its codes were loaded two steps earlier.
 //   - bf16 results: operands are the elements themselves, (code - 7.5) step + mid, times a power of two that holds the largest
-//     seen so far in fp16's range (rounded to fp16 once, 2^-12: less than the result's rounding; steps and centres, bf16, are exact in fp16).  Scores need no step or centre.
+//     seen so far in fp16's range (rounded to fp16 once, 2^-11: less than the result's rounding; steps and centres, bf16, are exact in fp16).  Scores need no step or centre.
 //   - fp16 results (EXACT): operands are codes - 7.5, which are exact, and steps and centres are applied to the scores as in the other
 //     kernel; four instructions a score and one product more.  Queries are two fp16 numbers.
 // A value row that is not finite becomes zeros and its key NaN: queries that do not see it stay what they are.
 //
-// 8192 tokens against themselves, 32 heads to 8 of keys, 128 elements: bf16 600 .. 635 us, 890 TFLOP/s of the products that a causal
-// prompt needs (a large matrix product: 1360); fp16 856.  A step of two waves a SIMD takes 4600 cycles: vector instructions
+// 8192 tokens against themselves, 32 heads to 8 of keys, 128 elements: bf16 597 .. 625 us, 880 to 920 TFLOP/s of the products that a causal
+// prompt needs (a large matrix product: 1360); fp16 864 .. 868.  A step of two waves a SIMD takes 4600 cycles: vector instructions
 // take 4.5 each and exponentials 9.7, some 2600 of them, the issue of 64 products 500; the rest is waiting for each other (counters: vector
-// issue 50 %, matrix cores 40 %, LDS 33 %).  Operands read two groups ahead, unpacking after and not beside the products: no faster.
+// issue 51 %, matrix cores 41 %, LDS 34 %).  Operands read two groups ahead, unpacking after and not beside the products: no faster.
 #include "kv4_attention.h"
 
 namespace rq {
