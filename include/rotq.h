@@ -514,6 +514,58 @@ int rq_kv4_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int 
                           int64_t max_len, int compute_units, rq_kv4_plan_t* plan);
 
 /*
+ * How much attention the positions of cached sequences receive, for deciding which of them to keep:
+ *     weights[b][y][j] <- decay * weights[b][y][j] + sum over the queries of sequence b and the heads x of kv head y of
+ *                         exp(scale * q . k_j - lse)
+ * for the positions j < kv_lens[b]; a query adds to positions that it sees only, and weights behind a sequence's last position stay what
+ * they are.  With decay 0 the old weights are not read.
+ * Arguments and what a query sees are rq_kv4_attention's; its lse is the one wanted here (that of bf16 results is off by the rounding of
+ * their queries, about 2^-12 of a score: so are the weights).  Here queries are rounded to 22 bits, all else is fp32.  Not finite: a key makes its
+ * own weights NaN, a query those of all positions that it sees.
+ *   lse          [in]  DEVICE, tokens x heads floats
+ *   tokens       [in]  0 .. 2^24 (none: the weights decay)
+ *   decay        [in]  0 .. 1
+ *   weights      [inout] DEVICE, element [b][y][j] at b * w_seq_stride + y * w_head_stride + j; rows of max_len must not overlap
+ *   workspace    [in]  DEVICE, >= rq_kv4_attention_weights_workspace(...) bytes, 16-byte aligned, scratch; NULL where that is 0
+ * The same call gives the same bits.  Errors: RQ_ERR_ARG, RQ_ERR_HIP.
+ */
+size_t rq_kv4_attention_weights_workspace(const rq_kv4_t* cache, int64_t tokens, int heads, int batch, int decode, int window, int64_t max_len);
+int rq_kv4_attention_weights(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* Q, int dtype, int64_t tokens, int heads,
+                             int64_t q_token_stride, int64_t q_head_stride, const float* lse, const int32_t* table, int batch, int width,
+                             const int32_t* kv_lens, const int32_t* q_start, float scale, int causal, int window, int64_t max_len, float decay,
+                             float* weights, int64_t w_seq_stride, int64_t w_head_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The positions of each layer, sequence and kv head that are worth keeping: the first `sinks`, the last `recent`, and of those between the
+ * ones with the largest weights, `keep` in all (ties: the lower positions; NaN is less than any number).
+ *   weights      [in]  DEVICE, element [layer][b][y][j] at layer * w_layer_stride + b * w_seq_stride + y * w_head_stride + j
+ *   n            [in]  positions of a row of weights, at most 2^30; kv_lens are taken to be in 0 .. n
+ *   kv_lens      [in]  DEVICE, batch int32
+ *   keep         [in]  at least sinks + recent
+ *   index        [out] DEVICE, layers x batch x kv_heads x keep int32, each row ascending; a sequence of no more than `keep` positions keeps
+ *                      all of them, and -1 stands in the places behind
+ * Errors: RQ_ERR_ARG, RQ_ERR_HIP.
+ */
+int rq_kv4_select(const float* weights, int layers, int batch, int kv_heads, int64_t n, int64_t w_layer_stride, int64_t w_seq_stride,
+                  int64_t w_head_stride, const int32_t* kv_lens, int64_t keep, int64_t sinks, int64_t recent, int32_t* index, void* stream);
+
+/*
+ * The kept rows moved together: position i of a kv head becomes what its position index[layer][b][y][i] was, as it is stored.  A row
+ * with a negative index or one that the table has no page for is not written.
+ * In place (new_table NULL): index has to ascend, from at least i at place i on, as rq_kv4_select's does; a page must not be another
+ * sequence's too.  Else the pages of new_table are written, none of which may be read by the call, nor be named twice.
+ *   layers, layer_stride   as in rq_kv4_copy_pages; the tables hold for all layers
+ *   index        [in]  DEVICE, layers x batch x kv_heads x keep int32
+ *   table        [in]  DEVICE, batch x width int32;  new_table: batch x new_width.  Places of `keep` positions at least where they are written
+ *   weights      [inout] DEVICE, as in rq_kv4_select, or NULL: moved along in place (index ascending here too); 0 from there to the end of
+ *                      a row, for tokens to come.  n at least keep; rows must not overlap
+ * Errors: RQ_ERR_ARG, RQ_ERR_HIP.
+ */
+int rq_kv4_evict(const rq_kv4_t* cache, int layers, int64_t layer_stride, const int32_t* index, int64_t keep, const int32_t* table, int batch, int width,
+                 const int32_t* new_table, int new_width, float* weights, int64_t n, int64_t w_layer_stride, int64_t w_seq_stride,
+                 int64_t w_head_stride, void* stream);
+
+/*
  * Select the kernel family for subsequent hot-path calls on this handle (testing /
  * measurement): 0 = automatic (fastest available), 1 = the general LDS kernel; for long
  * power-of-two rows 2 = one wave per row at any row count, 3 / 4 = a row split over 2 / 4 waves

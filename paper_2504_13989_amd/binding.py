@@ -94,6 +94,12 @@ def lib() -> C.CDLL:
     L.rq_kv4_attention.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, i32, i32, vp, vp, C.c_float, i32, i32, i64, vp,
                                    i64, i64, vp, vp, C.c_size_t, vp]
     L.rq_kv4_attention_plan.argtypes = [kv4p, i32, i64, i32, i32, i32, i32, i32, i64, i32, C.POINTER(RqKv4Plan)]
+    L.rq_kv4_attention_weights_workspace.argtypes = [kv4p, i64, i32, i32, i32, i32, i64]
+    L.rq_kv4_attention_weights_workspace.restype = C.c_size_t
+    L.rq_kv4_attention_weights.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, vp, i32, i32, vp, vp, C.c_float, i32, i32, i64, C.c_float,
+                                           vp, i64, i64, vp, C.c_size_t, vp]
+    L.rq_kv4_select.argtypes = [vp, i32, i32, i32, i64, i64, i64, i64, vp, i64, i64, i64, vp, vp]
+    L.rq_kv4_evict.argtypes = [kv4p, i32, i64, vp, i64, vp, i32, i32, vp, i32, vp, i64, i64, i64, i64, vp]
     L.rq_strerror.argtypes = [i32]
     L.rq_strerror.restype = C.c_char_p
     for name in ("rq_hadamard_build", "rq_hadamard_info", "rq_hadamard_dense", "rq_next_order",
@@ -377,3 +383,26 @@ def kv4_attention(h: Optional[Hadamard], cache: KV4Cache, q, table, kv_lens, q_s
     [tokens, heads]) receives the logarithms of the softmax sums.  `out` must not overlap q, nor its rows each other."""
     return (_nat or _native()).kv4_attention(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q,
                                              table, kv_lens, q_start, scale, causal, window, max_len, out, lse, workspace, stream)
+
+
+def kv4_attention_weights(h: Optional[Hadamard], cache: KV4Cache, q, lse, table, kv_lens, weights, q_start=None, scale: Optional[float] = None,
+                          causal: bool = True, window: int = 0, decay: float = 1.0, max_len: Optional[int] = None, workspace=None, stream=None) -> None:
+    """rq_kv4_attention_weights: weights (float32 [batch, kv_heads, positions], rows may be strided) become decay times what they were plus
+    the attention that each cached position receives from q, summed over queries and over the heads of a kv head.  lse: what
+    kv4_attention has returned for the same q, table, kv_lens, q_start, scale, causal and window."""
+    (_nat or _native()).kv4_attention_weights(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q, lse,
+                                              table, kv_lens, weights, q_start, scale, causal, window, decay, max_len, workspace, stream)
+
+
+def kv4_select(weights, kv_lens, keep: int, sinks: int = 0, recent: int = 0, index=None, stream=None):
+    """rq_kv4_select: the `keep` positions of each row of weights (float32 [(layers,) batch, kv_heads, positions]) to keep: the first `sinks`,
+    the last `recent` and the largest between them, ascending, as int32 [(layers,) batch, kv_heads, keep]; -1 behind the last position of a
+    sequence that has no more than `keep`."""
+    return (_nat or _native()).kv4_select(weights, kv_lens, keep, sinks, recent, index, stream)
+
+
+def kv4_evict(cache: KV4Cache, index, table, new_table=None, weights=None, stream=None) -> None:
+    """rq_kv4_evict: position i of each kv head becomes its position index[(layer,) b, head, i] (int32, ascending), in place or in the pages of
+    new_table (int32 [batch, new width]), in all layers of the cache.  weights (float32 [(layers,) batch, kv_heads, positions]) move along,
+    and are 0 behind."""
+    (_nat or _native()).kv4_evict(cache.data, cache.kv_heads, cache.head_dim, cache.page_size, index, table, new_table, weights, stream)

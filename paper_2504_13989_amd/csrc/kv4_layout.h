@@ -64,4 +64,32 @@ size_t kv4_attention_workspace(const Kv4& c, const Kv4Attention& a, int num_cu);
 rq_kv4_plan_t kv4_attention_plan(const Kv4& c, const Kv4Attention& a, int num_cu);
 int kv4_attention(const Kv4& c, const Kv4Attention& a, int num_cu, float* workspace, hipStream_t s);
 
+
+// Attention that positions have received, added up (q, lse, table ... of `a`; its o is not looked at).
+struct Kv4Weights {
+    Kv4Attention a;
+    float* weights;                               // [batch][kv_heads][positions]
+    int64_t w_seq, w_head;                        // strides
+    float decay;
+};
+size_t kv4_weights_workspace(const Kv4& c, const Kv4Attention& a, int num_cu);
+int kv4_weights(const Kv4& c, const Kv4Weights& w, int num_cu, void* workspace, hipStream_t s);
+
+struct Kv4Select {
+    const float* weights;                         // [layers][batch][kv_heads][n]
+    int64_t w_layer, w_seq, w_head;
+    const int32_t* kv_lens;
+    int layers, batch, kv_heads, n, keep, sinks, recent;
+    int32_t* index;                               // [layers][batch][kv_heads][keep]
+};
+int kv4_select(const Kv4Select& a, hipStream_t s);
+
+struct Kv4Evict {
+    const int32_t *index, *table, *new_table;     // new_table null: in place
+    float* weights;                               // or null
+    int64_t w_layer, w_seq, w_head, layer_bytes;
+    int layers, batch, keep, width, new_width, n;
+};
+int kv4_evict(const Kv4& c, const Kv4Evict& a, hipStream_t s);
+
 }  // namespace rq

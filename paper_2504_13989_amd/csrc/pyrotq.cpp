@@ -698,6 +698,150 @@ PyObject* kv4_attention(PyObject* const* a) {
     return o.take();
 }
 
+// A launch goes to the current device: memory of another one is not its own.
+void on_current(c10::Device device) {
+    if (device.index() != c10::hip::current_device()) raise(PyExc_ValueError, "tensors must be on the current device");
+}
+
+// float32 [(layers,) batch, kv_heads, n] with contiguous rows.
+struct Weights {
+    float* data;
+    int64_t layers, batch, heads, n, layer, seq, head;
+    bool layered;
+    Weights(const at::Tensor& t, const char* text) {
+        const int64_t nd = t.dim();
+        if (!t.is_cuda() || t.scalar_type() != at::kFloat || nd < 3 || nd > 4 || (t.size(nd - 1) > 1 && t.stride(nd - 1) != 1)) raise(PyExc_ValueError, text);
+        layered = nd == 4;
+        layers = layered ? t.size(0) : 1;
+        batch = t.size(nd - 3);
+        heads = t.size(nd - 2);
+        n = t.size(nd - 1);
+        // (a dimension of one has any stride)
+        head = heads > 1 ? t.stride(nd - 2) : 0;
+        seq = batch > 1 ? t.stride(nd - 3) : 0;
+        layer = layers > 1 ? t.stride(0) : 0;
+        data = static_cast<float*>(t.data_ptr());
+        if (layers > INT32_MAX || batch > INT32_MAX || heads > INT32_MAX) raise(PyExc_ValueError, text);
+    }
+};
+
+// (handle, data, kv_heads, head_dim, page_size, q, lse, table, kv_lens, weights, q_start, scale, causal, window, decay, max_len, workspace, stream)
+PyObject* kv4_attention_weights(PyObject* const* a) {
+    const char* where = "rq_kv4_attention_weights";
+    const rq_hadamard_t* h = handle(a[0]);
+    const Cache c(a + 1, where);
+    c.one_layer();
+    on_current(c.device);
+    const HeadRows q(tensor(a[5]), c, "q must be a device tensor [tokens, heads, head_dim] with contiguous rows");
+    const at::Tensor& lse = tensor(a[6]);
+    if (!lse.is_cuda() || lse.device() != c.device || lse.scalar_type() != at::kFloat || !lse.is_contiguous() || lse.numel() != q.tokens * q.heads)
+        raise(PyExc_ValueError, "lse must be a contiguous float32 device tensor [tokens, heads]");
+    const at::Tensor& table = numbers(a[7], at::kInt, 2, c, "table must be a contiguous int32 device tensor [batch, width]");
+    const int64_t batch = table.size(0), width = table.size(1);
+    const at::Tensor& lens = numbers(a[8], at::kInt, 1, c, "kv_lens must be a contiguous int32 device tensor [batch]");
+    if (lens.size(0) != batch) raise(PyExc_ValueError, "kv_lens must be a contiguous int32 device tensor [batch]");
+    const char* shape = "weights must be a float32 device tensor [batch, kv_heads, positions] with contiguous rows";
+    const Weights w(tensor(a[9]), shape);
+    if (tensor(a[9]).device() != c.device || w.layered || w.batch != batch || w.heads != c.c.kv_heads) raise(PyExc_ValueError, shape);
+    const int32_t* start = nullptr;
+    if (a[10] != Py_None) {
+        const at::Tensor& t = numbers(a[10], at::kInt, 1, c, "q_start must be a contiguous int32 device tensor [batch + 1]");
+        if (t.size(0) != batch + 1) raise(PyExc_ValueError, "q_start must be a contiguous int32 device tensor [batch + 1]");
+        start = static_cast<const int32_t*>(t.const_data_ptr());
+    } else if (q.tokens != batch) {
+        raise(PyExc_ValueError, "without q_start there must be one token a sequence");
+    }
+    const float scale = a[11] == Py_None ? (float)(1.0 / std::sqrt((double)c.c.head_dim)) : real(a[11]);
+    const int causal = truth(a[12]);
+    const long window = integer(a[13]);
+    const float decay = real(a[14]);
+    const int64_t most = width * c.c.page_size;
+    const int64_t max_len = a[15] == Py_None ? most : integer(a[15]);
+    if (window < 0 || window > INT32_MAX || width > INT32_MAX || batch > INT32_MAX || q.heads > INT32_MAX || max_len < 0) check(RQ_ERR_ARG, where);
+    const int64_t len = max_len < most ? max_len : most;
+    if (w.n < len) raise(PyExc_ValueError, "weights must have a place for each position: as many as the table's pages have, or max_len");
+    void* s = stream(a[17]);
+    const AllocateOn on(a[17]);
+    const size_t need = rq_kv4_attention_weights_workspace(&c.c, q.tokens, (int)q.heads, (int)batch, start == nullptr, (int)window, len);
+    std::optional<Scratch> ws;
+    if (need) ws.emplace(a[16], need, c.device);
+    check(unlocked([&] {
+        return rq_kv4_attention_weights(h, &c.c, q.data, q.dtype, q.tokens, (int)q.heads, q.token, q.head, static_cast<const float*>(lse.const_data_ptr()),
+                                        static_cast<const int32_t*>(table.const_data_ptr()), (int)batch, (int)width, static_cast<const int32_t*>(lens.const_data_ptr()), start,
+                                        scale, causal, (int)window, len, decay, w.data, w.seq, w.head,
+                                        ws ? ws->data : nullptr, ws ? ws->bytes : 0, s);
+    }), where);
+    Py_RETURN_NONE;
+}
+
+// (weights, kv_lens, keep, sinks, recent, index, stream)
+PyObject* kv4_select(PyObject* const* a) {
+    const char* where = "rq_kv4_select";
+    const at::Tensor& t = tensor(a[0]);
+    const Weights w(t, "weights must be a float32 device tensor [(layers,) batch, kv_heads, positions] with contiguous rows");
+    on_current(t.device());
+    const at::Tensor& lens = tensor(a[1]);
+    if (!lens.is_cuda() || lens.device() != t.device() || lens.scalar_type() != at::kInt || lens.dim() != 1 || !lens.is_contiguous() || lens.size(0) != w.batch)
+        raise(PyExc_ValueError, "kv_lens must be a contiguous int32 device tensor [batch]");
+    const long keep = integer(a[2]), sinks = integer(a[3]), recent = integer(a[4]);
+    if (keep < 0 || keep > (1 << 30) || sinks < 0 || recent < 0 || sinks > keep || recent > keep) check(RQ_ERR_ARG, where);
+    std::vector<int64_t> size(t.sizes().begin(), t.sizes().end());
+    size.back() = keep;
+    if (a[5] != Py_None) {
+        const at::Tensor& i = tensor(a[5]);
+        if (!i.is_cuda() || i.device() != t.device() || i.scalar_type() != at::kInt || !i.is_contiguous() || i.sizes() != at::IntArrayRef(size))
+            raise(PyExc_ValueError, "index must be a contiguous int32 device tensor of weights' shape with `keep` places a row");
+    }
+    void* s = stream(a[6]);
+    const AllocateOn on(a[6]);
+    Out index;
+    index.make(a[5], size, at::kInt, t.device());
+    check(unlocked([&] {
+        return rq_kv4_select(w.data, (int)w.layers, (int)w.batch, (int)w.heads, w.n, w.layer, w.seq, w.head, static_cast<const int32_t*>(lens.const_data_ptr()), keep, sinks,
+                             recent, static_cast<int32_t*>(index.data), s);
+    }), where);
+    return index.take();
+}
+
+// (data, kv_heads, head_dim, page_size, index, table, new_table, weights, stream)
+PyObject* kv4_evict(PyObject* const* a) {
+    const char* where = "rq_kv4_evict";
+    const Cache c(a, where);
+    on_current(c.device);
+    const at::Tensor& index = tensor(a[4]);
+    const int64_t nd = index.dim();
+    const char* shape = "index must be a contiguous int32 device tensor [(layers,) batch, kv_heads, keep], with the cache's layers";
+    if (!index.is_cuda() || index.device() != c.device || index.scalar_type() != at::kInt || !index.is_contiguous() || nd < 3 || nd > 4) raise(PyExc_ValueError, shape);
+    if ((nd == 4 ? index.size(0) : 1) != c.layers || index.size(nd - 2) != c.c.kv_heads) raise(PyExc_ValueError, shape);
+    const int64_t batch = index.size(nd - 3), keep = index.size(nd - 1);
+    const at::Tensor& table = numbers(a[5], at::kInt, 2, c, "table must be a contiguous int32 device tensor [batch, width]");
+    if (table.size(0) != batch) raise(PyExc_ValueError, "table must be a contiguous int32 device tensor [batch, width]");
+    const int32_t* fresh = nullptr;
+    int64_t new_width = 0;
+    if (a[6] != Py_None) {
+        const at::Tensor& t = numbers(a[6], at::kInt, 2, c, "new_table must be a contiguous int32 device tensor [batch, width]");
+        if (t.size(0) != batch) raise(PyExc_ValueError, "new_table must be a contiguous int32 device tensor [batch, width]");
+        new_width = t.size(1);
+        if (new_width * c.c.page_size < keep) check(RQ_ERR_ARG, where);     // (no pages are no table)
+        fresh = static_cast<const int32_t*>(t.const_data_ptr());
+    }
+    std::optional<Weights> w;
+    if (a[7] != Py_None) {
+        const char* text = "weights must be a float32 device tensor of index' layers, batch and kv_heads with contiguous rows of `keep` places at least";
+        w.emplace(tensor(a[7]), text);
+        if (tensor(a[7]).device() != c.device || w->layers != c.layers || w->batch != batch || w->heads != c.c.kv_heads || w->n < keep) raise(PyExc_ValueError, text);
+    }
+    if (c.layers > (1 << 16) || batch > (1 << 20) || keep > (1 << 30) || table.size(1) > INT32_MAX || new_width > INT32_MAX) check(RQ_ERR_ARG, where);
+    void* s = stream(a[8]);
+    if (batch == 0 || c.layers == 0) Py_RETURN_NONE;
+    check(unlocked([&] {
+        return rq_kv4_evict(&c.c, (int)c.layers, c.layer_stride, static_cast<const int32_t*>(index.const_data_ptr()), keep, static_cast<const int32_t*>(table.const_data_ptr()),
+                            (int)batch, (int)table.size(1), fresh, (int)new_width, w && w->n ? w->data : nullptr, w ? w->n : 0, w ? w->layer : 0, w ? w->seq : 0,
+                            w ? w->head : 0, s);
+    }), where);
+    Py_RETURN_NONE;
+}
+
 // Called once by the binding: the class of the errors raised for the library's error codes.
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
@@ -712,7 +856,8 @@ PyMethodDef methods[] = {
     RQ_ENTRY(quantize_asym, 7),     RQ_ENTRY(rotate, 7),               RQ_ENTRY(dequantize_rotate, 10),
     RQ_ENTRY(dequantize, 7),        RQ_ENTRY(quant_error, 8),          RQ_ENTRY(quant_error_noalloc, 6),
     RQ_ENTRY(gbs_search, 8),        RQ_ENTRY(kv4_append, 10),          RQ_ENTRY(kv4_read, 10),
-    RQ_ENTRY(kv4_copy_pages, 7),    RQ_ENTRY(kv4_attention, 17),       {"set_error", set_error, METH_O, nullptr},
+    RQ_ENTRY(kv4_copy_pages, 7),    RQ_ENTRY(kv4_attention, 17),
+    RQ_ENTRY(kv4_attention_weights, 18), RQ_ENTRY(kv4_select, 7),      RQ_ENTRY(kv4_evict, 9),         {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 #undef RQ_ENTRY
 
