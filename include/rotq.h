@@ -514,6 +514,47 @@ int rq_kv4_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int 
                           int64_t max_len, int compute_units, rq_kv4_plan_t* plan);
 
 /*
+ * Bytes of device workspace rq_kv4_prefix_attention needs for such a call on the current device; 0 where it needs none and on bad
+ * arguments.  decode: q_start will be NULL.
+ */
+size_t rq_kv4_prefix_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int heads, int groups, int batch, int decode, int window,
+                                         int64_t max_prefix, int64_t max_len);
+
+/*
+ * rq_kv4_attention for sequences that begin alike (branches of a prompt, requests behind a system prompt): the pages that a group of them
+ * shares are read for all of its queries together.  Sequences group_start[g] .. group_start[g + 1] - 1 have the first prefix_lens[g]
+ * positions in common, position j in slot prefix_table[g][j / page_size] * page_size + j % page_size; position prefix_lens[g] + j of
+ * sequence b is in slot table[b][j / page_size] * page_size + j % page_size, and there are kv_lens[b] of these.  The queries of a sequence
+ * stand at the last of all its positions, and see what rq_kv4_attention's do.  Any group may have one sequence or none, any prefix and any
+ * sequence no positions; a prefix need not end with its page.
+ *   prefix_table [in]  DEVICE, groups x prefix_width int32 page numbers;  prefix_lens: DEVICE, groups int32, taken to be in 0 .. max_prefix
+ *   group_start  [in]  DEVICE, groups + 1 int32, ascending from 0 to batch
+ *   table, kv_lens, max_len   of what is behind the prefixes; max_prefix: no prefix is longer, at most prefix_width * page_size;
+ *                max_prefix + max_len at most 2^30
+ * Other arguments, what is rounded, and errors as rq_kv4_attention; the same call gives the same bits.
+ */
+int rq_kv4_prefix_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* Q, int dtype, int64_t tokens, int heads,
+                            int64_t q_token_stride, int64_t q_head_stride, const int32_t* prefix_table, int groups, int prefix_width,
+                            const int32_t* prefix_lens, const int32_t* group_start, const int32_t* table, int batch, int width, const int32_t* kv_lens,
+                            const int32_t* q_start, float scale, int causal, int window, int64_t max_prefix, int64_t max_len, void* O,
+                            int64_t o_token_stride, int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * How rq_kv4_prefix_attention lays out such a call (testing / measurement), as rq_kv4_attention_plan does.
+ */
+typedef struct rq_kv4_prefix_plan {
+    int separate;      /* 1: each sequence takes its prefix and its own positions in one launch (then only own_rows, waves count) */
+    int waves;         /* of a workgroup: separate; else 4 for few rows, 4 times the groups of waves for many */
+    int many, own_many;                /* kernel for many rows: for the prefixes, for what is behind them */
+    int shared_rows, own_rows;         /* queries x heads of a row tile */
+    int shared_chunk, shared_chunks;   /* a row tile's keys of the prefix: shared_chunks times shared_chunk at most */
+    int own_chunk, own_chunks;         /* behind it */
+} rq_kv4_prefix_plan_t;
+
+int rq_kv4_prefix_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int heads, int groups, int batch, int decode, int window,
+                                 int64_t max_prefix, int64_t max_len, int compute_units, rq_kv4_prefix_plan_t* plan);
+
+/*
  * How much attention the positions of cached sequences receive, for deciding which of them to keep:
  *     weights[b][y][j] <- decay * weights[b][y][j] + sum over the queries of sequence b and the heads x of kv head y of
  *                         exp(scale * q . k_j - lse)

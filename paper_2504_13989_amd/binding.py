@@ -36,6 +36,12 @@ class RqKv4Plan(C.Structure):
     _fields_ = [(name, C.c_int) for name in ("many", "rows", "waves", "groups", "tiles", "workers", "chunk", "chunks")]
 
 
+class RqKv4PrefixPlan(C.Structure):
+    """rq_kv4_prefix_plan_t of include/rotq.h."""
+    _fields_ = [(name, C.c_int) for name in ("separate", "waves", "many", "own_many", "shared_rows", "own_rows", "shared_chunk", "shared_chunks",
+                                             "own_chunk", "own_chunks")]
+
+
 class RotqError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -94,6 +100,11 @@ def lib() -> C.CDLL:
     L.rq_kv4_attention.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, i32, i32, vp, vp, C.c_float, i32, i32, i64, vp,
                                    i64, i64, vp, vp, C.c_size_t, vp]
     L.rq_kv4_attention_plan.argtypes = [kv4p, i32, i64, i32, i32, i32, i32, i32, i64, i32, C.POINTER(RqKv4Plan)]
+    L.rq_kv4_prefix_attention_workspace.argtypes = [kv4p, i64, i32, i32, i32, i32, i32, i64, i64]
+    L.rq_kv4_prefix_attention_workspace.restype = C.c_size_t
+    L.rq_kv4_prefix_attention.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, C.c_float, i32, i32,
+                                          i64, i64, vp, i64, i64, vp, vp, C.c_size_t, vp]
+    L.rq_kv4_prefix_attention_plan.argtypes = [kv4p, i32, i64, i32, i32, i32, i32, i32, i64, i64, i32, C.POINTER(RqKv4PrefixPlan)]
     L.rq_kv4_attention_weights_workspace.argtypes = [kv4p, i64, i32, i32, i32, i32, i64]
     L.rq_kv4_attention_weights_workspace.restype = C.c_size_t
     L.rq_kv4_attention_weights.argtypes = [vp, kv4p, vp, i32, i64, i32, i64, i64, vp, vp, i32, i32, vp, vp, C.c_float, i32, i32, i64, C.c_float,
@@ -383,6 +394,17 @@ def kv4_attention(h: Optional[Hadamard], cache: KV4Cache, q, table, kv_lens, q_s
     [tokens, heads]) receives the logarithms of the softmax sums.  `out` must not overlap q, nor its rows each other."""
     return (_nat or _native()).kv4_attention(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q,
                                              table, kv_lens, q_start, scale, causal, window, max_len, out, lse, workspace, stream)
+
+
+def kv4_prefix_attention(h: Optional[Hadamard], cache: KV4Cache, q, prefix_table, prefix_lens, group_start, table, kv_lens, q_start=None,
+                         scale: Optional[float] = None, causal: bool = True, window: int = 0, max_prefix: Optional[int] = None,
+                         max_len: Optional[int] = None, out=None, lse=None, workspace=None, stream=None):
+    """rq_kv4_prefix_attention: kv4_attention for sequences that begin alike.  Sequences group_start[g] .. group_start[g + 1] - 1 (int32
+    [groups + 1]) have prefix_lens[g] positions (int32 [groups]) in the pages prefix_table[g] (int32 [groups, prefix width]) in common; table
+    and kv_lens are those of what is behind them, a sequence's own."""
+    return (_nat or _native()).kv4_prefix_attention(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q, prefix_table,
+                                                    prefix_lens, group_start, table, kv_lens, q_start, scale, causal, window, max_prefix, max_len,
+                                                    out, lse, workspace, stream)
 
 
 def kv4_attention_weights(h: Optional[Hadamard], cache: KV4Cache, q, lse, table, kv_lens, weights, q_start=None, scale: Optional[float] = None,

@@ -197,6 +197,11 @@ void launch_few(const KvJob& job, const Plan& p, hipStream_t s) {
 }
 
 template <int D, bool F16>
+void launch_join(const KvJob& job, hipStream_t s) {
+    launch_kernel(k_kv4_join<D, F16>, group_grid(((int64_t)job.a.tokens * job.a.heads + kWaves - 1) / kWaves, 64 * kWaves), dim3(64 * kWaves), 0, s, job);
+}
+
+template <int D, bool F16>
 int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
     switch (p.copies) {
         case 4: launch_few<D, 4, F16>(job, p, s); break;
@@ -204,13 +209,18 @@ int launch_attention(const KvJob& job, const Plan& p, hipStream_t s) {
         case 1: launch_few<D, 1, F16>(job, p, s); break;
         default:
             launch_prompt(job, p.waves, p.groups, s);
-            if (p.chunks > 1)
-                launch_kernel(k_kv4_join<D, F16>, group_grid(((int64_t)job.a.tokens * job.a.heads + kWaves - 1) / kWaves, 64 * kWaves), dim3(64 * kWaves), 0, s, job);
+            if (p.chunks > 1) launch_join<D, F16>(job, s);
     }
     return launch_rc();
 }
 
 }  // namespace
+
+void launch_join(const KvJob& job, hipStream_t s) {
+    const bool f16 = job.a.dtype == RQ_F16;
+    if (job.cache.head_dim == 128) f16 ? launch_join<128, true>(job, s) : launch_join<128, false>(job, s);
+    else f16 ? launch_join<64, true>(job, s) : launch_join<64, false>(job, s);
+}
 
 size_t kv4_attention_workspace(const Kv4& c, const Kv4Attention& a, int num_cu) {
     Kv4Attention x = a;                           // (the caller's size holds for results of either type, causal or not)

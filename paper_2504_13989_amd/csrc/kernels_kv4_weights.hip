@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
     if (k0 >= end) return;
     const CodeBits bits;
     const int32_t* table = a.table + (int64_t)seq * a.width;
-    int pages = load_pages<PAGED>(job, table, k0, stride, lane), number_of = 0;
+    int pages = load_pages<PAGED>(job.cache, table, a.width, k0, stride, lane), number_of = 0;
     KeyCodes<D> t;
     load_keys<D, PAGED>(t, job.cache, pages, 0, head_at, k0, lane);
     Query<D, 16> q;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
         KeyCodes<D> next;
         if (k0 + stride < end) {
             if (++number_of == kPagesOf<PAGED>) {
-                pages = load_pages<PAGED>(job, table, k0 + stride, stride, lane);
+                pages = load_pages<PAGED>(job.cache, table, a.width, k0 + stride, stride, lane);
                 number_of = 0;
             }
             load_keys<D, PAGED>(next, job.cache, pages, number_of, head_at, k0 + stride, lane);

@@ -262,4 +262,75 @@ int rq_kv4_evict(const rq_kv4_t* cache, int layers, int64_t layer_stride, const 
                                          batch, (int)keep, width, new_width, (int)n}, static_cast<hipStream_t>(stream));
 }
 
+size_t rq_kv4_prefix_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int heads, int groups, int batch, int decode, int window,
+                                         int64_t max_prefix, int64_t max_len) {
+    rq::Kv4 c;
+    if (cache_of(cache, &c) != RQ_OK || shape_ok(c, tokens, heads, batch, window, max_len) != RQ_OK || tokens == 0 || batch == 0) return 0;
+    if (groups < 1 || groups > (1 << 20) || max_prefix < 0 || max_prefix + max_len > (1 << 30)) return 0;
+    const int cu = num_cu();
+    if (cu <= 0) return 0;
+    rq::Kv4Attention a{};
+    a.tokens = (int)tokens;
+    a.heads = heads;
+    a.batch = batch;
+    a.window = window_of(window, max_prefix + max_len);
+    a.max_len = max_len;
+    a.q_start = decode ? nullptr : &kRagged;
+    return rq::kv4_prefix_workspace(c, a, rq::Kv4Prefix{nullptr, nullptr, nullptr, groups, 0, max_prefix}, cu);
+}
+
+int rq_kv4_prefix_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int heads, int groups, int batch, int decode, int window,
+                                 int64_t max_prefix, int64_t max_len, int compute_units, rq_kv4_prefix_plan_t* plan) {
+    rq::Kv4 c;
+    int rc = cache_of(cache, &c);
+    if (rc != RQ_OK) return rc;
+    if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
+    if (!plan || (dtype != RQ_BF16 && dtype != RQ_F16) || compute_units < 0) return RQ_ERR_ARG;
+    if (groups < 1 || groups > (1 << 20) || max_prefix < 0 || max_prefix + max_len > (1 << 30)) return RQ_ERR_ARG;
+    if (tokens == 0 || batch == 0 || (decode && tokens != batch)) return RQ_ERR_ARG;
+    const int cu = compute_units ? compute_units : num_cu();
+    if (cu <= 0) return RQ_ERR_HIP;
+    rq::Kv4Attention a{};
+    a.dtype = dtype;
+    a.tokens = (int)tokens;
+    a.heads = heads;
+    a.batch = batch;
+    a.window = window_of(window, max_prefix + max_len);
+    a.max_len = max_len;
+    a.q_start = decode ? nullptr : &kRagged;
+    *plan = rq::kv4_prefix_plan(c, a, rq::Kv4Prefix{nullptr, nullptr, nullptr, groups, 0, max_prefix}, cu);
+    return RQ_OK;
+}
+
+int rq_kv4_prefix_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* Q, int dtype, int64_t tokens, int heads,
+                            int64_t q_token_stride, int64_t q_head_stride, const int32_t* prefix_table, int groups, int prefix_width,
+                            const int32_t* prefix_lens, const int32_t* group_start, const int32_t* table, int batch, int width, const int32_t* kv_lens,
+                            const int32_t* q_start, float scale, int causal, int window, int64_t max_prefix, int64_t max_len, void* O,
+                            int64_t o_token_stride, int64_t o_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    rq::Kv4 c;
+    int rc = cache_of(cache, &c);
+    if (rc != RQ_OK) return rc;
+    if (!rotation_ok(h, c.head_dim) || (dtype != RQ_BF16 && dtype != RQ_F16)) return RQ_ERR_ARG;
+    if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
+    if (width < 0 || prefix_width < 0 || (causal != 0 && causal != 1) || !(scale > 0.0f) || !std::isfinite(scale)) return RQ_ERR_ARG;
+    if (groups < 0 || groups > (1 << 20) || max_prefix < 0 || max_prefix + max_len > (1 << 30)) return RQ_ERR_ARG;
+    if (q_token_stride < 0 || q_head_stride < 0 || o_token_stride < 0 || o_head_stride < 0) return RQ_ERR_ARG;
+    if ((tokens > 1 && o_token_stride < c.head_dim) || (heads > 1 && o_head_stride < c.head_dim)) return RQ_ERR_ARG;
+    if (!q_start && tokens != batch) return RQ_ERR_ARG;                    // a token a sequence
+    if (tokens == 0) return RQ_OK;
+    if (batch == 0 || groups == 0 || !Q || !O || !kv_lens || !prefix_lens || !group_start) return RQ_ERR_ARG;
+    if ((width > 0 && !table) || (prefix_width > 0 && !prefix_table) || (width + (int64_t)prefix_width > 0 && c.pages == 0)) return RQ_ERR_ARG;
+    if (!aligned(Q, 2) || !aligned(O, 2) || !aligned(table, 4) || !aligned(kv_lens, 4) || !aligned(q_start, 4) || !aligned(lse, 4)) return RQ_ERR_ARG;
+    if (!aligned(prefix_table, 4) || !aligned(prefix_lens, 4) || !aligned(group_start, 4)) return RQ_ERR_ARG;
+    if (max_len > (int64_t)width << c.page_shift || max_prefix > (int64_t)prefix_width << c.page_shift) return RQ_ERR_ARG;
+    const rq::Kv4Attention a{Q, O, lse, dtype, (int)tokens, heads, batch, width, q_token_stride, q_head_stride, o_token_stride, o_head_stride,
+                             table, kv_lens, q_start, scale, causal != 0, h != nullptr, window_of(window, max_prefix + max_len), max_len};
+    const rq::Kv4Prefix p{prefix_table, prefix_lens, group_start, groups, prefix_width, max_prefix};
+    const int cu = num_cu();
+    if (cu <= 0) return RQ_ERR_HIP;
+    const size_t need = rq::kv4_prefix_workspace(c, a, p, cu);
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return RQ_ERR_ARG;
+    return rq::kv4_prefix_attention(c, a, p, cu, static_cast<float*>(workspace), static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

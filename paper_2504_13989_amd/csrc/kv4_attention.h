@@ -16,6 +16,14 @@ struct KvJob {
     float* part;                                  // workspace
 };
 
+// Which positions a launch takes.  kWhole: a sequence's.  Where sequences share a prefix: kShared: the prefixes, the rows of all sequences of a
+// group against them, kOwn: those behind it, of a sequence at a time, both to partial results; kSeparate: one after the other.
+enum class Part { kWhole, kShared, kOwn, kSeparate };
+struct PrefixJob : KvJob {
+    Kv4Prefix p;
+    int part_first, part_chunks;                  // partial results [chunks][tokens][heads]: the launch's first, all there are
+};
+
 namespace {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -240,11 +248,11 @@ constexpr int kPagesOf = PAGED ? 16 : 64;         // tiles
 // The tiles that begin at k0, k0 + stride ...  Keys behind the sequence's last one are masked: whatever the table has for them is
 // a page or, as numbers that are none, stands for page 0.
 template <bool PAGED>
-__device__ __forceinline__ int load_pages(const KvJob& job, const int32_t* table, int k0, int stride, int lane) {
+__device__ __forceinline__ int load_pages(const Kv4& c, const int32_t* table, int width, int k0, int stride, int lane) {
     const int64_t k = PAGED ? k0 + (int64_t)(lane >> 2) * stride + 16 * (lane & 3) : k0 + (int64_t)lane * stride;
-    const int64_t at = k >> job.cache.page_shift;
-    const int page = table[at < job.a.width ? at : job.a.width - 1];
-    return (uint32_t)page < (uint32_t)job.cache.pages ? page : 0;
+    const int64_t at = k >> c.page_shift;
+    const int page = table[at < width ? at : width - 1];
+    return (uint32_t)page < (uint32_t)c.pages ? page : 0;
 }
 // The head's block of the page of quarter `quarter` of tile number n, and its first key's place in the page.  (`head_at`: of the kv
 // head's block in a page)
@@ -336,8 +344,61 @@ __device__ __forceinline__ void find_keys(const KvJob& job, Place& p, int len) {
     p.to = a.causal && p1 + 1 < p.len ? p1 + 1 : p.len;
 }
 
+// Tokens of the sequences of group g: the first, the one behind the last.
+__device__ __forceinline__ int group_begin(const PrefixJob& job, int g) {
+    int b = job.p.group_start[g];
+    b = b < 0 ? 0 : b > job.a.batch ? job.a.batch : b;
+    if (!job.a.q_start) return b;
+    const int q = job.a.q_start[b];
+    return q < 0 ? 0 : q > job.a.tokens ? job.a.tokens : q;
+}
+// find_rows for row tiles of groups (Place: b the group); len: of its prefix.
+template <int BM>
+__device__ __forceinline__ bool find_group_rows(const PrefixJob& job, int tile, Place& p) {
+    int lo = 0, hi = job.p.groups - 1;
+    while (lo < hi) {
+        const int at = (lo + hi + 1) >> 1;
+        if ((int)((int64_t)group_begin(job, at) * job.group / BM) + at <= tile) lo = at; else hi = at - 1;
+    }
+    const int q1 = group_begin(job, lo + 1);
+    p.b = lo;
+    p.q0 = group_begin(job, lo);
+    p.nq = q1 > p.q0 ? q1 - p.q0 : 0;
+    p.base = (tile - (int)((int64_t)p.q0 * job.group / BM) - lo) * BM;
+    return p.base >= 0 && p.base < p.nq * job.group;
+}
+__device__ __forceinline__ int prefix_len(const PrefixJob& job, int g) {
+    const int n = job.p.lens[g];
+    return n < 0 ? 0 : n > job.p.max_len ? (int)job.p.max_len : n;
+}
+__device__ __forceinline__ int own_len(const KvJob& job, int seq) {
+    const int n = job.a.kv_lens[seq];
+    return n < 0 ? 0 : n > job.a.max_len ? (int)job.a.max_len : n;
+}
+// The group of a sequence.
+__device__ __forceinline__ int group_of(const PrefixJob& job, int seq) {
+    int lo = 0, hi = job.p.groups - 1;
+    while (lo < hi) {
+        const int at = (lo + hi + 1) >> 1;
+        if (job.p.group_start[at] <= seq) lo = at; else hi = at - 1;
+    }
+    return lo;
+}
+// A token's position behind its group's prefix (below 0: in it).
+__device__ __forceinline__ int own_position(const KvJob& job, int token) {
+    if (!job.a.q_start) return own_len(job, token) - 1;
+    int lo = 0, hi = job.a.batch - 1;
+    while (lo < hi) {
+        const int at = (lo + hi + 1) >> 1;
+        if (job.a.q_start[at] <= token) lo = at; else hi = at - 1;
+    }
+    return own_len(job, lo) - job.a.q_start[lo + 1] + token;
+}
+
 }  // namespace
 
+// Joins partial results of a row: a wave a row (job.chunks of them).
+void launch_join(const KvJob& job, hipStream_t s);
 // kernels_kv4_prompt.hip: many rows, 32 a wave, a workgroup of one or two groups of 4 waves or one of 8
 void launch_prompt(const KvJob& job, int waves, int groups, hipStream_t s);
 

@@ -330,9 +330,11 @@ __device__ __forceinline__ int* part_workers(const KvJob& job) {
     return reinterpret_cast<int*>(part_sums<D, C>(job) + (int64_t)(job.workers + job.tiles) * job.cache.kv_heads * C);
 }
 
-// SHARED: workers share the keys out, else a workgroup takes a row tile.
-template <int D, int F, bool F16, bool PAGED, int W, bool SHARED>
-__global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
+// SHARED: workers share the keys out, else a workgroup takes a row tile, or (Part kShared, kOwn) a chunk of its keys.
+template <int D, int F, bool F16, bool PAGED, int W, bool SHARED, Part PART>
+__device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::kWhole, KvJob, PrefixJob>& job) {
+    static_assert(!SHARED || PART == Part::kWhole, "workers take whole sequences");
+    constexpr bool CHUNKED = PART == Part::kShared || PART == Part::kOwn;
     constexpr int C = 16 / F, E = D / 4;          // rows of the workgroup; elements of a row in a lane
     __shared__ __attribute__((aligned(16))) float lds_params[W][kParameters * kTile];
     __shared__ __attribute__((aligned(16))) float lds_o[W][16][D + 4];
@@ -346,6 +348,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
     const CodeBits bits;
     float* lds = lds_params[wave];
     int tile = number, share = 0, share_end = 1;  // SHARED: the workgroup's units
+    int chunk = 0;
+    if constexpr (CHUNKED) {
+        tile = number / job.chunks;
+        chunk = number - tile * job.chunks;
+    }
     if constexpr (SHARED) {
         const int each = share_out<C>(job, shares);
         share = number * each;
@@ -379,49 +386,97 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
             count = (share_end < end ? share_end : end) - keys - first;
             all = count == end - keys;
         }
-        if (!find_rows<C>(job, tile, at)) return; // (SHARED: such a tile has no units)
+        if constexpr (PART == Part::kShared) {
+            if (!find_group_rows<C>(job, tile, at)) return;
+        } else {
+            if (!find_rows<C>(job, tile, at)) return;                // (SHARED: such a tile has no units)
+        }
         const int rows = at.nq * job.group, n = at.base + (lane & 15) % C;
         const bool there = n < rows;
         const int token = there ? token_of(job, at, n) : 0;
         // everything that does not depend on the length is asked for before it is known
         int len;
         if constexpr (SHARED) len = shares.len[tile];
+        else if constexpr (PART == Part::kShared) len = prefix_len(job, at.b);
         else len = a.kv_lens[at.b];
         const RawQuery<D, 16> raw = load_query<D, 16>(job, there, at.q0 + token, head * job.group + (there ? n - token * job.group : 0), lane);
         const int32_t* table = a.table + (int64_t)at.b * a.width;
+        int width = a.width;
+        if constexpr (PART == Part::kShared) {
+            width = job.p.width;
+            table = job.p.table + (int64_t)at.b * width;
+        }
         const int shift = job.cache.page_shift;
         constexpr int stride = W * kTile;
         int pages = 0, number_of = 0;             // of the tile in hand: number among those of `pages`
-        if (a.window == 0 && a.width > 0) pages = load_pages<PAGED>(job, table, (first + wave) * kTile, stride, lane);
-        find_keys<C>(job, at, len);
+        if (PART != Part::kSeparate && a.window == 0 && width > 0)
+            pages = load_pages<PAGED>(job.cache, table, width, (CHUNKED ? chunk * job.chunk : first * kTile) + wave * kTile, stride, lane);
+        if constexpr (PART == Part::kShared) {
+            at.len = len;
+            at.from = 0;
+            at.to = len;
+        } else {
+            find_keys<C>(job, at, len);
+        }
         int from = at.from, to = at.to;
         if constexpr (SHARED) {
             from += first * kTile;
             if (to > from + count * kTile) to = from + count * kTile;
         }
+        if constexpr (CHUNKED) {
+            from += chunk * job.chunk;
+            if (to > from + job.chunk) to = from + job.chunk;
+        }
+        // kSeparate: positions count from the end of the prefix; those of the prefix itself come first
+        int behind = 0, own_from = 0, own_to = 0;
+        [[maybe_unused]] const int32_t* own_table = table;
+        if constexpr (PART == Part::kSeparate) {
+            const int g = group_of(job, at.b), last = (at.base + C < rows ? at.base + C : rows) - 1;
+            behind = prefix_len(job, g);
+            own_from = from;
+            own_to = to;
+            const int p0 = behind + at.len - at.nq + token_of(job, at, at.base), p1 = behind + at.len - at.nq + token_of(job, at, last);
+            from = a.window && p0 - a.window + 1 > 0 ? (p0 - a.window + 1) & ~(kTile - 1) : 0;
+            to = a.causal && p1 + 1 < behind ? p1 + 1 : behind;
+            width = job.p.width;
+            table = job.p.table + (int64_t)g * width;
+        }
         int k0 = from + wave * kTile;             // the tile in hand
         Codes<D> t;
-        if (k0 < to) {
-            if (a.window) pages = load_pages<PAGED>(job, table, k0, stride, lane);
-            const Source<PAGED> s = find_tile<PAGED>(job.cache, pages, 0, head_at, k0);
-            load_keys<D>(t, s, shift, lane);
-            load_values<D>(t, s, shift, lane);
-        }
+        const auto begin = [&] {
+            if (k0 < to) {
+                if (PART == Part::kSeparate || a.window) pages = load_pages<PAGED>(job.cache, table, width, k0, stride, lane);
+                number_of = 0;
+                const Source<PAGED> s = find_tile<PAGED>(job.cache, pages, 0, head_at, k0);
+                load_keys<D>(t, s, shift, lane);
+                load_values<D>(t, s, shift, lane);
+            }
+        };
+        begin();
         Columns<D> r;
         take_query<D, 16, F16, F16>(r.q, job, raw, lane);
         r.sum = r.q.even + r.q.odd;
         r.bias = -(1024.0f + 7.5f) * r.q.even - (64.0f + 7.5f) * r.q.odd;
         int all_lo, all_hi;                       // keys that all rows see
-        {
-            const int pos = at.len - at.nq + token;                  // the row's position in its sequence
-            const int hi = !there ? 0 : a.causal ? (pos + 1 < at.len ? pos + 1 : at.len) : at.len;
+        // of the first `len` positions, `behind` of them before position 0 of the sequence
+        const auto see = [&](int behind, int len) {
+            int pos = behind + at.len - at.nq + token;               // the row's position in its sequence
+            if constexpr (PART == Part::kShared) pos = there ? len + own_position(job, at.q0 + token) : 0;
+            const int hi = !there ? 0 : a.causal ? (pos + 1 < len ? pos + 1 : len) : len;
             r.lo = a.window ? (pos - a.window + 1 > 0 ? pos - a.window + 1 : 0) : 0;
             r.seen = hi > r.lo ? hi - r.lo : 0;
-            const int last = (at.base + C < rows ? at.base + C : rows) - 1;
-            const int p0 = at.len - at.nq + token_of(job, at, at.base), p1 = at.len - at.nq + token_of(job, at, last);
-            all_lo = a.window ? p1 - a.window + 1 : 0;
-            all_hi = a.causal && p0 + 1 < to ? p0 + 1 : to;
-        }
+            if constexpr (PART == Part::kShared) {                   // (rows of several sequences: none or all of the masks)
+                const bool some = __any(there && hi < len);
+                all_lo = 0;
+                all_hi = some ? 0 : to;
+            } else {
+                const int last = (at.base + C < rows ? at.base + C : rows) - 1;
+                const int p0 = behind + at.len - at.nq + token_of(job, at, at.base), p1 = behind + at.len - at.nq + token_of(job, at, last);
+                all_lo = a.window ? p1 - a.window + 1 : 0;
+                all_hi = a.causal && p0 + 1 < to ? p0 + 1 : to;
+            }
+        };
+        see(behind, PART == Part::kSeparate ? behind : at.len);
         r.m = -INFINITY;
         r.l = r.w = r.limit = 0.0f;
         r.factor = 1.0f;
@@ -433,7 +488,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
             Source<PAGED> s;
             if constexpr (more) {
                 if (++number_of == kPagesOf<PAGED>) {
-                    pages = load_pages<PAGED>(job, table, next, stride, lane);
+                    pages = load_pages<PAGED>(job.cache, table, width, next, stride, lane);
                     number_of = 0;
                 }
                 s = find_tile<PAGED>(job.cache, pages, number_of, head_at, next);
@@ -450,6 +505,16 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
         };
         while (k0 + stride < to) step(std::true_type{});
         if (k0 < to) step(std::false_type{});
+        if constexpr (PART == Part::kSeparate) {
+            table = own_table;
+            width = a.width;
+            to = own_to;
+            k0 = own_from + wave * kTile;
+            begin();
+            see(0, at.len);
+            while (k0 + stride < to) step(std::true_type{});
+            if (k0 < to) step(std::false_type{});
+        }
         // a column's results: normalised, with log2 of the sum of e^(scale q.k)
         {
             const float l = column_sum<16>(r.l), w = column_sum<16>(r.w);
@@ -487,7 +552,14 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
 #pragma unroll
             for (int e = 0; e < per; ++e) z[e] *= by;
             const float total = top + __builtin_amdgcn_logf(sum);
-            if (SHARED && !all) {
+            if constexpr (CHUNKED) {
+                const int token_m = token_of(job, at, at.base + mine), h = head * job.group + at.base + mine - token_m * job.group;
+                const int64_t rows_all = (int64_t)a.tokens * a.heads, part = (job.part_first + chunk) * rows_all + (int64_t)(at.q0 + token_m) * a.heads + h;
+                float* o = job.part + part * D + d;
+#pragma unroll
+                for (int e = 0; e < per; ++e) o[e] = z[e];
+                if (d == 0) job.part[job.part_chunks * rows_all * D + part] = total;
+            } else if (SHARED && !all) {
                 const int64_t slot = ((int64_t)(number + tile) * kv + head) * C + mine;
                 float* o = job.part + slot * D + d;
 #pragma unroll
@@ -502,6 +574,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
         if constexpr (!SHARED) return;
         __syncthreads();                          // (LDS is written again)
     }
+}
+
+template <int D, int F, bool F16, bool PAGED, int W, bool SHARED>
+__global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
+    few_rows<D, F, F16, PAGED, W, SHARED, Part::kWhole>(job);
 }
 
 }  // namespace

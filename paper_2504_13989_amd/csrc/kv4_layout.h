@@ -65,6 +65,16 @@ rq_kv4_plan_t kv4_attention_plan(const Kv4& c, const Kv4Attention& a, int num_cu
 int kv4_attention(const Kv4& c, const Kv4Attention& a, int num_cu, float* workspace, hipStream_t s);
 
 
+// What sequences share: `groups` groups of sequences that stand side by side.
+struct Kv4Prefix {
+    const int32_t *table, *lens, *group_start;    // [groups][width], [groups], [groups + 1] (sequences)
+    int groups, width;
+    int64_t max_len;
+};
+size_t kv4_prefix_workspace(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& p, int num_cu);
+rq_kv4_prefix_plan_t kv4_prefix_plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& p, int num_cu);
+int kv4_prefix_attention(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& p, int num_cu, float* workspace, hipStream_t s);
+
 // Attention that positions have received, added up (q, lse, table ... of `a`; its o is not looked at).
 struct Kv4Weights {
     Kv4Attention a;

@@ -20,6 +20,8 @@
 #pragma once
 #include "kv4_attention.h"
 
+#include <type_traits>
+
 namespace rq {
 namespace {
 
@@ -420,9 +422,10 @@ struct Handed {
 
 // GROUPS: 2 where a workgroup's rows are few: two groups of WAVES waves have the same rows and take turns at the tiles, each with tiles of
 // its own in LDS, and the second hands its sums to the first at the end.
-template <int D, int WAVES, int GROUPS, bool F16, bool PAGED>
-__global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job) {
+template <int D, int WAVES, int GROUPS, bool F16, bool PAGED, Part PART>
+__device__ __forceinline__ void many_rows(const std::conditional_t<PART == Part::kWhole, KvJob, PrefixJob>& job) {
     constexpr bool EXACT = F16;
+    constexpr bool PARTS = PART != Part::kWhole;  // partial results, of which other launches have some too
     constexpr int BM = 32 * WAVES, N = (kRuns<D> + 64 * WAVES - 1) / (64 * WAVES);
     // Eight waves are two groups, four SIMDs each, half a step apart: one has products of keys and unpacks while the other has
     // exponentials.  Three tiles then, since the one group still reads values of the last while the other unpacks the next.
@@ -439,15 +442,24 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
     const CodeBits bits;
     Place at;
     // the last rows of a causal prompt see most: they begin first
-    if (tile_no >= job.tiles || !find_rows<BM>(job, job.tiles - 1 - tile_no, at)) return;
-    find_keys<BM>(job, at, a.kv_lens[at.b]);
+    if (tile_no >= job.tiles) return;
+    if constexpr (PART == Part::kShared) {
+        if (!find_group_rows<BM>(job, job.tiles - 1 - tile_no, at)) return;
+        at.len = at.to = prefix_len(job, at.b);
+        at.from = 0;
+    } else {
+        if (!find_rows<BM>(job, job.tiles - 1 - tile_no, at)) return;
+        find_keys<BM>(job, at, a.kv_lens[at.b]);
+    }
     const int rows = at.nq * job.group, row = at.base + 32 * wave;
 
     // the chunk's share of the keys that the workgroup's rows see
     const int from = at.from + chunk * job.chunk, to = at.to > from + job.chunk ? from + job.chunk : at.to;
     // what the wave's rows see: some of them, all of them
     int any_lo = 0, any_hi = 0, all_lo = 0, all_hi = 0;
-    if (row < rows) {
+    if (PART == Part::kShared) {                  // (rows of several sequences: none or all of the masks, below)
+        any_hi = row < rows ? to : 0;
+    } else if (row < rows) {
         const int last = (row + 32 < rows ? row + 32 : rows) - 1;
         const int p0 = at.len - at.nq + token_of(job, at, row), p1 = at.len - at.nq + token_of(job, at, last);
         any_lo = a.window ? p0 - a.window + 1 : 0;
@@ -456,15 +468,27 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         all_hi = a.causal && p0 + 1 < to ? p0 + 1 : to;
     }
     const int32_t* table = a.table + (int64_t)at.b * a.width;
+    int width = a.width;
+    if constexpr (PART == Part::kShared) {
+        width = job.p.width;
+        table = job.p.table + (int64_t)at.b * width;
+    }
     const int mine = row + (lane & 31);
     const bool there = mine < rows;
     const int token = there ? token_of(job, at, mine) : 0, of = there ? mine - token * job.group : 0;
+    // (found out while registers are free)
+    int shared_seen = 0;
+    if constexpr (PART == Part::kShared) {
+        const int pos = there ? at.len + own_position(job, at.q0 + token) : -1;
+        shared_seen = !a.causal ? (there ? at.len : 0) : pos + 1 < at.len ? (pos + 1 > 0 ? pos + 1 : 0) : at.len;
+        all_hi = __any(there && shared_seen < at.len) ? 0 : to;
+    }
     const RawQuery<D, 32> raw_q = load_query<D, 32>(job, there, at.q0 + token, head * job.group + of, lane);
     const int head_at = head * ((D + 8) << job.cache.page_shift);
     int pages = 0, page_no = 0, asked = from + half * kTile;   // the tile asked for last, its number among those of `pages`
     Raw<N> raw, later;                            // the next tile, the one after it
     if (from < to) {
-        pages = load_pages<PAGED>(job, table, asked, kStride, lane);
+        pages = load_pages<PAGED>(job.cache, table, width, asked, kStride, lane);
         load_tile<D, WAVES, N, PAGED>(raw, job.cache, pages, 0, head_at, asked, thread);
         if (asked + kStride < to) {
             asked += kStride;
@@ -478,7 +502,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
     __builtin_amdgcn_s_waitcnt(0x0f70);
     const int pos = at.len - at.nq + token;
     const int hi = !there ? 0 : a.causal ? (pos + 1 < at.len ? pos + 1 : at.len) : at.len;
-    const int lo = a.window ? (pos - a.window + 1 > 0 ? pos - a.window + 1 : 0) : 0;
+    const int lo = PART != Part::kShared && a.window ? (pos - a.window + 1 > 0 ? pos - a.window + 1 : 0) : 0;
     Sums<D, EXACT> r;
     r.m = -INFINITY;
     r.l = r.w = 0.0f;
@@ -487,7 +511,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
 #pragma unroll
         for (int e = 0; e < 16; ++e) r.o[j][e] = 0.0f;
 
-    const int seen = hi > lo ? hi - lo : 0;
+    const int seen = PART == Part::kShared ? shared_seen : hi > lo ? hi - lo : 0;
 
     Range keys{0.0f, 0}, values{0.0f, 0};
     int at_tile = TILES - 1;                      // the tile in hand
@@ -524,7 +548,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
         if (asked + kStride < to) {
             asked += kStride;
             if (++page_no == kPagesOf<PAGED>) {
-                pages = load_pages<PAGED>(job, table, asked, kStride, lane);
+                pages = load_pages<PAGED>(job.cache, table, width, asked, kStride, lane);
                 page_no = 0;
             }
         }
@@ -578,29 +602,49 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job
 #pragma unroll
             for (int e = 0; e < 16; ++e) r.o[j][e] = fmaf(yo, h.o[16 * j + e][lane], xo * r.o[j][e]);
     }
-    if (!there) return;                           // (both lanes of the row)
+    int e_lane = lane;
+    bool e_there = there;
+    int e_token = token, e_of = of;
+    if constexpr (PARTS) {                        // (found again: registers are short)
+        asm volatile("" : "+v"(e_lane));
+        const int e_mine = at.base + 32 * wave + (e_lane & 31);
+        e_there = e_mine < at.nq * job.group;
+        e_token = e_there ? token_of(job, at, e_mine) : 0;
+        e_of = e_there ? e_mine - e_token * job.group : 0;
+    }
+    if (!e_there) return;                         // (both lanes of the row)
     const float l = column_sum<32>(r.l), w = EXACT ? column_sum<32>(r.w) : 0.0f;
     const float by = __builtin_amdgcn_ldexpf(l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l), -values.up);
     float lse = l == 0.0f ? -INFINITY : r.m + __builtin_amdgcn_logf(l);
     if constexpr (!EXACT) lse -= kUp;
-    const int t_row = at.q0 + token, h_row = head * job.group + of;
-    const int64_t part_row = ((int64_t)chunk * a.tokens + t_row) * a.heads + h_row;
+    const int t_row = at.q0 + e_token, h_row = head * job.group + e_of;
+    int part_first = 0, part_chunks = job.chunks;
+    if constexpr (PARTS) {
+        part_first = job.part_first;
+        part_chunks = job.part_chunks;
+    }
+    const int64_t part_row = ((int64_t)(part_first + chunk) * a.tokens + t_row) * a.heads + h_row;
     float* part = job.part + part_row * D;
     uint16_t* out = static_cast<uint16_t*>(a.o) + (int64_t)t_row * a.o_token + (int64_t)h_row * a.o_head;
     constexpr int B = D / 4 / 2;                  // fours of elements that the lane has
 #pragma unroll
     for (int i = 0; i < B; ++i) {
-        const int four = i % 4 + 8 * (i / 4) + 4 * (lane >> 5);
+        const int four = i % 4 + 8 * (i / 4) + 4 * (e_lane >> 5);
         float y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = ((D == 128 ? r.o[e][i] : r.o[e / 2][e % 2 * 8 + i]) + w) * by;
-        if (job.chunks > 1) *reinterpret_cast<f32x4*>(part + 4 * four) = f32x4{y[0], y[1], y[2], y[3]};
+        if (PARTS || job.chunks > 1) *reinterpret_cast<f32x4*>(part + 4 * four) = f32x4{y[0], y[1], y[2], y[3]};
         else store_row<4, F16>(out + 4 * four, y, job.wide_o);
     }
-    if (lane < 32) {
-        if (job.chunks > 1) job.part[(int64_t)job.chunks * a.tokens * a.heads * D + part_row] = lse;
+    if (e_lane < 32) {
+        if (PARTS || job.chunks > 1) job.part[(int64_t)part_chunks * a.tokens * a.heads * D + part_row] = lse;
         else if (a.lse) a.lse[(int64_t)t_row * a.heads + h_row] = lse * kLn2;
     }
+}
+
+template <int D, int WAVES, int GROUPS, bool F16, bool PAGED>
+__global__ __launch_bounds__(64 * WAVES * GROUPS, 2) void k_kv4_prompt(KvJob job) {
+    many_rows<D, WAVES, GROUPS, F16, PAGED, Part::kWhole>(job);
 }
 
 }  // namespace

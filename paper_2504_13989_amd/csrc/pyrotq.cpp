@@ -774,6 +774,72 @@ PyObject* kv4_attention_weights(PyObject* const* a) {
     Py_RETURN_NONE;
 }
 
+// (handle, data, kv_heads, head_dim, page_size, q, prefix_table, prefix_lens, group_start, table, kv_lens, q_start, scale, causal, window, max_prefix,
+//  max_len, out, lse, workspace, stream)
+PyObject* kv4_prefix_attention(PyObject* const* a) {
+    const char* where = "rq_kv4_prefix_attention";
+    const rq_hadamard_t* h = handle(a[0]);
+    const Cache c(a + 1, where);
+    c.one_layer();
+    on_current(c.device);
+    const at::Tensor& qt = tensor(a[5]);
+    const HeadRows q(qt, c, "q must be a device tensor [tokens, heads, head_dim] with contiguous rows");
+    const at::Tensor& prefix_table = numbers(a[6], at::kInt, 2, c, "prefix_table must be a contiguous int32 device tensor [groups, width]");
+    const int64_t groups = prefix_table.size(0), prefix_width = prefix_table.size(1);
+    const at::Tensor& prefix_lens = numbers(a[7], at::kInt, 1, c, "prefix_lens must be a contiguous int32 device tensor [groups]");
+    if (prefix_lens.size(0) != groups) raise(PyExc_ValueError, "prefix_lens must be a contiguous int32 device tensor [groups]");
+    const at::Tensor& group_start = numbers(a[8], at::kInt, 1, c, "group_start must be a contiguous int32 device tensor [groups + 1]");
+    if (group_start.size(0) != groups + 1) raise(PyExc_ValueError, "group_start must be a contiguous int32 device tensor [groups + 1]");
+    const at::Tensor& table = numbers(a[9], at::kInt, 2, c, "table must be a contiguous int32 device tensor [batch, width]");
+    const int64_t batch = table.size(0), width = table.size(1);
+    const at::Tensor& lens = numbers(a[10], at::kInt, 1, c, "kv_lens must be a contiguous int32 device tensor [batch]");
+    if (lens.size(0) != batch) raise(PyExc_ValueError, "kv_lens must be a contiguous int32 device tensor [batch]");
+    const int32_t* start = nullptr;
+    if (a[11] != Py_None) {
+        const at::Tensor& t = numbers(a[11], at::kInt, 1, c, "q_start must be a contiguous int32 device tensor [batch + 1]");
+        if (t.size(0) != batch + 1) raise(PyExc_ValueError, "q_start must be a contiguous int32 device tensor [batch + 1]");
+        start = static_cast<const int32_t*>(t.const_data_ptr());
+    } else if (q.tokens != batch) {
+        raise(PyExc_ValueError, "without q_start there must be one token a sequence");
+    }
+    const float scale = a[12] == Py_None ? (float)(1.0 / std::sqrt((double)c.c.head_dim)) : real(a[12]);
+    const int causal = truth(a[13]);
+    const long window = integer(a[14]);
+    const int64_t most_prefix = prefix_width * c.c.page_size, most = width * c.c.page_size;
+    const int64_t max_prefix = a[15] == Py_None ? most_prefix : integer(a[15]), max_len = a[16] == Py_None ? most : integer(a[16]);
+    if (window < 0 || window > INT32_MAX || width > INT32_MAX || prefix_width > INT32_MAX || batch > INT32_MAX || groups > INT32_MAX || q.heads > INT32_MAX ||
+        max_len < 0 || max_prefix < 0)
+        check(RQ_ERR_ARG, where);
+    if (a[17] != Py_None) {
+        const at::Tensor& t = tensor(a[17]);
+        if (t.scalar_type() != qt.scalar_type() || t.dim() != 3 || t.size(0) != q.tokens || t.size(1) != q.heads)
+            raise(PyExc_ValueError, "out must have q's shape and dtype");
+    }
+    float* lse = nullptr;
+    if (a[18] != Py_None) {
+        const at::Tensor& t = tensor(a[18]);
+        if (!t.is_cuda() || t.device() != c.device || t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() != q.tokens * q.heads)
+            raise(PyExc_ValueError, "lse must be a contiguous float32 device tensor [tokens, heads]");
+        lse = static_cast<float*>(t.data_ptr());
+    }
+    void* s = stream(a[20]);
+    const AllocateOn on(a[20]);
+    Out o;
+    o.make(a[17], {q.tokens, q.heads, c.c.head_dim}, qt.scalar_type(), c.device);
+    const HeadRows y(THPVariable_Unpack(o.ref), c, "out must be a device tensor [tokens, heads, head_dim] with contiguous rows");
+    const int64_t prefix = max_prefix < most_prefix ? max_prefix : most_prefix, len = max_len < most ? max_len : most;
+    const size_t need = rq_kv4_prefix_attention_workspace(&c.c, q.tokens, (int)q.heads, (int)groups, (int)batch, start == nullptr, (int)window, prefix, len);
+    std::optional<Scratch> ws;
+    if (need) ws.emplace(a[19], need, c.device);
+    const auto p = [](const at::Tensor& t) { return static_cast<const int32_t*>(t.const_data_ptr()); };
+    check(unlocked([&] {
+        return rq_kv4_prefix_attention(h, &c.c, q.data, q.dtype, q.tokens, (int)q.heads, q.token, q.head, p(prefix_table), (int)groups, (int)prefix_width, p(prefix_lens),
+                                       p(group_start), p(table), (int)batch, (int)width, p(lens), start, scale, causal, (int)window, prefix, len, y.data, y.token, y.head,
+                                       lse, ws ? ws->data : nullptr, ws ? ws->bytes : 0, s);
+    }), where);
+    return o.take();
+}
+
 // (weights, kv_lens, keep, sinks, recent, index, stream)
 PyObject* kv4_select(PyObject* const* a) {
     const char* where = "rq_kv4_select";
@@ -857,7 +923,8 @@ PyMethodDef methods[] = {
     RQ_ENTRY(dequantize, 7),        RQ_ENTRY(quant_error, 8),          RQ_ENTRY(quant_error_noalloc, 6),
     RQ_ENTRY(gbs_search, 8),        RQ_ENTRY(kv4_append, 10),          RQ_ENTRY(kv4_read, 10),
     RQ_ENTRY(kv4_copy_pages, 7),    RQ_ENTRY(kv4_attention, 17),
-    RQ_ENTRY(kv4_attention_weights, 18), RQ_ENTRY(kv4_select, 7),      RQ_ENTRY(kv4_evict, 9),         {"set_error", set_error, METH_O, nullptr},
+    RQ_ENTRY(kv4_prefix_attention, 21), RQ_ENTRY(kv4_attention_weights, 18), RQ_ENTRY(kv4_select, 7),
+    RQ_ENTRY(kv4_evict, 9),         {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 #undef RQ_ENTRY
 

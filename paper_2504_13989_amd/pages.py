@@ -79,6 +79,19 @@ class PagePool:
             self._held[page] += 1
         self._tables[new], self._lens[new] = list(self._tables[seq]), self._lens[seq]
 
+    def common_pages(self, seqs) -> int:
+        """How many pages the sequences begin with in common, filled in all of them: kv4_prefix_attention reads these once.  Their numbers are
+        the first ones of any of the tables; what is behind them is each sequence's own."""
+        seqs = list(seqs)
+        if not seqs:
+            return 0
+        n = min(self._lens[seq] for seq in seqs) // self.page_size
+        first = self._tables[seqs[0]]
+        for seq in seqs[1:]:
+            table = self._tables[seq]
+            n = next((i for i in range(n) if table[i] != first[i]), n)
+        return n
+
     def truncate(self, seq, length: int) -> None:
         """The sequence's first `length` tokens; pages behind them are freed."""
         if not 0 <= length <= self._lens[seq]:

@@ -1,0 +1,303 @@
+"""GPU: attention over the 4-bit cache for sequences that share a prefix, against attention of each sequence by itself (tests/kv4_reference.py,
+NumPy, 64 bits)."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import kv4_reference as ref
+
+torch = pytest.importorskip("torch")
+import paper_2504_13989_amd as rq  # noqa: E402
+from paper_2504_13989_amd import binding  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+U_OUT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32).cuda()
+
+
+class Batch:
+    """Groups of sequences: prefix lengths, sequences of each group, own lengths and queries of each sequence."""
+
+    def __init__(self, seed, prefix, sizes, lens, counts, heads, kv, d, page, dtype="bf16", rotate=True, width=None):
+        rng = np.random.default_rng(seed)
+        assert sum(sizes) == len(lens) == len(counts) and len(prefix) == len(sizes)
+        self.prefix, self.sizes, self.lens, self.counts, self.heads, self.kv, self.d, self.page, self.dtype = prefix, sizes, lens, counts, heads, kv, d, page, dtype
+        pages = sum(-(-n // page) for n in [*prefix, *lens]) + 2
+        self.cache, self.h = rq.kv4_cache(pages, kv, d, page), rq.hadamard_build(d) if rotate else None
+        order, at = rng.permutation(pages), 0
+        tables, self.slots = [], []
+        for lengths in (prefix, lens):
+            need = [-(-n // page) for n in lengths]
+            table, slots = np.full((len(need), max(need + [1])), -1), []
+            for i, (n, m) in enumerate(zip(lengths, need)):
+                table[i, :m] = order[at:at + m]
+                at += m
+                j = np.arange(n)
+                slots.append((table[i, j // page] * page + j % page).astype(np.int64))
+            tables.append(table), self.slots.append(slots)
+        total = np.concatenate([s for part in self.slots for s in part])
+        k, v = (torch.tensor(rng.standard_normal((len(total), kv, d)) * rng.uniform(0.5, 2, (len(total), kv, 1)) + 0.2, dtype=torch.float32).cuda() for _ in "kv")
+        rq.kv4_append(self.h, self.cache, k, v, torch.tensor(total).cuda())
+        self.prefix_table, self.table = (ints(t.tolist()) for t in tables)
+        self.prefix_lens, self.kv_lens = ints(list(prefix)), ints(list(lens))
+        self.group_start = ints([sum(sizes[:i]) for i in range(len(sizes) + 1)])
+        self.start = ints([sum(counts[:i]) for i in range(len(counts) + 1)])
+        self.q = torch.tensor(rng.standard_normal((sum(counts), heads, d)) * 1.5, dtype=torch.float32).to(DT[dtype]).cuda()
+
+    def attend(self, ragged=None, **kw):
+        ragged = set(self.counts) != {1} if ragged is None else ragged
+        return rq.kv4_prefix_attention(self.h, self.cache, kw.pop("q", self.q), self.prefix_table, kw.pop("prefix_lens", self.prefix_lens),
+                                       kw.pop("group_start", self.group_start), self.table, kw.pop("kv_lens", self.kv_lens), self.start if ragged else None, **kw)
+
+    def plan(self, ragged=None, window=0):
+        ragged = set(self.counts) != {1} if ragged is None else ragged
+        c, p = binding.RqKv4(1 << 20, self.cache.pages, self.kv, self.d, self.page), binding.RqKv4PrefixPlan()
+        assert binding.lib().rq_kv4_prefix_attention_plan(C.byref(c), 0 if self.dtype == "bf16" else 2, len(self.q), self.heads, len(self.prefix), len(self.lens),
+                                                          int(not ragged), window, self.prefix_table.shape[1] * self.page, self.table.shape[1] * self.page, 0, C.byref(p)) == 0
+        return p
+
+    def check(self, o, lse=None, causal=True, window=0, scale=None):
+        c = ref.Pages(0, self.kv, self.d, self.page)
+        c.data = self.cache.data.cpu().numpy()
+        u, scale = U_OUT[self.dtype], scale or 1 / math.sqrt(self.d)
+        x = self.q.double().cpu().numpy()
+        x = x @ ref.sylvester(self.d) if self.h else x
+        got, at, b = o.double().cpu().numpy(), 0, 0
+        for g, size in enumerate(self.sizes):
+            first = [*c.rows(self.slots[0][g]), c.steps(self.slots[0][g])]
+            for b in range(b, b + size):
+                own = [*c.rows(self.slots[1][b]), c.steps(self.slots[1][b])]
+                k, v, steps = (np.concatenate(t) for t in zip(first, own))
+                n = self.counts[b]
+                heads, kv = list(range(self.heads)), list(range(self.kv))
+                if n > 500:                        # (long ones: two heads of their own kv heads)
+                    heads, kv = [0, self.heads - 1], [0, self.kv - 1]
+                w, wl, bound = ref.attention(x[at:at + n][:, heads], k[:, kv], v[:, kv], steps[:, kv], scale, causal, window)
+                y = got[at:at + n][:, heads]
+                assert np.isfinite(y).all()
+                # (as for attention without a prefix: the join's roundings are those of the sums, 2^-16 in the bound)
+                assert (abs(y - w) <= bound * (1 + u) + u * abs(w)).all(), (g, b)
+                assert np.linalg.norm(y - w) <= 0.25 * np.linalg.norm(bound) + u * np.linalg.norm(w), (g, b)
+                if lse is not None:
+                    z = lse[at:at + n][:, heads].double().cpu().numpy()
+                    none = np.isinf(wl)
+                    assert np.array_equal(np.isinf(z), none) and (z[none] < 0).all()
+                    assert (abs(z[~none] - wl[~none]) <= 0.05 + 1e-3 * abs(wl[~none])).all()
+                at += n
+            b += size > 0
+
+
+#        prefix, sizes, lens, counts, heads, kv, d, page, dtype, rotate, causal, window
+CASES = [
+    ([70], [3], [5, 1, 17], [1, 1, 1], 4, 2, 128, 16, "bf16", True, True, 0),
+    ([64], [2], [64, 65], [1, 1], 8, 1, 64, 64, "f16", False, True, 0),
+    ([0], [2], [30, 1], [1, 1], 2, 2, 64, 16, "bf16", True, True, 0),                       # no prefix
+    ([100], [3], [0, 0, 3], [1, 1, 1], 4, 4, 128, 32, "f16", True, True, 0),                # no positions of their own
+    ([33, 0, 129], [2, 1, 2], [4, 50, 1, 7, 0], [1] * 5, 5, 1, 128, 16, "bf16", True, True, 0),
+    ([90, 40], [0, 2], [3, 5], [1, 1], 4, 2, 64, 16, "bf16", True, True, 0),                # a group of none
+    ([40, 90], [2, 0], [3, 5], [1, 1], 4, 2, 64, 16, "f16", True, True, 0),
+    ([150], [4], [20, 9, 1, 40], [20, 4, 1, 33], 6, 2, 128, 64, "bf16", True, True, 0),
+    ([150], [3], [20, 0, 40], [20, 0, 33], 40, 2, 64, 16, "f16", False, False, 0),          # a sequence of nothing; not causal
+    ([20, 7], [2, 2], [3, 0, 1, 2], [9, 25, 1, 30], 4, 2, 64, 16, "bf16", True, True, 0),   # queries in the prefix, and before it
+    ([300], [3], [50, 3, 0], [1, 1, 1], 8, 2, 128, 32, "f16", True, True, 40),              # windows that reach back into it
+    ([300, 100], [2, 2], [50, 3, 200, 64], [50, 3, 100, 1], 4, 1, 64, 16, "bf16", True, True, 70),
+    ([300], [2], [50, 3], [20, 3], 4, 1, 128, 64, "bf16", True, False, 70),
+    ([200], [2], [70, 20], [70, 20], 24, 1, 128, 16, "f16", True, True, 1),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_small(case):
+    *shape, causal, window = CASES[case]
+    b = Batch(case, *shape)
+    lse = torch.empty(b.q.shape[:2], device="cuda")
+    o = b.attend(causal=causal, window=window, lse=lse)
+    assert o.shape == b.q.shape and o.dtype == b.q.dtype
+    b.check(o, lse, causal, window)
+    if set(b.counts) == {1}:                       # the same as queries of a ragged batch
+        b.check(b.attend(ragged=True, causal=causal, window=window), None, causal, window)
+
+
+#         prefix, sizes, lens, counts, heads, kv, d, page, dtype | many, own_many
+SHARED = [
+    ([1000], [70], None, [1] * 70, 16, 16, 64, 16, "bf16", 0, 0),
+    ([1000], [70], None, [1] * 70, 16, 16, 128, 64, "f16", 0, 0),
+    ([700, 1100], [60, 30], None, [1] * 90, 32, 8, 128, 32, "bf16", 0, 0),
+    ([2000], [12], None, [1, 3, 2] * 4, 12, 12, 128, 16, "bf16", 0, 0),
+    ([700, 1100], [100, 60], None, [1] * 160, 32, 4, 128, 32, "bf16", 1, 0),
+    ([1100, 500, 0], [40, 30, 8], None, [1] * 78, 40, 8, 64, 64, "f16", 1, 0),
+    ([1100], [100], None, [1] * 100, 40, 8, 128, 16, "f16", 1, 0),
+    ([1300, 70], [30, 50], None, [1, 2, 3, 4] * 20, 16, 8, 64, 16, "bf16", 1, 0),
+    ([1500, 100, 1300], [2, 1, 2], [1300, 2, 1100, 300, 1200], [1300, 2, 1100, 100, 1200], 24, 8, 64, 16, "bf16", 1, 1),
+    ([900, 100], [1, 2], [1300, 1100, 300], [1300, 1100, 100], 24, 8, 128, 64, "f16", 1, 1),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", range(len(SHARED)))
+def test_shared(case, causal):
+    prefix, sizes, lens, counts, heads, kv, d, page, dtype, many, own_many = SHARED[case]
+    lens = lens or [(i * 37) % 90 + max(0, counts[i] - (i % 5 == 0)) * (i % 7 != 0) for i in range(len(counts))]     # among them queries in the prefix
+    b = Batch(case, prefix, sizes, lens, counts, heads, kv, d, page, dtype)
+    p = b.plan()
+    assert (p.separate, p.many, p.own_many) == (0, many, own_many)
+    lse = torch.empty(b.q.shape[:2], device="cuda")
+    o = b.attend(lse=lse, causal=causal)
+    b.check(o, lse, causal)
+    for _ in range(3):
+        assert torch.equal(o, b.attend(causal=causal))
+
+
+def test_forked_sequences_as_the_pool_has_them():
+    """a prompt, forked; the same from whole tables by kv4_attention, to the roundings of both"""
+    page, kv, heads, d = 16, 4, 16, 128
+    pool, cache, h = rq.PagePool(200, page), rq.kv4_cache(200, kv, d, page), rq.hadamard_build(d)
+    g = torch.Generator(device="cuda").manual_seed(0)
+
+    def extend(seq, n):
+        slots, copies = pool.extend(seq, n)
+        if copies:
+            src, dst = torch.tensor(copies, dtype=torch.int32).t().contiguous().cuda()
+            rq.kv4_copy_pages(cache, src, dst)
+        k, v = torch.randn((2, n, kv, d), generator=g, device="cuda", dtype=torch.bfloat16)
+        rq.kv4_append(h, cache, k, v, torch.tensor(slots).cuda())
+
+    pool.add(0)
+    extend(0, 531)
+    for s in range(1, 20):
+        pool.fork(0, s)
+    for s in range(20):
+        extend(s, 1 + 3 * s % 40)
+    tables = [pool.table(s) for s in range(20)]
+    shared = pool.common_pages(range(20))
+    assert shared == 531 // page and all(t[:shared] == tables[0][:shared] for t in tables)
+    q = torch.randn((20, heads, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    pad = lambda rows: ints([r + [-1] * (max(map(len, rows)) - len(r)) for r in rows])  # noqa: E731
+    lens = [pool.length(s) for s in range(20)]
+    whole = rq.kv4_attention(h, cache, q, pad(tables), ints(lens))
+    o = rq.kv4_prefix_attention(h, cache, q, ints([tables[0][:shared]]), ints([shared * page]), ints([0, 20]), pad([t[shared:] for t in tables]),
+                                ints([n - shared * page for n in lens]))
+    # (both are within the bound of kv4_reference of the true result, which is about this; and a rounding each)
+    assert (o.float() - whole.float()).norm() <= 2.0 ** -7 * whole.float().norm()
+
+
+def test_lengths_and_groups_out_of_range():
+    b = Batch(20, [48, 20], [2, 2], [16, 3, 9, 16], [1] * 4, 4, 2, 64, 16)
+    want = b.attend()
+    assert torch.equal(want, b.attend(max_prefix=48, max_len=16))
+    assert torch.equal(b.attend(prefix_lens=ints([1000, -3]), kv_lens=ints([99, -1, 9, 16])), b.attend(prefix_lens=ints([48, 0]), kv_lens=ints([16, 0, 9, 16])))
+    assert torch.equal(b.attend(max_prefix=30, max_len=5), b.attend(prefix_lens=ints([30, 20]), kv_lens=ints([5, 3, 5, 5])))
+    none = b.attend(prefix_lens=ints([0, 0]), kv_lens=ints([0, 0, 0, 0]))
+    assert (none == 0).all()
+    b.prefix_table.fill_(1 << 30)                   # pages that are none read page 0
+    b.table.fill_(-9)
+    far = b.attend()
+    b.prefix_table.zero_(), b.table.zero_()
+    assert torch.equal(far, b.attend())
+
+
+@pytest.mark.parametrize("shape", [([200], [4], [20, 9, 1, 40], [20, 4, 1, 33], 6, 2, 64, 16), ([900], [70], [i % 80 + 1 for i in range(70)], [1] * 70, 16, 8, 64, 16),
+                                   ([900], [70], [i % 80 + 1 for i in range(70)], [1] * 70, 16, 16, 128, 64)])
+def test_what_a_query_does_not_see_does_not_reach_it(shape):
+    """a key of one sequence's own, and one of the prefix that only queries in it do not see"""
+    b = Batch(21, *shape)
+    clean = b.attend()
+    bad = torch.full((1, b.kv, b.d), float("nan"), device="cuda")
+    rq.kv4_append(b.h, b.cache, bad, bad, torch.tensor(b.slots[1][1][:1]).cuda())
+    o = b.attend()
+    at, n = sum(b.counts[:1]), b.counts[1]
+    see = slice(at + max(0, n - b.lens[1]), at + n)
+    assert torch.isnan(o[see]).all()
+    o[see] = clean[see]
+    assert torch.equal(o, clean)
+    rq.kv4_append(b.h, b.cache, bad, bad, torch.tensor(b.slots[0][0][5:6]).cuda())
+    assert torch.isnan(b.attend()).all()
+
+
+@pytest.mark.parametrize("pad", [8, 1])
+@pytest.mark.parametrize("n", [3, 70])
+def test_strides(pad, n):
+    b = Batch(22, [700], [n], [i % 30 + 1 for i in range(n)], [1] * n, 16, 16, 64, 16, "f16")
+    want = b.attend()
+    wide = torch.zeros((n, 18, 64 + pad), dtype=torch.float16, device="cuda")
+    wide[:, 1:17, pad:] = b.q
+    out = torch.full((n, 20, 64 + pad), 7.0, dtype=torch.float16, device="cuda")
+    b.attend(q=wide[:, 1:17, pad:], out=out[:, 4:, pad:])
+    assert torch.equal(out[:, 4:, pad:], want) and (out[:, :4] == 7).all() and (out[:, :, :pad] == 7).all()
+
+
+def test_in_graphs_with_one_workspace_and_on_another_stream():
+    """two graphs of calls that share a caller's workspace, replayed in turn with eager calls between"""
+    bs = [Batch(23, [900], [70], [i % 30 + 1 for i in range(70)], [1] * 70, 16, 16, 64, 16), Batch(24, [800, 90], [40, 30], [i % 30 + 1 for i in range(70)], [1] * 70, 32, 8, 128, 64)]
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for b in bs:
+        out = torch.empty_like(b.q)
+        b.attend(out=out, workspace=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.attend(out=out, workspace=ws)
+        graphs.append(g), outs.append(out)
+    for i in range(3):
+        for b, g, out in zip(bs, graphs, outs):
+            b.q.normal_()
+            b.kv_lens.fill_(i + 1)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, b.attend())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = [b.attend(stream=s) for b in bs]
+    s.synchronize()
+    assert all(torch.equal(x, b.attend()) for x, b in zip(got, bs))
+
+
+def test_offsets_beyond_four_gigabytes():
+    size = binding.kv4_page_bytes(8, 128, 256)
+    pages = (9 << 30) // size
+    big, small = rq.KV4Cache(torch.empty((pages, size), dtype=torch.uint8, device="cuda"), 8, 128, 256), rq.kv4_cache(4, 8, 128, 256)
+    k = torch.randn((1000, 8, 128), device="cuda", dtype=torch.bfloat16)
+    slots = torch.arange(1000).cuda()
+    far = torch.tensor([pages - 1, pages - 7, pages // 2 + 1, pages - 3]).cuda()
+    for c, s in ((small, slots), (big, far[slots // 256] * 256 + slots % 256)):
+        rq.kv4_append(None, c, k, k, s)
+    q = torch.randn((3, 8, 128), device="cuda", dtype=torch.bfloat16)
+    lens, start = ints([400]), ints([0, 3])
+    out = []
+    for c, t in ((small, ints([0, 1, 2, 3])), (big, far.int())):
+        out.append(rq.kv4_prefix_attention(None, c, q, t[None, :2], lens, start, t[2:].view(1, 2).expand(3, 2).contiguous(), ints([400, 3, 257])))
+        w, lse = torch.zeros((1, 8, 1024), device="cuda"), torch.zeros((1, 8), device="cuda")
+        rq.kv4_attention(None, c, q[:1], t[None], ints([1000]), lse=lse)
+        rq.kv4_attention_weights(None, c, q[:1], lse, t[None], ints([1000]), w)
+        index = rq.kv4_select(w, ints([1000]), 300, 4, 40)
+        rq.kv4_evict(c, index, t[None], weights=w)
+        at = t.long()[slots[:300] // 256] * 256 + slots[:300] % 256
+        out += [w, index, *rq.kv4_read(None, c, at)]
+    assert all(torch.equal(x, y) for x, y in zip(out[:len(out) // 2], out[len(out) // 2:]))
+
+
+def test_refusals():
+    b = Batch(25, [40], [2], [5, 9], [1, 1], 4, 2, 64, 16)
+    call = dict(h=b.h, cache=b.cache, q=b.q, prefix_table=b.prefix_table, prefix_lens=b.prefix_lens, group_start=b.group_start, table=b.table, kv_lens=b.kv_lens)
+    rq.kv4_prefix_attention(**call)
+    for bad in (dict(q=b.q.cpu()), dict(q=b.q[..., :32]), dict(q=b.q[:1]), dict(prefix_table=b.prefix_table.long()), dict(prefix_table=b.prefix_table[0]),
+                dict(prefix_lens=b.prefix_lens.long()), dict(prefix_lens=ints([1, 2])), dict(group_start=ints([0])), dict(group_start=b.group_start.cpu()),
+                dict(table=b.table[:1]), dict(kv_lens=b.kv_lens[:1]), dict(q_start=ints([0, 2])), dict(out=torch.empty_like(b.q).float()),
+                dict(lse=torch.empty((2, 3), device="cuda"))):
+        with pytest.raises(ValueError):
+            rq.kv4_prefix_attention(**{**call, **bad})
+    for bad in (dict(q=b.q.float()), dict(scale=0.0), dict(window=-1), dict(max_len=-1), dict(max_prefix=-1), dict(h=rq.hadamard_build(128)),
+                dict(prefix_table=b.prefix_table[:0], prefix_lens=b.prefix_lens[:0], group_start=ints([0])), dict(out=torch.empty_like(b.q)[:, :1].expand(2, 4, 64))):
+        with pytest.raises(rq.RotqError):
+            rq.kv4_prefix_attention(**{**call, **bad})
+    many = Batch(26, [900], [70], [3] * 70, [1] * 70, 16, 16, 64, 16)
+    with pytest.raises(rq.RotqError):
+        many.attend(workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))

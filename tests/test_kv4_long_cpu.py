@@ -1,9 +1,11 @@
 """CPU-only: argument checks of the 4-bit cache's calls for long contexts."""
 import ctypes as C
+import random
 
 import pytest
 
 from paper_2504_13989_amd import binding
+from paper_2504_13989_amd.pages import PagePool
 from test_kv4_cpu import BAD_CACHES, cache
 
 ARG, OK = binding.RQ_ERR_ARG, binding.RQ_OK
@@ -66,3 +68,88 @@ def test_evict_refuses(L):
         assert evict(**bad) == ARG, bad
     assert evict(layers=0, index=None, table=None) == evict(batch=0, index=None, table=None) == OK
     assert evict(keep=0, index=None, table=None, w=None, n=0) == OK
+
+
+def test_prefix_attention_refuses(L):
+    ok = dict(h=None, c=cache(), Q=64, dtype=0, tokens=3, heads=4, q=(512, 128), ptable=64, groups=2, pwidth=3, plens=64, gstart=64, table=64, batch=3, width=2,
+              lens=64, start=None, scale=0.1, causal=1, window=0, max_prefix=48, max_len=32, out=4096, o=(512, 128), lse=None, ws=None, ws_bytes=0)
+
+    def attend(**kw):
+        a = {**ok, **kw}
+        return L.rq_kv4_prefix_attention(a["h"], a["c"], a["Q"], a["dtype"], a["tokens"], a["heads"], *a["q"], a["ptable"], a["groups"], a["pwidth"], a["plens"],
+                                         a["gstart"], a["table"], a["batch"], a["width"], a["lens"], a["start"], a["scale"], a["causal"], a["window"],
+                                         a["max_prefix"], a["max_len"], a["out"], *a["o"], a["lse"], a["ws"], a["ws_bytes"], None)
+
+    for bad in BAD_CACHES:
+        assert attend(c=cache(**bad)) == ARG, bad
+    for bad in (dict(Q=None), dict(Q=65), dict(out=None), dict(out=65), dict(dtype=binding.RQ_F32), dict(dtype=9), dict(tokens=-1), dict(tokens=1 << 25),
+                dict(heads=0), dict(heads=3), dict(heads=2 * 257), dict(q=(-1, 128)), dict(o=(512, -1)), dict(o=(100, 128)), dict(o=(512, 127)),
+                dict(ptable=None), dict(ptable=66), dict(groups=0), dict(groups=-1), dict(groups=1 << 21), dict(pwidth=-1), dict(plens=None), dict(plens=66),
+                dict(gstart=None), dict(gstart=66), dict(table=None), dict(table=66), dict(batch=-1), dict(batch=0), dict(width=-1), dict(lens=None),
+                dict(lens=66), dict(start=66), dict(tokens=4), dict(scale=0.0), dict(scale=float("nan")), dict(causal=2), dict(window=-1), dict(max_prefix=-1),
+                dict(max_prefix=49), dict(max_len=-1), dict(max_len=33), dict(pwidth=1 << 27, max_prefix=1 << 30), dict(lse=66)):
+        assert attend(**bad) == ARG, bad
+    assert attend(h=binding.hadamard_build(64)._h) == ARG
+    assert attend(tokens=0, batch=0, groups=0, Q=None, out=None, lens=None, table=None, ptable=None, plens=None, gstart=None) == OK
+
+
+def prefix_plan(L, units=256, **kw):
+    a = dict(dtype=0, tokens=3, heads=4, groups=1, batch=3, decode=1, window=0, max_prefix=4096, max_len=64)
+    a.update(kw)
+    p = binding.RqKv4PrefixPlan()
+    rc = L.rq_kv4_prefix_attention_plan(cache(kv_heads=a.pop("kv", 2), head_dim=a.pop("d", 128)), *a.values(), units, C.byref(p))
+    return p if rc == OK else rc
+
+
+def test_prefix_plan_refuses(L):
+    assert prefix_plan(L).separate == 1
+    for bad in (dict(dtype=1), dict(tokens=0), dict(tokens=4), dict(heads=3), dict(groups=0), dict(groups=1 << 21), dict(batch=0, tokens=0), dict(window=-1),
+                dict(max_prefix=-1), dict(max_len=-1), dict(max_prefix=1 << 30), dict(units=-1)):
+        assert prefix_plan(L, **bad) == ARG, bad
+        if "units" not in bad and "dtype" not in bad:
+            a = dict(tokens=3, heads=4, groups=1, batch=3, decode=1, window=0, max_prefix=4096, max_len=64)
+            a.update(bad)
+            if a["tokens"] != 4:
+                assert L.rq_kv4_prefix_attention_workspace(cache(), *a.values()) == 0, bad
+
+
+def test_prefix_chunks_cover_all_keys(L):
+    rng, seen = random.Random(2), {}
+    for _ in range(6000):
+        kv, group = rng.choice((1, 2, 4, 8, 32)), rng.choice((1, 1, 2, 4, 5, 8, 40))
+        batch = int(2 ** rng.uniform(0, 8))
+        counts = rng.choice((1, 1, 3, 50, 700))
+        a = dict(kv=kv, heads=kv * group, d=rng.choice((64, 128)), dtype=rng.choice((0, 2)), tokens=batch * counts, batch=batch, groups=min(batch, rng.choice((1, 1, 2, 9))),
+                 decode=int(counts == 1), window=rng.choice((0, 0, 0, 100)), max_prefix=int(2 ** rng.uniform(0, 17)), max_len=int(2 ** rng.uniform(0, 13)))
+        p = prefix_plan(L, units=rng.choice((64, 256, 304)), **a)
+        assert p.own_rows in (4, 8, 16, 128)
+        if p.separate:
+            assert p.waves in (4, 8) and not p.many and not p.own_many
+        else:
+            assert a["window"] in (0, 100) and (a["window"] == 0 or a["max_prefix"] + a["max_len"] <= 100) and p.shared_rows in (4, 8, 16, 128)
+            assert p.shared_chunk % 64 == p.own_chunk % 64 == 0
+            assert p.shared_chunk * p.shared_chunks >= a["max_prefix"] and p.own_chunk * p.own_chunks >= a["max_len"]
+            assert p.shared_chunk * (p.shared_chunks - 1) < a["max_prefix"] + 64 and p.own_chunk * (p.own_chunks - 1) < a["max_len"] + 64
+        key = (p.separate, p.many, p.own_many, p.shared_chunks > 1)
+        seen[key] = seen.get(key, 0) + 1
+    assert all(seen.get(k, 0) >= 10 for k in ((1, 0, 0, False), (0, 0, 0, True), (0, 1, 0, True), (0, 1, 1, True))), seen
+
+
+def test_common_pages():
+    pool = PagePool(40, 16)
+    pool.add("a")
+    pool.extend("a", 50)
+    assert pool.common_pages(["a"]) == 3 and pool.common_pages([]) == 0
+    pool.fork("a", "b")
+    assert pool.common_pages("ab") == 3            # the fourth is not full
+    pool.extend("a", 1)
+    pool.extend("b", 30)
+    assert pool.common_pages(["a", "b"]) == pool.common_pages(["b", "a"]) == 3
+    pool.fork("b", "c")
+    assert pool.common_pages("bc") == 5 and pool.common_pages("abc") == 3
+    pool.truncate("c", 20)
+    assert pool.common_pages("bc") == 1
+    pool.add("d")
+    assert pool.common_pages("ad") == 0
+    pool.extend("d", 64)
+    assert pool.common_pages("ad") == 0
