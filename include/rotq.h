@@ -567,6 +567,7 @@ int rq_kv4_prefix_attention_plan(const rq_kv4_t* cache, int dtype, int64_t token
  *   tokens       [in]  0 .. 2^24 (none: the weights decay)
  *   decay        [in]  0 .. 1
  *   weights      [inout] DEVICE, element [b][y][j] at b * w_seq_stride + y * w_head_stride + j; rows of max_len must not overlap
+ *   max_len      [in]  times batch, at most 2^37
  *   workspace    [in]  DEVICE, >= rq_kv4_attention_weights_workspace(...) bytes, 16-byte aligned, scratch; NULL where that is 0
  * The same call gives the same bits.  Errors: RQ_ERR_ARG, RQ_ERR_HIP.
  */

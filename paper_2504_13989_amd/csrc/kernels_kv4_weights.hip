@@ -13,6 +13,7 @@ namespace rq {
 namespace {
 
 constexpr int kWaves = 4;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // A tile's key codes and parameters (of key 16 i + lane % 16).
 template <int D>
@@ -41,16 +42,21 @@ __device__ __forceinline__ f16x8 key_operand(uint32_t w, const CodeBits& bits) {
     return __builtin_bit_cast(f16x8, u32x4{f(bits.low(w), low), f(bits.high(w), high), f(bits.low(h), low), f(bits.high(h), high)});
 }
 
+// The same less 7.5, which costs two shifts more.
+__device__ __forceinline__ f16x8 key_codes(uint32_t w, const CodeBits& bits) {
+    const f16x2 less{(_Float16)-71.5f, (_Float16)-71.5f};
+    const auto f = [&](uint32_t x) { return __builtin_bit_cast(uint32_t, as_f16(bits.high(x)) + less); };
+    return __builtin_bit_cast(f16x8, u32x4{f(w << 4), f(w), f(w >> 4), f(w >> 8)});
+}
+
 // What a row needs besides its operand, in the lanes of the row's results.
 struct RowTerms {
     float f;                                      // log2 of the weight for a unit of the product, a power of two
     float sum;                                    // of the row's elements
     float lse;                                    // log2 of the softmax's sum; infinity where there is no row
-    int lo, seen;                                 // the first position that it sees, how many
 };
 struct Rows {
     float f[4], sum[4], lse[4];
-    int lo[4], seen[4];
 };
 __device__ __forceinline__ void spread(Rows& r, const RowTerms& t, int lane) {
 #pragma unroll
@@ -59,26 +65,12 @@ __device__ __forceinline__ void spread(Rows& r, const RowTerms& t, int lane) {
         r.f[e] = __shfl(t.f, from);
         r.sum[e] = __shfl(t.sum, from);
         r.lse[e] = __shfl(t.lse, from);
-        r.lo[e] = __shfl(t.lo, from);
-        r.seen[e] = __shfl(t.seen, from);
     }
 }
 
-// Weights of one block of 16 keys for the tile's rows, summed over the lane's four.
-__device__ __forceinline__ float weigh(const f32x4& s, const Rows& r, float step, float mid, int key, bool whole) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        float x = fmaf(step, r.f[e] * s[e], fmaf(mid, r.f[e] * r.sum[e], -r.lse[e]));
-        if (!whole) x = (uint32_t)(key - r.lo[e]) < (uint32_t)r.seen[e] ? x : -INFINITY;
-        sum += __builtin_amdgcn_exp2f(x);
-    }
-    return sum;
-}
-
-// F: copies of 16 / F rows among the sixteen, of which each takes every F-th 16 keys (few rows: one tile of them a sequence).
-// MANY: row tiles of 16 one after the other.  A wave takes every fourth tile of 64 keys of the workgroup's chunk.
-template <int D, int F, bool F16, bool PAGED, bool MANY>
+// One query a sequence, at most sixteen heads a kv head.  F: copies of 16 / F rows among the sixteen, of which each takes every F-th 16 keys.
+// A wave takes every fourth tile of 64 keys of the workgroup's chunk.
+template <int D, int F, bool F16, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4Weights out) {
     constexpr int C = 16 / F;
     const Kv4Attention& a = job.a;
@@ -89,15 +81,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
     const int head_at = head * ((D + 8) << job.cache.page_shift);
     int len = a.kv_lens[seq];
     len = len < 0 ? 0 : len > a.max_len ? (int)a.max_len : len;
-    int q0 = seq, nq = 1;
-    if (a.q_start) {
-        q0 = a.q_start[seq];
-        int q1 = a.q_start[seq + 1];
-        q0 = q0 < 0 ? 0 : q0 > a.tokens ? a.tokens : q0;
-        q1 = q1 < q0 ? q0 : q1 > a.tokens ? a.tokens : q1;
-        nq = q1 - q0;
-    }
-    const int rows = nq * job.group;
     const int begin = chunk * job.chunk, end = begin + job.chunk < len ? begin + job.chunk : len;
     constexpr int stride = kWaves * kTile;
     int k0 = begin + wave * kTile;
@@ -109,24 +92,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
     load_keys<D, PAGED>(t, job.cache, pages, 0, head_at, k0, lane);
     Query<D, 16> q;
     Rows r;
-    int all_lo = 0, all_hi = 0;                   // what all rows of the tile see
-    const auto take_rows = [&](int base) {
-        const int n = base + (lane & 15) % C;
-        const bool there = n < rows;
-        const int token = there ? (nq == 1 ? 0 : n / job.group) : 0, of = there ? n - token * job.group : 0;
-        const RawQuery<D, 16> raw = load_query<D, 16>(job, there, q0 + token, head * job.group + of, lane);
-        const float lse = there ? a.lse[(int64_t)(q0 + token) * a.heads + head * job.group + of] : 0.0f;
+    const int n = (lane & 15) % C;
+    const bool there = n < job.group;
+    {
+        const int x = head * job.group + (there ? n : 0);
+        const RawQuery<D, 16> raw = load_query<D, 16>(job, there, seq, x, lane);
+        const float lse = there ? a.lse[(int64_t)seq * a.heads + x] : 0.0f;
         take_query<D, 16, F16, true>(q, job, raw, lane);
-        const int pos = len - nq + token;
-        const int hi = !there ? 0 : a.causal ? (pos + 1 < len ? pos + 1 : len) : len;
-        const int lo = a.window ? (pos - a.window + 1 > 0 ? pos - a.window + 1 : 0) : 0;
-        spread(r, RowTerms{q.f, q.even + q.odd, there ? lse * kLog2e : INFINITY, lo, hi > lo ? hi - lo : 0}, lane);
-        const int last = (base + C < rows ? base + C : rows) - 1;
-        const int p0 = len - nq + (nq == 1 ? 0 : base / job.group), p1 = len - nq + (nq == 1 ? 0 : last / job.group);
-        all_lo = a.window ? p1 - a.window + 1 : 0;
-        all_hi = a.causal && p0 + 1 < len ? p0 + 1 : len;
-    };
-    if (!MANY) take_rows(0);
+        spread(r, RowTerms{q.f, q.even + q.odd, there ? lse * kLog2e : INFINITY}, lane);
+    }
+    const int lo = a.window && len > a.window ? len - a.window : 0;          // the first position that the query sees: it stands at the last
     for (; k0 < end; k0 += stride) {
         KeyCodes<D> next;
         if (k0 + stride < end) {
@@ -137,44 +112,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
             load_keys<D, PAGED>(next, job.cache, pages, number_of, head_at, k0 + stride, lane);
         }
         float sums[4 / F] = {};
-        const auto take = [&] {
-            const bool whole = k0 >= all_lo && k0 + kTile <= all_hi;
 #pragma unroll
-            for (int u = 0; u < 4 / F; ++u) {
-                f32x4 s{};
-                float step = 0.0f, mid = 0.0f;
+        for (int u = 0; u < 4 / F; ++u) {
+            f32x4 s{};
+            float step = 0.0f, mid = 0.0f;
 #pragma unroll
-                for (int f = 0; f < F; ++f) {
-                    const int i = u * F + f;
-                    f32x4 acc;
+            for (int f = 0; f < F; ++f) {
+                const int i = u * F + f;
+                f32x4 acc;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[e] = 0.5f * r.sum[e];
+                for (int e = 0; e < 4; ++e) acc[e] = 0.5f * r.sum[e];
 #pragma unroll
-                    for (int j = 0; j < D / 32; ++j) {
-                        const f16x8 b = key_operand(t.k[i][j], bits);
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(q.hi[j], b, acc, 0, 0, 0);
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(q.lo[j], b, acc, 0, 0, 0);
-                    }
-                    const bool mine = F == 1 || copy == f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = mine ? acc[e] : s[e];
-                    step = mine ? __uint_as_float(t.kp[i] << 16) : step;
-                    mid = mine ? __uint_as_float(t.kp[i] & 0xffff0000u) : mid;
+                for (int j = 0; j < D / 32; ++j) {
+                    const f16x8 b = key_operand(t.k[i][j], bits);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(q.hi[j], b, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(q.lo[j], b, acc, 0, 0, 0);
                 }
-                sums[u] += weigh(s, r, step, mid, k0 + 16 * (u * F + (F == 1 ? 0 : copy)) + (lane & 15), whole);
+                const bool mine = F == 1 || copy == f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = mine ? acc[e] : s[e];
+                step = mine ? __uint_as_float(t.kp[i] << 16) : step;
+                mid = mine ? __uint_as_float(t.kp[i] & 0xffff0000u) : mid;
             }
-        };
-        if constexpr (MANY) {
-            // the row tiles that see some of the tile: positions from k0 on if causal, and not behind the window's reach
-            int first = 0, last = rows;
-            if (a.causal && k0 - (len - nq) > 0) first = (k0 - (len - nq)) * job.group / C * C;
-            if (a.window && k0 + kTile - 1 + a.window - (len - nq) < nq) last = (k0 + kTile - 1 + a.window - (len - nq)) * job.group;
-            for (int base = first; base < last; base += C) {
-                take_rows(base);
-                take();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = fmaf(step, r.f[e] * s[e], fmaf(mid, r.f[e] * r.sum[e], -r.lse[e]));
+                sums[u] += __builtin_amdgcn_exp2f(x);
             }
-        } else if (rows > 0) {
-            take();
         }
         // a key's sum is in the lanes of its column that have rows of its copy
         float total = 0.0f;
@@ -199,41 +163,305 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
         const int key = k0 + 16 * block + (lane & 15);
         if (key < end) {
             float* w = out.weights + seq * out.w_seq + head * out.w_head + key;
-            *w = out.decay == 0.0f ? total : fmaf(out.decay, *w, total);
+            const float seen = key >= lo ? total : 0.0f;
+            *w = out.decay == 0.0f ? seen : fmaf(out.decay, *w, seen);
         }
         t = next;
     }
 }
 
-template <int D, int F, bool F16, bool MANY>
-void launch(const KvJob& job, const Kv4Weights& w, hipStream_t s) {
+// ---- many rows
+
+// Row tile `tile` of 32 as the matrix cores take it, for every kv head: [tile][kv head][step][high, low][lane] sixteens of bytes, as
+// Query<D, 32> has them, and [tile][kv head] terms of its rows.
+struct TileTerms {
+    float f[32], shift[32], lse[32];              // f as in RowTerms, f times the sum of the row's elements, -lse
+    int at[32];                                   // the row's query among its sequence's
+};
+template <int D>
+constexpr int kTileBytes = 32 * D * 4;
+template <int D>
+__device__ __forceinline__ uint8_t* tile_at(const KvJob& job, int tile, int head) {
+    return reinterpret_cast<uint8_t*>(job.part) + ((int64_t)tile * job.cache.kv_heads + head) * (kTileBytes<D> + (int)sizeof(TileTerms));
+}
+
+template <int D, bool F16>
+__global__ __launch_bounds__(64 * kWaves) void k_kv4_weights_rows(KvJob job) {
+    const Kv4Attention& a = job.a;
+    const int lane = threadIdx.x & 63, tile = item_number() * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.x;
+    Place at;
+    if (tile >= job.tiles || !find_rows<32>(job, tile, at)) return;
+    const int n = at.base + (lane & 31);
+    const bool there = n < at.nq * job.group;
+    const int token = there ? token_of(job, at, n) : 0, x = head * job.group + (there ? n - token * job.group : 0);
+    const RawQuery<D, 32> raw = load_query<D, 32>(job, there, at.q0 + token, x, lane);
+    const float lse = there ? a.lse[(int64_t)(at.q0 + token) * a.heads + x] : 0.0f;
+    Query<D, 32> q;
+    take_query<D, 32, F16, true>(q, job, raw, lane);
+    uint8_t* to = tile_at<D>(job, tile, head);
+    u32x4* w = reinterpret_cast<u32x4*>(to);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+        w[(2 * j) * 64 + lane] = __builtin_bit_cast(u32x4, q.hi[j]);
+        w[(2 * j + 1) * 64 + lane] = __builtin_bit_cast(u32x4, q.lo[j]);
+    }
+    TileTerms* terms = reinterpret_cast<TileTerms*>(to + kTileBytes<D>);
+    if (lane < 32) {
+        terms->f[lane] = q.f;
+        terms->shift[lane] = q.f * (q.even + q.odd);
+        terms->lse[lane] = there ? -lse * kLog2e : -INFINITY;
+        terms->at[lane] = token;
+    }
+}
+
+// A workgroup takes 256 keys, 64 a wave, unpacked once into registers, and a share of the row tiles that see some of them; row tiles come
+// through LDS, the next one while this one is multiplied.
+template <int D, bool PAGED>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, Kv4Weights out, float* parts) {
+    constexpr int S = D / 16, N = 2 * S * 64 / (64 * kWaves);        // steps; sixteens of bytes of a tile that a thread brings
+    struct Staged {
+        u32x4 q[2 * S * 64];
+        TileTerms terms;
+    };
+    __shared__ __attribute__((aligned(16))) Staged staged[2];
+    static_assert(sizeof(TileTerms) == 16 * 32, "half a wave brings the terms");
+    const Kv4Attention& a = job.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    // (the last keys of a causal sequence are seen least: the first begin first)
+    const int per = job.chunks * job.workers, item = item_number(), seq = item / per, rest = item - seq * per, chunk = rest / job.workers, share = rest - chunk * job.workers;
+    const int head = blockIdx.x;
+    if (seq >= a.batch) return;
+    const int len = own_len(job, seq), first_key = chunk * (kWaves * kTile);
+    if (first_key >= len) return;
+    int q0 = seq, nq = 1;
+    if (a.q_start) {
+        q0 = a.q_start[seq];
+        int q1 = a.q_start[seq + 1];
+        q0 = q0 < 0 ? 0 : q0 > a.tokens ? a.tokens : q0;
+        q1 = q1 < q0 ? q0 : q1 > a.tokens ? a.tokens : q1;
+        nq = q1 - q0;
+    }
+    const int first_pos = len - nq;               // of the sequence's first query
+    const int first_tile = a.q_start ? (int)((int64_t)q0 * job.group / 32) + seq : seq * ((job.group + 31) / 32);
+    // queries that see some of the workgroup's keys: those from the first key on, if causal, and before the window has passed the last
+    int from = 0, to = nq;
+    if (a.causal && first_key > first_pos) from = first_key - first_pos;
+    const int last_key = first_key + kWaves * kTile - 1 < len - 1 ? first_key + kWaves * kTile - 1 : len - 1;
+    if (a.window && (int64_t)last_key + a.window - first_pos < to) to = last_key + a.window - first_pos;
+    int t0 = from * job.group / 32, t1 = to > from ? (to * job.group + 31) / 32 : t0;
+    {
+        const int each = (t1 - t0 + job.workers - 1) / job.workers;
+        t0 += share * each;
+        t1 = t1 < t0 + each ? t1 : t0 + each;
+    }
+    const int k0 = first_key + wave * kTile;
+    const int head_at = head * ((D + 8) << job.cache.page_shift);
+    // the wave's keys: lane n of a block of 32 has the half-row `half` of key n
+    f16x8 keys[2][S];
+    float step[2], mid[2], sum[2] = {};
+    u32x4 next[N];
+    const auto bring = [&](int tile) {
+        const u32x4* x = reinterpret_cast<const u32x4*>(tile_at<D>(job, first_tile + tile, head));
+#pragma unroll
+        for (int i = 0; i < N; ++i) next[i] = x[threadIdx.x + 64 * kWaves * i];
+    };
+    const auto bring_terms = [&](int tile) { return reinterpret_cast<const u32x4*>(tile_at<D>(job, first_tile + tile, head) + kTileBytes<D>)[threadIdx.x & 31]; };
+    u32x4 next_terms{};
+    if (t0 < t1) {
+        bring(t0);
+        next_terms = bring_terms(t0);
+    }
+    {
+        const CodeBits bits;
+        const int32_t* table = a.table + (int64_t)seq * a.width;
+        const int pages = load_pages<PAGED>(job.cache, table, a.width, k0, kTile, lane);
+        uint32_t raw[2][S], kp[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int n = 32 * i + (lane & 31);   // (a half of 32 lies in one page, or two quarters do)
+            const uint8_t* block;
+            int at;
+            if constexpr (PAGED) {
+                const bool second = (n >> 4) & 1;
+                block = second ? block_of<PAGED>(job.cache, pages, 0, 2 * i + 1, head_at) : block_of<PAGED>(job.cache, pages, 0, 2 * i, head_at);
+                at = (second ? place_of(job.cache, k0, 2 * i + 1) : place_of(job.cache, k0, 2 * i)) + (n & 15);
+            } else {
+                block = block_of<PAGED>(job.cache, pages, 0, 0, head_at);
+                at = place_of(job.cache, k0, 0) + n;
+            }
+            const u32x4* x = reinterpret_cast<const u32x4*>(block + at * (D / 2) + half * (D / 4));
+#pragma unroll
+            for (int j = 0; j < S / 4; ++j) {
+                const u32x4 y = x[j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) raw[i][4 * j + e] = y[e];
+            }
+            kp[i] = *reinterpret_cast<const uint32_t*>(block + ((D << job.cache.page_shift) + 4 * at));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int j = 0; j < S; ++j) keys[i][j] = key_codes(raw[i][j], bits);
+            step[i] = __uint_as_float(kp[i] << 16);
+            mid[i] = __uint_as_float(kp[i] & 0xffff0000u);
+        }
+    }
+    int turn = 0;
+    for (int tile = t0; tile < t1; ++tile) {
+        Staged& now = staged[turn];
+        turn ^= 1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) now.q[threadIdx.x + 64 * kWaves * i] = next[i];
+        if (threadIdx.x < 32) reinterpret_cast<u32x4*>(&now.terms)[threadIdx.x] = next_terms;
+        // (one barrier a tile: the other part of LDS was read before the last one)
+        __syncthreads();
+        if (tile + 1 < t1) {
+            bring(tile + 1);
+            next_terms = bring_terms(tile + 1);
+        }
+        f32x16 s[2] = {};
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+            const f16x8 hi = __builtin_bit_cast(f16x8, now.q[(2 * j) * 64 + lane]), lo = __builtin_bit_cast(f16x8, now.q[(2 * j + 1) * 64 + lane]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, keys[i][j], s[i], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, keys[i][j], s[i], 0, 0, 0);
+        }
+        // what all rows of the tile see: from the last one's window on to the first one's position
+        const int q_first = tile * 32 / job.group, q_last = (tile * 32 + 31) / job.group < nq ? (tile * 32 + 31) / job.group : nq - 1;
+        const bool whole = (!a.causal || k0 + kTile - 1 <= first_pos + q_first) && (!a.window || k0 > first_pos + q_last - a.window);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int row = 2 * e + 4 * half;
+            const f32x4 f = *reinterpret_cast<const f32x4*>(&now.terms.f[row]), shift = *reinterpret_cast<const f32x4*>(&now.terms.shift[row]),
+                        lse = *reinterpret_cast<const f32x4*>(&now.terms.lse[row]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) s[i][e + u] = fmaf(step[i], f[u] * s[i][e + u], fmaf(mid[i], shift[u], lse[u]));
+            if (!whole) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int pos = first_pos + now.terms.at[row + u];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int key = k0 + 32 * i + (lane & 31);
+                        if ((a.causal && key > pos) || (a.window && key <= pos - a.window)) s[i][e + u] = -INFINITY;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sum[i] += __builtin_amdgcn_exp2f(s[i][e + u]);
+        }
+    }
+    float x, y;
+    other_rows(sum[0], true, x, y);
+    const float first = x + y;
+    other_rows(sum[1], true, x, y);
+    const float total = half ? x + y : first;
+    const int key = k0 + lane;
+    if (key >= len) return;
+    if (job.workers > 1) {
+        parts[(((int64_t)share * a.batch + seq) * job.cache.kv_heads + head) * a.max_len + key] = total;
+    } else {
+        float* w = out.weights + seq * out.w_seq + head * out.w_head + key;
+        *w = out.decay == 0.0f ? total : fmaf(out.decay, *w, total);
+    }
+}
+
+// Shares of rows added up.
+__global__ __launch_bounds__(256) void k_kv4_weights_join(KvJob job, Kv4Weights out, const float* parts) {
+    const Kv4Attention& a = job.a;
+    const int64_t item = group_index(), per = (a.max_len + 255) / 256, row = item / per;
+    if (row >= (int64_t)a.batch * job.cache.kv_heads) return;
+    const int seq = (int)(row / job.cache.kv_heads), head = (int)(row - (int64_t)seq * job.cache.kv_heads);
+    const int key = (int)(item - row * per) * 256 + (int)threadIdx.x;
+    if (key >= own_len(job, seq)) return;
+    const int64_t rows = (int64_t)a.batch * job.cache.kv_heads;
+    float total = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < job.workers; ++i) total += parts[(i * rows + row) * a.max_len + key];
+    float* w = out.weights + seq * out.w_seq + head * out.w_head + key;
+    *w = out.decay == 0.0f ? total : fmaf(out.decay, *w, total);
+}
+
+// ---- launches
+
+bool few(const Kv4& c, const Kv4Attention& a) { return !a.q_start && a.heads / c.kv_heads <= 16; }
+
+// Many rows: row tiles, chunks of 256 keys, shares of the rows.
+struct Plan {
+    int tiles, chunks, shares;
+    size_t rows_bytes, bytes;
+};
+Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
+    const int64_t group = a.heads / c.kv_heads, rows = (int64_t)a.tokens * group;
+    Plan p{};
+    p.tiles = (int)(a.q_start ? rows / 32 + a.batch : (int64_t)a.batch * ((group + 31) / 32));
+    p.chunks = (int)((a.max_len + kWaves * kTile - 1) / (kWaves * kTile));
+    const int64_t wgs = (int64_t)a.batch * c.kv_heads * p.chunks, want = (2 * (int64_t)num_cu + wgs - 1) / wgs, most = (rows / 32 / a.batch + 3) / 4;
+    p.shares = (int)(want < most ? want : most);
+    if (p.shares < 1) p.shares = 1;
+    p.rows_bytes = (size_t)p.tiles * c.kv_heads * (32 * c.head_dim * 4 + sizeof(TileTerms));
+    p.bytes = p.rows_bytes + (p.shares > 1 ? (size_t)p.shares * a.batch * c.kv_heads * a.max_len * sizeof(float) : 0);
+    return p;
+}
+
+template <int D, int F, bool F16>
+void launch_few(const KvJob& job, const Kv4Weights& w, hipStream_t s) {
     const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.a.batch * job.chunks), block(64 * kWaves);
-    if (job.cache.page_shift < 6) launch_kernel(k_kv4_weights<D, F, F16, true, MANY>, grid, block, 0, s, job, w);
-    else launch_kernel(k_kv4_weights<D, F, F16, false, MANY>, grid, block, 0, s, job, w);
+    if (job.cache.page_shift < 6) launch_kernel(k_kv4_weights<D, F, F16, true>, grid, block, 0, s, job, w);
+    else launch_kernel(k_kv4_weights<D, F, F16, false>, grid, block, 0, s, job, w);
 }
 template <int D, bool F16>
-void launch(const KvJob& job, const Kv4Weights& w, hipStream_t s) {
-    if (job.a.q_start || job.group > 16) launch<D, 1, F16, true>(job, w, s);
-    else if (job.group > 8) launch<D, 1, F16, false>(job, w, s);
-    else if (job.group > 4) launch<D, 2, F16, false>(job, w, s);
-    else launch<D, 4, F16, false>(job, w, s);
+void launch_few(const KvJob& job, const Kv4Weights& w, hipStream_t s) {
+    if (job.group > 8) launch_few<D, 1, F16>(job, w, s);
+    else if (job.group > 4) launch_few<D, 2, F16>(job, w, s);
+    else launch_few<D, 4, F16>(job, w, s);
+}
+template <int D>
+void launch_many(const KvJob& job, const Kv4Weights& w, const Plan& p, hipStream_t s) {
+    const dim3 block(64 * kWaves);
+    if (job.tiles > 0 && job.a.tokens > 0) {
+        const dim3 grid = item_grid(job.cache.kv_heads, (job.tiles + kWaves - 1) / kWaves);
+        if (job.a.dtype == RQ_F16) launch_kernel(k_kv4_weights_rows<D, true>, grid, block, 0, s, job);
+        else launch_kernel(k_kv4_weights_rows<D, false>, grid, block, 0, s, job);
+    }
+    float* parts = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(job.part) + p.rows_bytes);
+    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.a.batch * p.chunks * p.shares);
+    if (job.cache.page_shift < 6) launch_kernel(k_kv4_weights_many<D, true>, grid, block, 0, s, job, w, parts);
+    else launch_kernel(k_kv4_weights_many<D, false>, grid, block, 0, s, job, w, parts);
+    if (p.shares > 1)
+        launch_kernel(k_kv4_weights_join, group_grid((job.a.max_len + 255) / 256 * job.a.batch * job.cache.kv_heads, 256), dim3(256), 0, s, job, w, parts);
 }
 
 }  // namespace
 
-size_t kv4_weights_workspace(const Kv4&, const Kv4Attention&, int) { return 0; }
+size_t kv4_weights_workspace(const Kv4& c, const Kv4Attention& a, int num_cu) { return few(c, a) || a.tokens == 0 ? 0 : plan(c, a, num_cu).bytes; }
 
-int kv4_weights(const Kv4& c, const Kv4Weights& w, int num_cu, void*, hipStream_t s) {
+int kv4_weights(const Kv4& c, const Kv4Weights& w, int num_cu, void* workspace, hipStream_t s) {
     const Kv4Attention& a = w.a;
     const bool wide_q = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_token % 8 == 0 && a.q_head % 8 == 0;
+    KvJob job{c, a, a.heads / c.kv_heads, 0, 0, 0, 0, wide_q, false, static_cast<float*>(workspace)};
+    if (!few(c, a)) {
+        const Plan p = plan(c, a, num_cu);
+        job.tiles = p.tiles;
+        job.workers = p.shares;
+        job.chunks = p.chunks;
+        c.head_dim == 128 ? launch_many<128>(job, w, p, s) : launch_many<64>(job, w, p, s);
+        return launch_rc();
+    }
     // workgroups of at least a tile a wave, eight a compute unit where there are as many
     const int64_t units = (a.max_len + kWaves * kTile - 1) / (kWaves * kTile), want = (8 * (int64_t)num_cu + (int64_t)a.batch * c.kv_heads - 1) / ((int64_t)a.batch * c.kv_heads);
     const int64_t chunks = want < units ? want : units;
-    const int chunk = (int)((units + chunks - 1) / chunks) * kWaves * kTile;
-    const KvJob job{c, a, a.heads / c.kv_heads, 0, 0, chunk, (int)((a.max_len + chunk - 1) / chunk), wide_q, false, nullptr};
+    job.chunk = (int)((units + chunks - 1) / chunks) * kWaves * kTile;
+    job.chunks = (int)((a.max_len + job.chunk - 1) / job.chunk);
     const bool f16 = a.dtype == RQ_F16;
-    if (c.head_dim == 128) f16 ? launch<128, true>(job, w, s) : launch<128, false>(job, w, s);
-    else f16 ? launch<64, true>(job, w, s) : launch<64, false>(job, w, s);
+    if (c.head_dim == 128) f16 ? launch_few<128, true>(job, w, s) : launch_few<128, false>(job, w, s);
+    else f16 ? launch_few<64, true>(job, w, s) : launch_few<64, false>(job, w, s);
     return launch_rc();
 }
 

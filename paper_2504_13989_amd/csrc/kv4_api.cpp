@@ -214,6 +214,8 @@ int rq_kv4_attention_weights(const rq_hadamard_t* h, const rq_kv4_t* cache, cons
     if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
     if (width < 0 || (causal != 0 && causal != 1) || !(scale > 0.0f) || !std::isfinite(scale) || !(decay >= 0.0f && decay <= 1.0f)) return RQ_ERR_ARG;
     if (q_token_stride < 0 || q_head_stride < 0 || w_seq_stride < 0 || w_head_stride < 0) return RQ_ERR_ARG;
+    // (a workgroup for every 256 positions, counted in 32 bits)
+    if (batch * (max_len / 256 + 1) > (1 << 30)) return RQ_ERR_ARG;
     if (!rows_apart(max_len, 1, 0, batch, w_seq_stride, c.kv_heads, w_head_stride)) return RQ_ERR_ARG;
     if (!q_start && tokens != batch) return RQ_ERR_ARG;                    // a token a sequence
     if (max_len > (int64_t)width << c.page_shift) return RQ_ERR_ARG;

@@ -29,7 +29,8 @@ def test_attention_weights_refuses(L):
                 dict(width=-1), dict(lens=None), dict(lens=66), dict(start=66), dict(tokens=4), dict(scale=0.0), dict(scale=float("inf")),
                 dict(scale=float("nan")), dict(causal=2), dict(window=-1), dict(max_len=-1), dict(max_len=33), dict(decay=-0.5), dict(decay=1.5),
                 dict(decay=float("nan")), dict(w=None), dict(w=66), dict(strides=(-64, 32)), dict(strides=(64, -32)), dict(strides=(64, 31)),
-                dict(strides=(63, 32)), dict(strides=(32, 64)), dict(strides=(0, 32)), dict(strides=(1 << 62, 32))):
+                dict(strides=(63, 32)), dict(strides=(32, 64)), dict(strides=(0, 32)), dict(strides=(1 << 62, 32)),
+                dict(batch=1 << 10, tokens=1 << 10, width=1 << 26, max_len=1 << 30, strides=(1 << 31, 1 << 30))):
         assert weigh(**bad) == ARG, bad
     assert weigh(h=binding.hadamard_build(64)._h) == ARG
     assert weigh(tokens=0, batch=0, Q=None, lse=None, lens=None, table=None, w=None) == OK
@@ -132,7 +133,7 @@ def test_prefix_chunks_cover_all_keys(L):
             assert p.shared_chunk * (p.shared_chunks - 1) < a["max_prefix"] + 64 and p.own_chunk * (p.own_chunks - 1) < a["max_len"] + 64
         key = (p.separate, p.many, p.own_many, p.shared_chunks > 1)
         seen[key] = seen.get(key, 0) + 1
-    assert all(seen.get(k, 0) >= 10 for k in ((1, 0, 0, False), (0, 0, 0, True), (0, 1, 0, True), (0, 1, 1, True))), seen
+    assert all(seen.get(k, 0) >= 10 for k in ((1, 0, 0, False), (0, 0, 0, True), (0, 1, 0, True), (0, 1, 1, False))), seen
 
 
 def test_common_pages():
