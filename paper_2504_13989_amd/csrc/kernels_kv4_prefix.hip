@@ -19,8 +19,10 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_prefix(PrefixJob job) {
 PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num_cu) {
     const int group = a.heads / c.kv_heads;
     const int64_t rows = (int64_t)a.tokens * group, shared_keys = x.max_len / kTile + 1, own_keys = a.max_len / kTile + 1;
-    const auto shared_tiles = [&](int bm) { return rows / bm + x.groups; };
-    const auto own_tiles = [&](int bm) { return a.q_start ? rows / bm + a.batch : (int64_t)a.batch * ((group + bm - 1) / bm); };
+    // (of n stretches of rows in a row, which begin where those before them end, rounded down to a tile, and one tile further each)
+    const auto tiles_of = [&](int bm, int n) { return (rows + bm - 1) / bm + n - 1; };
+    const auto shared_tiles = [&](int bm) { return tiles_of(bm, x.groups); };
+    const auto own_tiles = [&](int bm) { return a.q_start ? tiles_of(bm, a.batch) : (int64_t)a.batch * ((group + bm - 1) / bm); };
     const auto copies_of = [](int64_t mean) { return mean <= 4 ? 4 : mean <= 8 ? 2 : 1; };
     // What a row tile of 64 keys costs, in those of the kernel for few rows: one of 128 of the other as much as three of 16.
     constexpr int kManyCost = 3;
@@ -38,16 +40,25 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
         p.waves = few * c.kv_heads <= num_cu ? 8 : 4;
         return p;
     }
-    const auto split = [&](int64_t wgs, int64_t keys, int least, int64_t per_cu, int& chunk, int& chunks) {
-        const int64_t want = per_cu * num_cu / wgs, most = keys / least, n = want < most ? want : most;
-        const int64_t each = n > 1 ? (keys + n - 1) / n : keys;
-        chunk = (int)(each * kTile);
-        chunks = (int)((keys + each - 1) / each);
+    // A row tile's keys in as many chunks as cost least: rounds of workgroups that the chip holds at once, of `at_once` tiles of keys a step and
+    // kStart steps besides; partial results that are written and read again (4 TB/s, steps of 1.5 us).
+    constexpr int kStart = 3;
+    const auto split = [&](int64_t wgs, int64_t keys, int at_once, int64_t per_cu, int& chunk, int& chunks) {
+        const double join = 2.0 * a.tokens * a.heads * c.head_dim * sizeof(float) / 6e6;
+        double least = 0.0;
+        for (int64_t n = 1; n <= 256 && (n == 1 || n * at_once <= keys); ++n) {
+            const int64_t each = (keys + n - 1) / n, real = (keys + each - 1) / each;
+            const double cost = (double)((wgs * real + per_cu * num_cu - 1) / (per_cu * num_cu)) * (double)((each + at_once - 1) / at_once + kStart) + join * (double)real;
+            if (n > 1 && cost >= least) continue;
+            least = cost;
+            chunk = (int)(each * kTile);
+            chunks = (int)real;
+        }
     };
     if (p.many) {
         p.shared_tiles = (int)shared_tiles(128);
         p.groups = a.dtype != RQ_F16 || c.head_dim == 64 ? 2 : 1;
-        split((int64_t)p.shared_tiles * c.kv_heads, shared_keys, 8, p.groups == 2 ? 1 : 2, p.shared_chunk, p.shared_chunks);
+        split((int64_t)p.shared_tiles * c.kv_heads, shared_keys, p.groups, p.groups == 2 ? 1 : 2, p.shared_chunk, p.shared_chunks);
     } else {
         const int64_t mean = rows / x.groups;
         p.shared_copies = copies_of(mean);

@@ -9,6 +9,8 @@
 //   - Queries are two fp16 numbers each (kv4_attention.h): 22 bits.
 #include "kv4_attention.h"
 
+#include <type_traits>
+
 namespace rq {
 namespace {
 
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
 // Query<D, 32> has them, and [tile][kv head] terms of its rows.
 struct TileTerms {
     float f[32], shift[32], lse[32];              // f as in RowTerms, f times the sum of the row's elements, -lse
-    int at[32];                                   // the row's query among its sequence's
+    int at[32];                                   // the row's query among its sequence's; the last one where there is no row
 };
 template <int D>
 constexpr int kTileBytes = 32 * D * 4;
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_weights_rows(KvJob job) {
         terms->f[lane] = q.f;
         terms->shift[lane] = q.f * (q.even + q.odd);
         terms->lse[lane] = there ? -lse * kLog2e : -INFINITY;
-        terms->at[lane] = token;
+        terms->at[lane] = there ? token : at.nq - 1;
     }
 }
 
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, 
         u32x4 q[2 * S * 64];
         TileTerms terms;
     };
-    __shared__ __attribute__((aligned(16))) Staged staged[2];
+    __shared__ __attribute__((aligned(16))) Staged staged[3];        // the tile being multiplied, the one whose terms are in use, the next
     static_assert(sizeof(TileTerms) == 16 * 32, "half a wave brings the terms");
     const Kv4Attention& a = job.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -231,8 +233,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, 
     const int per = job.chunks * job.workers, item = item_number(), seq = item / per, rest = item - seq * per, chunk = rest / job.workers, share = rest - chunk * job.workers;
     const int head = blockIdx.x;
     if (seq >= a.batch) return;
-    const int len = own_len(job, seq), first_key = chunk * (kWaves * kTile);
-    if (first_key >= len) return;
+    const int first_key = chunk * (kWaves * kTile), k0 = first_key + wave * kTile;
+    const int head_at = head * ((D + 8) << job.cache.page_shift);
+    // (asked for before the length is known)
+    const int pages = load_pages<PAGED>(job.cache, a.table + (int64_t)seq * a.width, a.width, k0, kTile, lane);
+    const int len = own_len(job, seq);
     int q0 = seq, nq = 1;
     if (a.q_start) {
         q0 = a.q_start[seq];
@@ -241,6 +246,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, 
         q1 = q1 < q0 ? q0 : q1 > a.tokens ? a.tokens : q1;
         nq = q1 - q0;
     }
+    if (first_key >= len) return;
     const int first_pos = len - nq;               // of the sequence's first query
     const int first_tile = a.q_start ? (int)((int64_t)q0 * job.group / 32) + seq : seq * ((job.group + 31) / 32);
     // queries that see some of the workgroup's keys: those from the first key on, if causal, and before the window has passed the last
@@ -254,27 +260,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, 
         t0 += share * each;
         t1 = t1 < t0 + each ? t1 : t0 + each;
     }
-    const int k0 = first_key + wave * kTile;
-    const int head_at = head * ((D + 8) << job.cache.page_shift);
     // the wave's keys: lane n of a block of 32 has the half-row `half` of key n
     f16x8 keys[2][S];
     float step[2], mid[2], sum[2] = {};
-    u32x4 next[N];
-    const auto bring = [&](int tile) {
-        const u32x4* x = reinterpret_cast<const u32x4*>(tile_at<D>(job, first_tile + tile, head));
+    // the row tile under way (the last one again at the end: where a load may be left out, all before it is waited for)
+    u32x4 brought[N], brought_terms;
+    const auto bring = [&](int tile) __attribute__((always_inline)) {
+        const u32x4* x = reinterpret_cast<const u32x4*>(tile_at<D>(job, first_tile + (tile < t1 ? tile : t1 - 1), head));
 #pragma unroll
-        for (int i = 0; i < N; ++i) next[i] = x[threadIdx.x + 64 * kWaves * i];
+        for (int i = 0; i < N; ++i) brought[i] = x[threadIdx.x + 64 * kWaves * i];
+        brought_terms = x[2 * S * 64 + (threadIdx.x & 31)];
     };
-    const auto bring_terms = [&](int tile) { return reinterpret_cast<const u32x4*>(tile_at<D>(job, first_tile + tile, head) + kTileBytes<D>)[threadIdx.x & 31]; };
-    u32x4 next_terms{};
-    if (t0 < t1) {
-        bring(t0);
-        next_terms = bring_terms(t0);
-    }
+    const auto put = [&](Staged& to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) to.q[threadIdx.x + 64 * kWaves * i] = brought[i];
+        reinterpret_cast<u32x4*>(&to.terms)[threadIdx.x & 31] = brought_terms;   // (eight threads the same: no branch, behind which all loads were waited for)
+    };
+    if (t0 < t1) bring(t0);
     {
         const CodeBits bits;
-        const int32_t* table = a.table + (int64_t)seq * a.width;
-        const int pages = load_pages<PAGED>(job.cache, table, a.width, k0, kTile, lane);
         uint32_t raw[2][S], kp[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -306,56 +310,112 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, 
             mid[i] = __uint_as_float(kp[i] & 0xffff0000u);
         }
     }
-    int turn = 0;
-    for (int tile = t0; tile < t1; ++tile) {
-        Staged& now = staged[turn];
-        turn ^= 1;
+    // what four rows (e: of the lane's sixteen) need besides their products; MASKED: and where they stand
+    struct Four {
+        f32x4 f, shift, lse;
+        u32x4 at;
+    };
+    const auto terms_of = [&](const Staged& of, int e, auto masked) __attribute__((always_inline)) {
+        const int row = 2 * e + 4 * half;
+        const auto four = [&](const void* x) { return reinterpret_cast<const u32x4*>(x)[row / 4]; };
+        Four t{__builtin_bit_cast(f32x4, four(of.terms.f)), __builtin_bit_cast(f32x4, four(of.terms.shift)), __builtin_bit_cast(f32x4, four(of.terms.lse)), u32x4{}};
+        if constexpr (masked) t.at = four(of.terms.at);
+        return t;
+    };
+    // Their weights for both blocks; MASKED: of keys that they see.  The key at place i of the sequence is seen by queries i - first_pos and on, if
+    // causal, and by no later one than i - first_pos + window - 1.
+    // (`most` queries from `sees` on; not causal: from 2^30 before that on)
+    uint32_t sees[2];
 #pragma unroll
-        for (int i = 0; i < N; ++i) now.q[threadIdx.x + 64 * kWaves * i] = next[i];
-        if (threadIdx.x < 32) reinterpret_cast<u32x4*>(&now.terms)[threadIdx.x] = next_terms;
-        // (one barrier a tile: the other part of LDS was read before the last one)
-        __syncthreads();
-        if (tile + 1 < t1) {
-            bring(tile + 1);
-            next_terms = bring_terms(tile + 1);
-        }
-        f32x16 s[2] = {};
+    for (int i = 0; i < 2; ++i) sees[i] = a.causal || a.window ? (uint32_t)(k0 + 32 * i + (lane & 31) - first_pos) - (a.causal ? 0u : 1u << 30) : 0u;
+    const uint32_t most = !a.window ? 0x7fffffffu : (uint32_t)a.window + (a.causal ? 0u : 1u << 30);
+    const auto weigh = [&](f32x16 (&s)[2], const Four& t, int e, auto masked) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < S; ++j) {
-            const f16x8 hi = __builtin_bit_cast(f16x8, now.q[(2 * j) * 64 + lane]), lo = __builtin_bit_cast(f16x8, now.q[(2 * j + 1) * 64 + lane]);
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, keys[i][j], s[i], 0, 0, 0);
+            for (int i = 0; i < 2; ++i) {
+                float x = fmaf(step[i], t.f[u] * s[i][e + u], fmaf(mid[i], t.shift[u], t.lse[u]));
+                if constexpr (masked) x = t.at[u] - sees[i] < most ? x : -INFINITY;
+                sum[i] += __builtin_amdgcn_exp2f(x);
+            }
+    };
+    f16x8 q[2][4];
+    const auto read = [&](const Staged& of, int g) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, keys[i][j], s[i], 0, 0, 0);
-        }
-        // what all rows of the tile see: from the last one's window on to the first one's position
-        const int q_first = tile * 32 / job.group, q_last = (tile * 32 + 31) / job.group < nq ? (tile * 32 + 31) / job.group : nq - 1;
-        const bool whole = (!a.causal || k0 + kTile - 1 <= first_pos + q_first) && (!a.window || k0 > first_pos + q_last - a.window);
+        for (int i = 0; i < 4; ++i) q[g % 2][i] = __builtin_bit_cast(f16x8, of.q[(4 * g + i) * 64 + lane]);
+    };
+    const auto multiply = [&](f32x16 (&s)[2], int g) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const int row = 2 * e + 4 * half;
-            const f32x4 f = *reinterpret_cast<const f32x4*>(&now.terms.f[row]), shift = *reinterpret_cast<const f32x4*>(&now.terms.shift[row]),
-                        lse = *reinterpret_cast<const f32x4*>(&now.terms.lse[row]);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int part = 0; part < 2; ++part)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) s[i][e + u] = fmaf(step[i], f[u] * s[i][e + u], fmaf(mid[i], shift[u], lse[u]));
-            if (!whole) {
+                for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(q[g % 2][2 * j + part], keys[i][2 * g + j], s[i], 0, 0, 0);
+    };
+    // A row tile's products, and beside them the weights of the one before it; the next tile goes into LDS, the one after it is asked for.
+    // (Operands are read a group of products ahead; nothing moves from group to group.)
+    constexpr int G = S / 2;
+    Staged *last = &staged[2], *now = &staged[0], *then = &staged[1];
+    bool whole = true;                            // all rows of the tile before see all of the wave's keys
+    const auto take = [&](int tile, f32x16 (&s)[2], f32x16 (&before)[2]) __attribute__((always_inline)) {
+        put(*then);
+        bring(tile + 2);
+        read(*now, 0);
+        const int first_at = __builtin_amdgcn_readfirstlane(now->terms.at[0]), last_at = __builtin_amdgcn_readfirstlane(now->terms.at[31]);
+        s[0] = s[1] = f32x16{};
+        const auto both = [&](auto masked) __attribute__((always_inline)) {
+            constexpr int E = 4 / G;              // fours of rows beside a group
+            constexpr int P = masked ? 1 : 2;     // (masked: registers are too few for the next group's)
+            Four t[P][E];
+            const auto read_terms = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int pos = first_pos + now.terms.at[row + u];
+                for (int e = 0; e < E; ++e) t[g % P][e] = terms_of(*last, 4 * (E * g + e), masked);
+            };
+            if (P == 2) read_terms(0);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int key = k0 + 32 * i + (lane & 31);
-                        if ((a.causal && key > pos) || (a.window && key <= pos - a.window)) s[i][e + u] = -INFINITY;
-                    }
+            for (int g = 0; g < G; ++g) {
+                RQ_FENCE();
+                if (P == 1) read_terms(g);
+                if (g + 1 < G) read(*now, g + 1);
+                if (P == 2 && g + 1 < G) read_terms(g + 1);
+                multiply(s, g);
+#pragma unroll
+                for (int e = 0; e < E; ++e) weigh(before, t[g % P][e], 4 * (E * g + e), masked);
+                if (g + 1 < G) RQ_NEXT(kLdsRead, 4 + (P == 1 ? 4 : 3) * E);
+                else if (P == 1) RQ_NEXT(kLdsRead, 4 * E);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    RQ_NEXT(kMfma, 1);
+                    RQ_NEXT(kValu, (masked ? 8 : 5) * E);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) sum[i] += __builtin_amdgcn_exp2f(s[i][e + u]);
+            RQ_FENCE();
+        };
+        if (whole) both(std::false_type{});
+        else both(std::true_type{});
+        // (from the last one's window on to the first one's position)
+        whole = (!a.causal || k0 + kTile - 1 <= first_pos + first_at) && (!a.window || k0 > first_pos + last_at - a.window);
+        Staged* free = last;
+        last = now;
+        now = then;
+        then = free;
+        lds_barrier();                            // (one a tile: what goes into LDS next takes the place of terms that were read before it)
+    };
+    if (t0 < t1) {
+        f32x16 even[2], odd[2];
+        odd[0] = odd[1] = f32x16{};               // before the first tile: rows of no weight
+        last->terms.f[lane & 31] = last->terms.shift[lane & 31] = 0.0f;
+        last->terms.lse[lane & 31] = -INFINITY;
+        put(*now);
+        bring(t0 + 1);
+        lds_barrier();
+        for (int tile = t0; tile < t1; tile += 2) {
+            take(tile, even, odd);
+            take(tile + 1, odd, even);            // (where there is no such tile, the last one again, whose weights are not taken)
         }
+        if ((t1 - t0) % 2 == 0)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) weigh(odd, terms_of(*last, e, std::true_type{}), e, std::true_type{});
     }
     float x, y;
     other_rows(sum[0], true, x, y);
@@ -402,9 +462,19 @@ Plan plan(const Kv4& c, const Kv4Attention& a, int num_cu) {
     Plan p{};
     p.tiles = (int)(a.q_start ? rows / 32 + a.batch : (int64_t)a.batch * ((group + 31) / 32));
     p.chunks = (int)((a.max_len + kWaves * kTile - 1) / (kWaves * kTile));
-    const int64_t wgs = (int64_t)a.batch * c.kv_heads * p.chunks, want = (2 * (int64_t)num_cu + wgs - 1) / wgs, most = (rows / 32 / a.batch + 3) / 4;
-    p.shares = (int)(want < most ? want : most);
-    if (p.shares < 1) p.shares = 1;
+    // Shares of a workgroup's rows, by what they cost in row tiles: two workgroups a compute unit, each as long as its row tiles and two more;
+    // what all of them take together, and one of them, which is what the last ones take (causal masks and windows make them unlike);
+    // adding the shares up, a launch more, four.  Two prompts of 5003, window 1024, 14 heads to 2: 20 or 30 shares 65 us, 7: 74; 64 queries
+    // against 16384 positions: one share 25, two 29.
+    const int64_t wgs = (int64_t)a.batch * c.kv_heads * p.chunks, seen = a.window ? ((int64_t)a.window + kWaves * kTile) * group / 32 + 1 : INT64_MAX;
+    const int64_t mean = rows / 32 / a.batch + 1, tiles = mean < seen ? mean : seen;
+    double least = 0.0;
+    for (int n = 1; n <= 64 && n <= tiles; ++n) {
+        const double one = (double)((tiles + n - 1) / n + 2), cost = one * (double)(wgs * n) / (2.0 * num_cu) + one + (n > 1 ? 4.0 : 0.0);
+        if (n > 1 && cost >= least) continue;
+        least = cost;
+        p.shares = n;
+    }
     p.rows_bytes = (size_t)p.tiles * c.kv_heads * (32 * c.head_dim * 4 + sizeof(TileTerms));
     p.bytes = p.rows_bytes + (p.shares > 1 ? (size_t)p.shares * a.batch * c.kv_heads * a.max_len * sizeof(float) : 0);
     return p;

@@ -238,6 +238,18 @@ __device__ __forceinline__ void store_row(uint16_t* o, const float (&y)[N], bool
     }
 }
 
+// Nothing moves over RQ_FENCE; RQ_NEXT: of what stands between two of them, n of a kind come next.
+constexpr int kValu = 0x2, kMfma = 0x8, kLdsRead = 0x100;
+#define RQ_FENCE() __builtin_amdgcn_sched_barrier(0)
+#define RQ_NEXT(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
+
+// A barrier for what lies in LDS: loads from memory stay under way.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
 // The pages of tiles of 64 keys, read 64 at once, so that no step waits for the table before it can ask for codes.  PAGED: pages of

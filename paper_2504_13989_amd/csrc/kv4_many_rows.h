@@ -240,10 +240,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // Operands come from LDS a group of products ahead of their use.  The compiler would rather read each right before its product, in
 // few registers, and wait for LDS every time: nothing moves over RQ_FENCE, and in a group the reads come first, then products
-// with vector instructions between them.
-constexpr int kValu = 0x2, kMfma = 0x8, kLdsRead = 0x100;
-#define RQ_FENCE() __builtin_amdgcn_sched_barrier(0)
-#define RQ_NEXT(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
+// with vector instructions between them (RQ_NEXT).
 
 // Scores of a tile: products of 32 keys each with the wave's queries, before steps and centres; beside them the next tile is unpacked.
 template <int D, int WAVES, int N, bool EXACT>
@@ -404,13 +401,6 @@ __device__ __forceinline__ void take_scores(Sums<D, EXACT>& r, f32x16 (&s)[2], c
         }
     }
     RQ_FENCE();
-}
-
-// A barrier for what lies in LDS: loads from memory stay under way.
-__device__ __forceinline__ void lds_barrier() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // What a wave of the second group hands to its counterpart of the first, a lane's words side by side.
