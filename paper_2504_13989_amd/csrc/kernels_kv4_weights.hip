@@ -3,9 +3,8 @@
 //
 // Products are queries x keys: a key is a column, column n the lanes n, n + 16, n + 32, n + 48, of which lane g has rows 4 g + 0 .. 3.  A
 // key's step and centre and its sum stay in its lanes, and the sum over a tile's rows is three additions.
-//   - Codes become fp16 numbers c - 8, exactly (mantissas of 1024 and 64, less 1032 and 72); the half that is missing is the sum of the
-//     row's elements, which the accumulator starts from.  (The 1024 could be taken off there too, as attention does, but sums that
-//     carry it are good to 2^-12, and weights are 32 bits.)
+//   - Codes are exact operands: c - 8 for few rows, whose half the accumulator starts from, half the sum of the row's elements; c - 7.5 for
+//     many.  (Attention has 1024 + c, and takes the 1024 off the sums: they are good to 2^-12 then, and weights are 32 bits.)
 //   - Queries are two fp16 numbers each (kv4_attention.h): 22 bits.
 #include "kv4_attention.h"
 
@@ -17,13 +16,14 @@ namespace {
 constexpr int kWaves = 4;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// A tile's key codes and parameters (of key 16 i + lane % 16).
-template <int D>
+// A tile's key codes and parameters (of key 16 i + lane % 16; F == 4: of key `lane`), and the weight of the key that the lane writes.
+template <int D, int F>
 struct KeyCodes {
-    uint32_t k[4][D / 32], kp[4];
+    float old;
+    uint32_t k[4][D / 32], kp[F == 4 ? 1 : 4];
 };
-template <int D, bool PAGED>
-__device__ __forceinline__ void load_keys(KeyCodes<D>& t, const Kv4& c, int pages, int n, int head_at, int k0, int lane) {
+template <int D, int F, bool PAGED>
+__device__ __forceinline__ void load_keys(KeyCodes<D, F>& t, const Kv4& c, int pages, int n, int head_at, int k0, int lane) {
     typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -32,11 +32,29 @@ __device__ __forceinline__ void load_keys(KeyCodes<D>& t, const Kv4& c, int page
         const words x = __builtin_nontemporal_load(reinterpret_cast<const words*>(block + at * (D / 2) + (uint32_t)((lane & 15) * (D / 2) + (lane >> 4) * (D / 8))));
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) t.k[i][j] = x[j];
-        t.kp[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + ((D << c.page_shift) + 4 * at) + (uint32_t)(4 * (lane & 15))));
+        if constexpr (F != 4) t.kp[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + ((D << c.page_shift) + 4 * at) + (uint32_t)(4 * (lane & 15))));
+    }
+    if constexpr (F == 4) {
+        const uint8_t* w;
+        if constexpr (PAGED) {
+            const int mine = lane >> 4;
+            const uint8_t* block = nullptr;
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                block = mine == i ? block_of<PAGED>(c, pages, n, i, head_at) : block;
+                at = mine == i ? place_of(c, k0, i) : at;
+            }
+            w = block + (uint32_t)((D << c.page_shift) + 4 * (at + (lane & 15)));
+        } else {
+            w = block_of<PAGED>(c, pages, n, 0, head_at) + ((D << c.page_shift) + 4 * place_of(c, k0, 0)) + (uint32_t)(4 * lane);
+        }
+        t.kp[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(w));
     }
 }
 
-// Eight codes less 8, in the order (0, 4), (1, 5), (2, 6), (3, 7).
+// Eight codes less 8, in the order (0, 4), (1, 5), (2, 6), (3, 7).  (A code's bits by themselves are an fp16 number below the normal ones, c 2^-24,
+// four instructions fewer a dword: right, but the matrix cores then keep some bits less of the sums, 1e-5 of a weight.)
 __device__ __forceinline__ f16x8 key_operand(uint32_t w, const CodeBits& bits) {
     const f16x2 low{(_Float16)-1032.0f, (_Float16)-1032.0f}, high{(_Float16)-72.0f, (_Float16)-72.0f};
     const uint32_t h = w >> 8;
@@ -44,7 +62,7 @@ __device__ __forceinline__ f16x8 key_operand(uint32_t w, const CodeBits& bits) {
     return __builtin_bit_cast(f16x8, u32x4{f(bits.low(w), low), f(bits.high(w), high), f(bits.low(h), low), f(bits.high(h), high)});
 }
 
-// The same less 7.5, which costs two shifts more.
+// Eight codes less 7.5.
 __device__ __forceinline__ f16x8 key_codes(uint32_t w, const CodeBits& bits) {
     const f16x2 less{(_Float16)-71.5f, (_Float16)-71.5f};
     const auto f = [&](uint32_t x) { return __builtin_bit_cast(uint32_t, as_f16(bits.high(x)) + less); };
@@ -87,11 +105,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
     constexpr int stride = kWaves * kTile;
     int k0 = begin + wave * kTile;
     if (k0 >= end) return;
+    const int lo = a.window && len > a.window ? len - a.window : 0;          // the first position that the query sees: it stands at the last
+    float* weights = out.weights + seq * out.w_seq + head * out.w_head;
+    const int of_lane = F == 2 ? 16 * (2 * (g & 1) + copy) + (lane & 15) : lane;            // of a tile's keys, the one that the lane writes
+    // keys before the window: the weights decay
+    for (; k0 + kTile <= lo; k0 += stride) {
+        if (k0 >= end) return;
+        if (out.decay != 1.0f && k0 + of_lane < end) weights[k0 + of_lane] = out.decay == 0.0f ? 0.0f : out.decay * weights[k0 + of_lane];
+    }
+    if (k0 >= end) return;
     const CodeBits bits;
     const int32_t* table = a.table + (int64_t)seq * a.width;
     int pages = load_pages<PAGED>(job.cache, table, a.width, k0, stride, lane), number_of = 0;
-    KeyCodes<D> t;
-    load_keys<D, PAGED>(t, job.cache, pages, 0, head_at, k0, lane);
+    // Weights of a tile, those behind the end out of range: loads and stores without a branch, after which all that is under way would be waited
+    // for (16 sequences x 32 heads x 8192: 62.5 us with one).  The old ones first: what may not be asked for comes before what is.
+    const auto weights_of = [&](int k0) { return __builtin_amdgcn_make_buffer_rsrc(weights + k0, 0, 4 * (end - k0 < kTile ? end - k0 : kTile), 0x00020000); };
+    const auto load = [&](KeyCodes<D, F>& t, int k0) {
+        if (out.decay != 0.0f) t.old = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(weights_of(k0), 4 * of_lane, 0, 2));
+        load_keys<D, F, PAGED>(t, job.cache, pages, number_of, head_at, k0, lane);
+    };
+    KeyCodes<D, F> even, odd;
+    load(even, k0);
     Query<D, 16> q;
     Rows r;
     const int n = (lane & 15) % C;
@@ -103,27 +137,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
         take_query<D, 16, F16, true>(q, job, raw, lane);
         spread(r, RowTerms{q.f, q.even + q.odd, there ? lse * kLog2e : INFINITY}, lane);
     }
-    const int lo = a.window && len > a.window ? len - a.window : 0;          // the first position that the query sees: it stands at the last
-    for (; k0 < end; k0 += stride) {
-        KeyCodes<D> next;
-        if (k0 + stride < end) {
+    f32x4 start;                                  // the accumulator's first value
+#pragma unroll
+    for (int e = 0; e < 4; ++e) start[e] = 0.5f * r.sum[e];
+    // The tile `t`, and the next one asked for.
+    const auto take = [&](KeyCodes<D, F>& t, KeyCodes<D, F>& next, auto more) __attribute__((always_inline)) {
+        if constexpr (more) {
             if (++number_of == kPagesOf<PAGED>) {
                 pages = load_pages<PAGED>(job.cache, table, a.width, k0 + stride, stride, lane);
                 number_of = 0;
             }
-            load_keys<D, PAGED>(next, job.cache, pages, number_of, head_at, k0 + stride, lane);
+            load(next, k0 + stride);
+            RQ_FENCE();                           // (the compiler would ask for them behind half of this tile's work)
         }
         float sums[4 / F] = {};
 #pragma unroll
         for (int u = 0; u < 4 / F; ++u) {
             f32x4 s{};
-            float step = 0.0f, mid = 0.0f;
+            uint32_t p = t.kp[0];
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const int i = u * F + f;
-                f32x4 acc;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = 0.5f * r.sum[e];
+                f32x4 acc = start;
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) {
                     const f16x8 b = key_operand(t.k[i][j], bits);
@@ -133,9 +168,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
                 const bool mine = F == 1 || copy == f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[e] = mine ? acc[e] : s[e];
-                step = mine ? __uint_as_float(t.kp[i] << 16) : step;
-                mid = mine ? __uint_as_float(t.kp[i] & 0xffff0000u) : mid;
+                if constexpr (F != 4) p = mine ? t.kp[i] : p;
             }
+            const float step = __uint_as_float(p << 16), mid = __uint_as_float(p & 0xffff0000u);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float x = fmaf(step, r.f[e] * s[e], fmaf(mid, r.f[e] * r.sum[e], -r.lse[e]));
@@ -155,20 +190,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4We
                 other_rows(x, true, x, b);
                 x += b;
             }
-            // lane g writes keys 16 g ...
-            if constexpr (F == 1) total = g == u ? x : total;
-            else if constexpr (F == 2) {          // block 2 u + copy, in lanes 2 copy, 2 copy + 1
-                total = (g & 1) == u ? x : total;
-            } else total = x;
+            // (F == 2: block 2 u + copy, in lanes 2 copy, 2 copy + 1)
+            total = F == 4 || (F == 2 ? (g & 1) == u : g == u) ? x : total;
         }
-        const int block = F == 2 ? 2 * (g & 1) + copy : g;
-        const int key = k0 + 16 * block + (lane & 15);
-        if (key < end) {
-            float* w = out.weights + seq * out.w_seq + head * out.w_head + key;
-            const float seen = key >= lo ? total : 0.0f;
-            *w = out.decay == 0.0f ? seen : fmaf(out.decay, *w, seen);
+        total = k0 + of_lane >= lo ? total : 0.0f;
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(out.decay == 0.0f ? total : fmaf(out.decay, t.old, total)), weights_of(k0), 4 * of_lane, 0, 2);
+        k0 += stride;
+    };
+    while (true) {
+        if (k0 + stride >= end) {
+            take(even, odd, std::false_type{});
+            return;
         }
-        t = next;
+        take(even, odd, std::true_type{});
+        if (k0 + stride >= end) {
+            take(odd, even, std::false_type{});
+            return;
+        }
+        take(odd, even, std::true_type{});
     }
 }
 
