@@ -1,7 +1,9 @@
 // Which positions of a cached sequence are kept, and the kept rows moved together (kv4_layout.h).
 //
-// select: a row of weights is held in registers by one workgroup, as integers in the order of the numbers; the k-th largest is found
-// bit by bit, a count over the row each, until as many are at or above the threshold as are wanted.
+// select: a workgroup takes a row of weights, as integers in the order of the numbers, in registers up to 32768 of them.  The k-th largest is found
+// in up to four passes of eight bits: how many there are of each digit among those whose bits before it are the ones found so far, until
+// all that are left of a digit are wanted.  Weights crowd in a few digits, so each has sixteen counters, one for every fourth lane of a
+// wave (2048 of one counter each: bound by lanes that wait for each other's additions, 4096 rows of 8192 in 101 us).
 // evict: codes and parameters move as they are, nothing is quantized again.
 #include "kv4_layout.h"
 #include "wave_common.h"
@@ -9,7 +11,8 @@
 namespace rq {
 namespace {
 
-// Numbers as integers of the same order: -infinity .. infinity above NaN, which is 1, and 0 is none of them.  Both zeros are one.
+// Numbers as integers of the same order: -infinity .. infinity (0xff800000) above NaN, which is 1; 0 is none of them, and 0xffffffff what is kept in any
+// case.  Both zeros are one.
 __device__ __forceinline__ uint32_t ordered(float x) {
     uint32_t u = __float_as_uint(x);
     if ((u << 1) > 0xff000000u) return 1u;
@@ -21,185 +24,198 @@ __device__ __forceinline__ int below(uint64_t mask) {                // set bits
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
+constexpr int kPasses = 4, kCopies = 16;
+struct Digits {
+    uint32_t count[2][256 * kCopies];             // [digit][copy]; passes in turn
+    uint32_t found[kPasses][4];                   // the threshold's digit, how many are above it, how many have it
+};
+
+// Sums over the lanes up to this one.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true); }
+__device__ __forceinline__ int wave_prefix(int x) {
+    x = plus_dpp<0x118, 0xf>(plus_dpp<0x114, 0xf>(plus_dpp<0x112, 0xf>(plus_dpp<0x111, 0xf>(x))));   // row_shr:1, 2, 4, 8
+    return plus_dpp<0x143, 0xc>(plus_dpp<0x142, 0xa>(x));            // row_bcast:15, 31
+}
+
+// What is taken of a row: keys >= `least`, and of those that are least - 1 the first `ties`.
+struct Threshold {
+    uint32_t least;
+    int ties;
+};
+// The `want` (at least 1) largest of more keys.  each(f): f(key) for the thread's keys, 0 where there is none.
+template <int W, typename EACH>
+__device__ __forceinline__ Threshold find_threshold(Digits& d, int want, EACH each) {
+    const int lane = threadIdx.x & 63;
+    const auto clear = [&](uint32_t* count) {
+        for (int i = threadIdx.x; i < 256 * kCopies / 4; i += 64 * W) reinterpret_cast<u32x4*>(count)[i] = u32x4{0, 0, 0, 0};
+    };
+    clear(d.count[0]);
+    __syncthreads();
+    uint32_t found = 0;                           // the bits of the threshold so far
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+        const int shift = 24 - 8 * pass;
+        uint32_t* count = d.count[pass % 2];
+        each([&](uint32_t key) {
+            if (pass == 0 || (key >> (shift + 8)) == found) atomicAdd(&count[(key >> shift & 255u) * kCopies + (lane & (kCopies - 1))], 1u);
+        });
+        if (pass + 1 < kPasses) clear(d.count[(pass + 1) % 2]);      // (read before the barrier that the last pass ended with)
+        __syncthreads();
+        if (W == 1 || threadIdx.x < 64) {         // a wave's work, and the others' meanwhile would be the same
+            // from the largest digit down, four a lane: 64 counters, from another one on in each lane, so that lanes use all banks
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const u32x4 x = reinterpret_cast<const u32x4*>(count)[(63 - lane) * 16 + ((i + lane) & 15)];
+                sum += (int)(x[0] + x[1] + x[2] + x[3]);
+            }
+            int upto = wave_prefix(sum);
+            const int at = __builtin_ctzll(__ballot(upto >= want));  // (there are as many)
+            const int before = __builtin_amdgcn_readlane(upto - sum, at);
+            // its four digits, sixteen lanes each, the largest first
+            const int mine = (int)count[(63 - at) * 64 + (63 - lane)];
+            upto = wave_prefix(mine);
+            const int s0 = __builtin_amdgcn_readlane(upto, 15), s1 = __builtin_amdgcn_readlane(upto, 31), s2 = __builtin_amdgcn_readlane(upto, 47),
+                      s3 = __builtin_amdgcn_readlane(upto, 63), left = want - before;
+            const int i = left <= s0 ? 0 : left <= s1 ? 1 : left <= s2 ? 2 : 3;
+            const int above = i == 0 ? 0 : i == 1 ? s0 : i == 2 ? s1 : s2, to = i == 0 ? s0 : i == 1 ? s1 : i == 2 ? s2 : s3;
+            if (lane == 0) *reinterpret_cast<u32x4*>(d.found[pass]) = u32x4{(uint32_t)((63 - at) * 4 + 3 - i), (uint32_t)(before + above), (uint32_t)(to - above), 0u};
+        }
+        __syncthreads();
+        const u32x4 x = *reinterpret_cast<const u32x4*>(d.found[pass]);
+        found = (found << 8) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x[0]);
+        want -= __builtin_amdgcn_readfirstlane((int)x[1]);
+        if (want == __builtin_amdgcn_readfirstlane((int)x[2])) return Threshold{found << shift, 0};  // all of them
+    }
+    return Threshold{found + 1, want};
+}
+
+// Which row a workgroup has, and what of it is kept in any case: before lo, from hi on.
+struct SelectRow {
+    const float* w;
+    int32_t* out;
+    int len, lo, hi;
+    __device__ __forceinline__ SelectRow(const Kv4Select& a, int64_t row) {
+        const int head = (int)(row % a.kv_heads);
+        const int64_t rest = row / a.kv_heads, layer = rest / a.batch;
+        const int seq = (int)(rest - layer * a.batch);
+        w = a.weights + layer * a.w_layer + seq * a.w_seq + head * a.w_head;
+        out = a.index + row * a.keep;
+        const int n = a.kv_lens[seq];
+        len = n < 0 ? 0 : n > a.n ? a.n : n;
+        lo = a.sinks;
+        hi = len - a.recent;
+    }
+    __device__ __forceinline__ uint32_t key(int64_t j, float x) const { return j >= len ? 0u : j < lo || j >= hi ? 0xffffffffu : ordered(x); }
+    // All of a row that has no more than are kept.
+    __device__ __forceinline__ bool whole(const Kv4Select& a, int threads) const {
+        if (len > a.keep) return false;
+        for (int i = threadIdx.x; i < a.keep; i += threads) out[i] = i < len ? i : -1;
+        return true;
+    }
+};
+
 // A row of at most 64 W R weights.  Wave w has the R * 64 from 64 R w on, lane by lane.
 template <int W, int R>
 __global__ __launch_bounds__(64 * W) void k_kv4_select(Kv4Select a, int64_t rows) {
-    __shared__ int counts[2][W], eq_counts[W];
+    __shared__ __attribute__((aligned(16))) Digits digits;
+    __shared__ int taken_of[W], equal_of[W];
     const int64_t row = group_index();
     if (row >= rows) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = (int)(row % a.kv_heads);
-    const int64_t rest = row / a.kv_heads, layer = rest / a.batch;
-    const int seq = (int)(rest - layer * a.batch);
-    const float* w = a.weights + layer * a.w_layer + seq * a.w_seq + head * a.w_head;
-    int32_t* out = a.index + row * a.keep;
-    int len = a.kv_lens[seq];
-    len = len < 0 ? 0 : len > a.n ? a.n : len;
-    if (len <= a.keep) {                          // all of it
-        for (int i = threadIdx.x; i < a.keep; i += 64 * W) out[i] = i < len ? i : -1;
-        return;
-    }
-    const int lo = a.sinks, hi = len - a.recent, want = a.keep - a.sinks - a.recent, first = wave * (64 * R) + lane;
+    const SelectRow at(a, row);
+    if (at.whole(a, 64 * W)) return;
+    const int len = at.len, first = wave * (64 * R) + lane;
     uint32_t key[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int j = first + 64 * r;
-        key[r] = __float_as_uint(w[j < len ? j : len - 1]);
+        key[r] = __float_as_uint(at.w[j < len ? j : len - 1]);
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) key[r] = (uint32_t)(first + 64 * r - lo) < (uint32_t)(hi - lo) ? ordered(__uint_as_float(key[r])) : 0u;
-    int turn = 0;
-    const auto count = [&](uint32_t t) {          // of keys at or above t, over the workgroup
-        int n = 0;
+    for (int r = 0; r < R; ++r) key[r] = at.key(first + 64 * r, __uint_as_float(key[r]));
+    const Threshold t = find_threshold<W>(digits, a.keep, [&](auto count) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) n += __builtin_popcountll(__ballot(key[r] >= t));
-        if constexpr (W > 1) {
-            if (lane == 0) counts[turn][wave] = n;
-            __syncthreads();
-            n = lane < W ? counts[turn][lane] : 0;
-#pragma unroll
-            for (int x = 1; x < W; x *= 2) n += __shfl_xor(n, x);
-            n = __builtin_amdgcn_readfirstlane(n);
-            turn ^= 1;
-        }
-        return n;
-    };
-    // keys >= `least` are taken, and the first `ties` that are least - 1
-    uint32_t least = 0xffffffffu;
-    int ties = 0;
-    if (want > 0) {
-        uint32_t t = 0;
-        int n = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t to = t | (1u << bit);
-            const int c = count(to);
-            if (c < want) continue;
-            t = to;
-            n = c;
-            if (c == want) break;
-        }
-        least = t;
-        if (n != want) {                          // t is the last one that is taken, some of those equal to it are not
-            least = t + 1;
-            ties = want - count(least);
-        }
-    }
-    int place = first;                            // (the compiler would keep the masks of the first pass for the second, in more registers than there are)
-    const auto is_taken = [&](int r) {
-        const int j = place + 64 * r;
-        return key[r] >= least || (j < len && (j < lo || j >= hi));
-    };
-    const auto is_equal = [&](int r) { return ties && key[r] == least - 1; };
+        for (int r = 0; r < R; ++r) count(key[r]);
+    });
     int n = 0, e = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        n += __builtin_popcountll(__ballot(is_taken(r)));
-        e += __builtin_popcountll(__ballot(is_equal(r)));
-    }
-    if constexpr (W > 1) {                        // those of the waves before
-        if (lane == 0) {
-            counts[turn][wave] = n;
-            eq_counts[wave] = e;
-        }
-        __syncthreads();
-        n = e = 0;
+    for (int r = 0; r < R; ++r) n += __builtin_popcountll(__ballot(key[r] >= t.least));
+    if (t.ties)
 #pragma unroll
-        for (int x = 0; x < W; ++x) {
-            n += x < wave ? counts[turn][x] : 0;
-            e += x < wave ? eq_counts[x] : 0;
-        }
-    } else {
-        n = e = 0;
+        for (int r = 0; r < R; ++r) e += __builtin_popcountll(__ballot(key[r] == t.least - 1));
+    if (lane == 0) {
+        taken_of[wave] = n;
+        equal_of[wave] = e;
     }
-    asm volatile("" : "+v"(place), "+s"(least));
+    __syncthreads();
+    n = e = 0;                                    // those of the waves before
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+        n += x < wave ? taken_of[x] : 0;
+        e += x < wave ? equal_of[x] : 0;
+    }
+    uint32_t least = t.least;                     // (the compiler would keep the masks of the count, in more registers than there are)
+    asm volatile("" : "+s"(least));
+    int32_t* out = at.out + n;
+    if (t.ties == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint64_t taken = __ballot(key[r] >= least);
+            if (key[r] >= least) out[below(taken)] = first + 64 * r;
+            out += __builtin_popcountll(taken);
+        }
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const bool mine = is_taken(r), tie = is_equal(r);
+        const bool mine = key[r] >= least, tie = key[r] == least - 1;
         const uint64_t taken = __ballot(mine), equal = __ballot(tie);
-        const int rank = e + below(equal);        // ties before this one
-        if (mine || (tie && rank < ties)) out[n + below(taken) + (rank < ties ? rank : ties)] = place + 64 * r;
-        n += __builtin_popcountll(taken);
+        const int rank = e + below(equal), before = rank < t.ties ? rank : t.ties;                   // ties before this one; those of them that are taken
+        if (mine || (tie && rank < t.ties)) out[below(taken) + before] = first + 64 * r;
+        out += __builtin_popcountll(taken);
         e += __builtin_popcountll(equal);
     }
 }
 
-// Rows of any length: the same, with the row read again for every count.
+// Rows of any length: the same, with the row read again for every pass.
 constexpr int kLongWaves = 16;
 __global__ __launch_bounds__(64 * kLongWaves) void k_kv4_select_long(Kv4Select a, int64_t rows) {
     constexpr int W = kLongWaves, T = 64 * W;
-    __shared__ int counts[2][W], eq_counts[2][W];
+    __shared__ __attribute__((aligned(16))) Digits digits;
+    __shared__ int taken_of[2][W], equal_of[2][W];
     const int64_t row = group_index();
     if (row >= rows) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = (int)(row % a.kv_heads);
-    const int64_t rest = row / a.kv_heads, layer = rest / a.batch;
-    const int seq = (int)(rest - layer * a.batch);
-    const float* w = a.weights + layer * a.w_layer + seq * a.w_seq + head * a.w_head;
-    int32_t* out = a.index + row * a.keep;
-    int len = a.kv_lens[seq];
-    len = len < 0 ? 0 : len > a.n ? a.n : len;
-    if (len <= a.keep) {
-        for (int i = threadIdx.x; i < a.keep; i += T) out[i] = i < len ? i : -1;
-        return;
-    }
-    const int lo = a.sinks, hi = len - a.recent, want = a.keep - a.sinks - a.recent;
-    int turn = 0;
-    const auto count = [&](uint32_t t) {
-        int n = 0;
-        for (int j = lo + (int)threadIdx.x; j < hi; j += T) n += ordered(w[j]) >= t;
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) n += __shfl_xor(n, x);
-        if (lane == 0) counts[turn][wave] = n;
-        __syncthreads();
-        n = lane < W ? counts[turn][lane] : 0;
-#pragma unroll
-        for (int x = 1; x < W; x *= 2) n += __shfl_xor(n, x);
-        turn ^= 1;
-        return __builtin_amdgcn_readfirstlane(n);
-    };
-    uint32_t least = 0xffffffffu;
-    int ties = 0;
-    if (want > 0) {
-        uint32_t t = 0;
-        int n = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t to = t | (1u << bit);
-            const int c = count(to);
-            if (c < want) continue;
-            t = to;
-            n = c;
-            if (c == want) break;
-        }
-        least = t;
-        if (n != want) {
-            least = t + 1;
-            ties = want - count(least);
-        }
-    }
-    int n = 0, e = 0;                             // written, and ties met, before the stretch in hand
-    for (int at = 0; at < len; at += T) {
-        const int j = at + (int)threadIdx.x;
-        const bool there = j < len, candidate = j >= lo && j < hi;
-        const uint32_t key = candidate ? ordered(w[j]) : 0u;
-        const uint64_t taken = __ballot(there && (!candidate || key >= least)), equal = __ballot(ties && candidate && key == least - 1);
+    const SelectRow at(a, row);
+    if (at.whole(a, T)) return;
+    const int len = at.len;
+    const Threshold t = find_threshold<W>(digits, a.keep, [&](auto count) {
+        for (int64_t j = threadIdx.x; j < len; j += T) count(at.key(j, at.w[j]));
+    });
+    int n = 0, e = 0, turn = 0;                   // written, and ties met, before the stretch in hand
+    for (int64_t from = 0; from < len; from += T, turn ^= 1) {
+        const int64_t j = from + threadIdx.x;
+        const uint32_t key = j < len ? at.key(j, at.w[j]) : 0u;
+        const bool mine = j < len && key >= t.least, tie = t.ties && j < len && key == t.least - 1;
+        const uint64_t taken = __ballot(mine), equal = __ballot(tie);
         if (lane == 0) {
-            counts[turn][wave] = __builtin_popcountll(taken);
-            eq_counts[turn][wave] = __builtin_popcountll(equal);
+            taken_of[turn][wave] = __builtin_popcountll(taken);
+            equal_of[turn][wave] = __builtin_popcountll(equal);
         }
         __syncthreads();
         int n0 = n, e0 = e;                       // ... and before this wave's part of it
 #pragma unroll
         for (int x = 0; x < W; ++x) {
-            const int cn = counts[turn][x], ce = eq_counts[turn][x];
+            const int cn = taken_of[turn][x], ce = equal_of[turn][x];
             n0 += x < wave ? cn : 0;
             e0 += x < wave ? ce : 0;
             n += cn;
             e += ce;
         }
-        const uint64_t mine = (uint64_t)1 << lane;
         const int rank = e0 + below(equal);
-        if ((taken & mine) || ((equal & mine) && rank < ties)) out[n0 + below(taken) + (rank < ties ? rank : ties)] = j;
-        turn ^= 1;
+        if (mine || (tie && rank < t.ties)) at.out[n0 + below(taken) + (rank < t.ties ? rank : t.ties)] = (int)j;
     }
 }
 
