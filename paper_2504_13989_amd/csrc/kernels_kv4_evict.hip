@@ -223,31 +223,38 @@ __global__ __launch_bounds__(64 * kLongWaves) void k_kv4_select_long(Kv4Select a
 
 constexpr int kTokens = 16;                       // of a wave: they lie in one page where they go
 
+// Where four times kTokens rows come from, a row a lane: the page (-1: there is none), the place in it.
+struct Sources {
+    int page, place;
+};
+__device__ __forceinline__ Sources find_sources(const Kv4& c, const Kv4Evict& a, const int32_t* index, const int32_t* table, int64_t i) {
+    const int at = i < a.keep ? index[i] : -1;
+    int page = at >= 0 && (at >> c.page_shift) < a.width ? table[at >> c.page_shift] : -1;
+    if (page >= c.pages) page = -1;
+    return Sources{page < 0 ? -1 : page, at & ((1 << c.page_shift) - 1)};
+}
+
 // What a wave holds of its tokens.  Keys: lane l has part l % 4 of token l / 4.  Values: fours of tokens of a run, as the layout has them.
 // Parameters: lanes 0 .. 15 keys', 16 .. 31 values'.
 template <int D>
 struct Held {
     uint32_t k[D / 32];
-    uint16_t v[D / 64][4];
+    uint32_t v[D / 64][4];
     uint32_t p;
     int from;                                     // of token `lane & 15`: its page; -1: none
 };
 
+// Tokens whose sources are those of lanes 16 n + 0 .. 15.  (Rows that are not there come from page 0, and go nowhere: no branch, behind which
+// all loads would be waited for.)
 template <int D>
-__device__ __forceinline__ void load_rows(Held<D>& t, const uint8_t* base, const Kv4& c, const Kv4Evict& a, const int32_t* index, const int32_t* table, int i0, int head_at,
-                                          int lane) {
+__device__ __forceinline__ void load_rows(Held<D>& t, const uint8_t* base, const Kv4& c, const Sources& s, int n, int head_at, int lane) {
     typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
-    const int p = 1 << c.page_shift, i = i0 + (lane & 15);
-    const int at = i < a.keep ? index[i] : -1;
-    int page = at >= 0 && (at >> c.page_shift) < a.width ? table[at >> c.page_shift] : -1;
-    if (page >= c.pages) page = -1;
-    t.from = page < 0 ? -1 : page;
-    const int place = at & (p - 1);
-    const auto block = [&](int page) { return base + (uint64_t)(uint32_t)page * (uint32_t)c.page_bytes + head_at; };
+    const int p = 1 << c.page_shift;
+    t.from = __shfl(s.page, 16 * n + (lane & 15));
+    const auto block = [&](int page) { return base + (uint64_t)(uint32_t)(page < 0 ? 0 : page) * (uint32_t)c.page_bytes + head_at; };
     {
-        const int from = __shfl(t.from, lane >> 2), in = __shfl(place, lane >> 2);
-        words x{};
-        if (from >= 0) x = *reinterpret_cast<const words*>(block(from) + in * (D / 2) + (lane & 3) * (D / 8));
+        const int from = __shfl(s.page, 16 * n + (lane >> 2)), in = __shfl(s.place, 16 * n + (lane >> 2));
+        const words x = *reinterpret_cast<const words*>(block(from) + in * (D / 2) + (lane & 3) * (D / 8));
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) t.k[j] = x[j];
     }
@@ -256,13 +263,12 @@ __device__ __forceinline__ void load_rows(Held<D>& t, const uint8_t* base, const
         const int run = lane + 64 * r, four = run / (D / 4), within = run % (D / 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int from = __shfl(t.from, 4 * four + e), in = __shfl(place, 4 * four + e);
-            t.v[r][e] = 0;
-            if (from >= 0) t.v[r][e] = *reinterpret_cast<const uint16_t*>(block(from) + p * (D / 2) + (in >> 2) * (2 * D) + within * 8 + 2 * (in & 3));
+            const int from = __shfl(s.page, 16 * n + 4 * four + e), in = __shfl(s.place, 16 * n + 4 * four + e);
+            t.v[r][e] = *reinterpret_cast<const uint16_t*>(block(from) + p * (D / 2) + (in >> 2) * (2 * D) + within * 8 + 2 * (in & 3));
         }
     }
-    t.p = 0;
-    if (lane < 32 && t.from >= 0) t.p = *reinterpret_cast<const uint32_t*>(block(t.from) + p * D + (lane >> 4) * 4 * p + 4 * place);
+    const int in = __shfl(s.place, 16 * n + (lane & 15));
+    t.p = *reinterpret_cast<const uint32_t*>(block(t.from) + p * D + (lane >> 4 & 1) * 4 * p + 4 * in);
 }
 
 template <int D>
@@ -287,11 +293,11 @@ __device__ __forceinline__ void store_rows(const Held<D>& t, uint8_t* base, cons
         }
         uint16_t* v = reinterpret_cast<uint16_t*>(block + p * (D / 2) + ((in >> 2) + four) * (2 * D) + within * 8);
         if (all) {
-            *reinterpret_cast<u32x2*>(v) = u32x2{(uint32_t)t.v[r][0] | ((uint32_t)t.v[r][1] << 16), (uint32_t)t.v[r][2] | ((uint32_t)t.v[r][3] << 16)};
+            *reinterpret_cast<u32x2*>(v) = u32x2{t.v[r][0] | (t.v[r][1] << 16), t.v[r][2] | (t.v[r][3] << 16)};
         } else {                                  // (rows that do not move leave others' bytes)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (there[e]) v[e] = t.v[r][e];
+                if (there[e]) v[e] = (uint16_t)t.v[r][e];
         }
     }
     if (lane < 32 && t.from >= 0) *reinterpret_cast<uint32_t*>(block + p * D + (lane >> 4) * 4 * p + 4 * (in + (lane & 15))) = t.p;
@@ -324,7 +330,7 @@ struct Row {
 };
 
 // In place: a workgroup a row, stretch by stretch.  A position is read by stretches up to its own, which is written once all waves have
-// read theirs; what the next one reads lies behind it.
+// read theirs; what the next one reads lies behind it, and is asked for before that.
 constexpr int kPlaceWaves = 8;
 template <int D>
 __global__ __launch_bounds__(64 * kPlaceWaves) void k_kv4_evict_in_place(Kv4 c, Kv4Evict a, int64_t rows) {
@@ -336,15 +342,40 @@ __global__ __launch_bounds__(64 * kPlaceWaves) void k_kv4_evict_in_place(Kv4 c, 
     const int32_t *index = a.index + row * a.keep, *table = a.table + (int64_t)at.seq * a.width;
     const int head_at = at.head * ((D + 8) << c.page_shift);
     uint8_t* base = c.data + at.layer * a.layer_bytes;
-    for (int i0 = 0; i0 < a.keep; i0 += S) {
+    // the wave's tokens of four stretches: a lane each
+    const auto sources = [&](int first) { return find_sources(c, a, index, table, (int64_t)first + (lane >> 4) * S + wave * kTokens + (lane & 15)); };
+    Sources from = sources(0), later = sources(4 * S);
+    int n = 0;                                    // of the stretch that is asked for next, among those of `from`
+    Held<D> even, odd;
+    const auto ask = [&](Held<D>& t, int i0) {    // stretch i0
+        if (n == 4) {
+            n = 0;
+            from = later;
+            later = sources(i0 + 4 * S);
+        }
+        load_rows<D>(t, base, c, from, n++, head_at, lane);
+    };
+    const auto move = [&](Held<D>& t, Held<D>& next, int i0) {
+        ask(next, i0 + S);
+        // what this stretch has asked for is here, and so it is in the other waves
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) asm volatile("" : "+v"(t.k[j]));
+#pragma unroll
+        for (int r = 0; r < D / 64; ++r) asm volatile("" : "+v"(t.v[r][0]), "+v"(t.v[r][1]), "+v"(t.v[r][2]), "+v"(t.v[r][3]));
+        asm volatile("" : "+v"(t.p) : : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
         const int i = i0 + wave * kTokens;
-        Held<D> t;
-        load_rows<D>(t, base, c, a, index, table, i, head_at, lane);
-        __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
-        __syncthreads();
         if (i < a.keep) {
             const int page = table[i >> c.page_shift];
             if (page >= 0 && page < c.pages) store_rows<D>(t, base, c, page, i, head_at, lane);
+        }
+    };
+    if (a.keep > 0 && c.pages > 0) {
+        ask(even, 0);
+        for (int64_t i0 = 0; i0 < a.keep; i0 += 2 * S) {
+            move(even, odd, (int)i0);
+            if (i0 + S < a.keep) move(odd, even, (int)i0 + S);
         }
     }
     if (a.weights) move_weights<64 * kPlaceWaves>(a.weights + at.layer * a.w_layer + at.seq * a.w_seq + at.head * a.w_head, index, a);
@@ -365,12 +396,12 @@ __global__ __launch_bounds__(64 * kMoveWaves) void k_kv4_evict(Kv4 c, Kv4Evict a
         return;
     }
     const int lane = threadIdx.x & 63, i = (part * kMoveWaves + (int)(threadIdx.x >> 6)) * kTokens;
-    if (i >= a.keep) return;
+    if (i >= a.keep || c.pages == 0) return;
     const int head_at = at.head * ((D + 8) << c.page_shift);
     uint8_t* base = c.data + at.layer * a.layer_bytes;
     const int page = a.new_table[(int64_t)at.seq * a.new_width + (i >> c.page_shift)];
     Held<D> t;
-    load_rows<D>(t, base, c, a, index, table, i, head_at, lane);
+    load_rows<D>(t, base, c, find_sources(c, a, index, table, i + (lane & 15)), 0, head_at, lane);
     if (page >= 0 && page < c.pages) store_rows<D>(t, base, c, page, i, head_at, lane);
 }
 
