@@ -11,9 +11,31 @@
 namespace rq {
 namespace {
 
-template <int D, int F, bool F16, bool PAGED, int W, Part PART>
-__global__ __launch_bounds__(64 * W, 2) void k_kv4_prefix(PrefixJob job) {
-    few_rows<D, F, F16, PAGED, W, false, PART>(job);
+// The kernel for few rows.  The first of a kv head's workgroups take prefixes, the others what is behind them: either fills what the other
+// leaves of the chip.
+struct SharedPart {
+    int tiles, chunk, chunks;
+};
+template <int D, int F, bool F16, bool PAGED>
+__global__ __launch_bounds__(256, 2) void k_kv4_prefix(PrefixJob job, SharedPart shared) {
+    __shared__ FewLds<D, 4> lds;
+    int none;
+    const int number = item_number(), first = shared.tiles * shared.chunks;
+    if (number >= first) {
+        few_rows<D, F, F16, PAGED, 4, false, Part::kOwn>(job, number - first, lds, none);
+        return;
+    }
+    job.tiles = shared.tiles;
+    job.chunk = shared.chunk;
+    job.chunks = shared.chunks;
+    job.part_first = 0;
+    few_rows<D, 1, F16, PAGED, 4, false, Part::kShared>(job, number, lds, none);
+}
+template <int D, int F, bool F16, bool PAGED, int W>
+__global__ __launch_bounds__(64 * W, 2) void k_kv4_prefix_separate(PrefixJob job) {
+    __shared__ FewLds<D, W> lds;
+    int none;
+    few_rows<D, F, F16, PAGED, W, false, Part::kSeparate>(job, item_number(), lds, none);
 }
 
 PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num_cu) {
@@ -23,77 +45,101 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
     const auto tiles_of = [&](int bm, int n) { return (rows + bm - 1) / bm + n - 1; };
     const auto shared_tiles = [&](int bm) { return tiles_of(bm, x.groups); };
     const auto own_tiles = [&](int bm) { return a.q_start ? tiles_of(bm, a.batch) : (int64_t)a.batch * ((group + bm - 1) / bm); };
-    const auto copies_of = [](int64_t mean) { return mean <= 4 ? 4 : mean <= 8 ? 2 : 1; };
-    // What a row tile of 64 keys costs, in those of the kernel for few rows: one of 128 of the other as much as three of 16.
-    constexpr int kManyCost = 3;
+    // What 64 keys cost a row tile of 128, in those of 16 rows.
+    const int many_cost = a.dtype == RQ_F16 && c.head_dim == 128 ? 6 : 4;
     PrefixPlan p{};
-    p.own_copies = copies_of(rows / a.batch);
+    p.own_copies = rows / a.batch <= 4 ? 4 : rows / a.batch <= 8 ? 2 : 1;
     const int64_t few = own_tiles(16 / p.own_copies), own_few = few * own_keys;
-    const int64_t shared_few = shared_tiles(16) * shared_keys, shared_many = kManyCost * shared_tiles(128) * shared_keys, own_many = kManyCost * own_tiles(128) * own_keys;
-    p.many = shared_many < shared_few && shared_few * c.kv_heads > 16 * (int64_t)num_cu;
+    const int64_t shared_few = shared_tiles(16) * shared_keys, shared_many = many_cost * shared_tiles(128) * shared_keys, own_many = many_cost * own_tiles(128) * own_keys;
+    p.many = (shared_few - shared_many) * c.kv_heads > 90 * (int64_t)num_cu;
     p.own_many = own_many < own_few && own_few * c.kv_heads > 256 * (int64_t)num_cu;
-    const int64_t together = (p.many ? shared_many : shared_few) + (p.own_many ? own_many : own_few), apart = few * shared_keys + own_few;
-    p.separate = a.window != 0 || x.max_len < kTile || (apart - together) * c.kv_heads < 16 * (int64_t)num_cu;
-    if (p.separate) {
-        p.many = p.own_many = false;
-        p.own_tiles = (int)few;
-        p.waves = few * c.kv_heads <= num_cu ? 8 : 4;
-        return p;
-    }
-    // A row tile's keys in as many chunks as cost least: rounds of workgroups that the chip holds at once, of `at_once` tiles of keys a step and
-    // kStart steps besides; partial results that are written and read again (4 TB/s, steps of 1.5 us).
+    // Chunks of as many tiles of keys as cost least, in steps of 1.5 us.  A workgroup takes `at_once` tiles a step and kStart steps besides; the
+    // chip holds per_cu * num_cu of them.  Those for many rows are all alike and take whole rounds; of those for few rows, which are of all
+    // lengths, one begins when another ends, and the last ends kTail of the longest after most have.  Partial results are written and read
+    // again at 4 TB/s.  (64 queries of 32 heads on 8 against 8192 keys: 33 us, in whole rounds 34.5; 90 queries of 7 tokens, 32 heads, 1000
+    // keys: 64 and 84; 12 of 40 tokens x 64 heads on 8, 65411 keys, many rows: 1144 and 1095.)
     constexpr int kStart = 3;
-    const auto split = [&](int64_t wgs, int64_t keys, int at_once, int64_t per_cu, int& chunk, int& chunks) {
-        const double join = 2.0 * a.tokens * a.heads * c.head_dim * sizeof(float) / 6e6;
+    constexpr double kTail = 0.25;
+    const double join = 2.0 * a.tokens * a.heads * c.head_dim * sizeof(float) / 6e6;
+    const auto chunks_of = [](int64_t keys, int64_t each) { return (keys + each - 1) / each; };
+    const auto time_of = [&](int64_t sum, int64_t longest, int64_t per_cu) {
+        const double t = (double)sum / (double)(per_cu * num_cu) + kTail * (double)longest;
+        return t > (double)longest ? t : (double)longest;
+    };
+    const auto split = [&](int64_t shared_tiles, int64_t own_tiles, int at_once, int64_t per_cu, bool many) {
+        const int64_t most = shared_tiles && (shared_keys > own_keys || !own_tiles) ? shared_keys : own_keys;
         double least = 0.0;
-        for (int64_t n = 1; n <= 256 && (n == 1 || n * at_once <= keys); ++n) {
-            const int64_t each = (keys + n - 1) / n, real = (keys + each - 1) / each;
-            const double cost = (double)((wgs * real + per_cu * num_cu - 1) / (per_cu * num_cu)) * (double)((each + at_once - 1) / at_once + kStart) + join * (double)real;
+        int64_t best = most;
+        for (int64_t n = 1; n <= 256 && (n == 1 || n * at_once <= most); ++n) {
+            const int64_t each = chunks_of(most, n), shared_n = shared_tiles ? chunks_of(shared_keys, each) : 0, own_n = own_tiles ? chunks_of(own_keys, each) : 0;
+            const auto steps = [&](int64_t keys) { return chunks_of(each < keys ? each : keys, at_once) + kStart; };
+            const int64_t sum = (shared_tiles * shared_n * steps(shared_keys) + own_tiles * own_n * steps(own_keys)) * c.kv_heads;
+            const double cost = (many ? (double)(chunks_of(sum / steps(most), per_cu * num_cu) * steps(most)) : time_of(sum, steps(most), per_cu)) + join * (double)(shared_n + own_n);
             if (n > 1 && cost >= least) continue;
             least = cost;
-            chunk = (int)(each * kTile);
-            chunks = (int)real;
+            best = each;
         }
+        if (shared_tiles) {
+            p.shared_chunk = (int)(best * kTile);
+            p.shared_chunks = (int)chunks_of(shared_keys, best);
+        }
+        if (own_tiles) {
+            p.own_chunk = (int)(best * kTile);
+            p.own_chunks = (int)chunks_of(own_keys, best);
+        }
+        return least;
     };
-    if (p.many) {
-        p.shared_tiles = (int)shared_tiles(128);
-        p.groups = a.dtype != RQ_F16 || c.head_dim == 64 ? 2 : 1;
-        split((int64_t)p.shared_tiles * c.kv_heads, shared_keys, p.groups, p.groups == 2 ? 1 : 2, p.shared_chunk, p.shared_chunks);
-    } else {
-        const int64_t mean = rows / x.groups;
-        p.shared_copies = copies_of(mean);
-        p.shared_tiles = (int)shared_tiles(16 / p.shared_copies);
-        split((int64_t)p.shared_tiles * c.kv_heads, shared_keys, 4, 2, p.shared_chunk, p.shared_chunks);
-    }
+    p.groups = a.dtype != RQ_F16 || c.head_dim == 64 ? 2 : 1;
+    p.shared_tiles = (int)shared_tiles(p.many ? 128 : 16);
     p.own_tiles = (int)(p.own_many ? own_tiles(128) : few);
-    split((int64_t)p.own_tiles * c.kv_heads, own_keys, 4, 2, p.own_chunk, p.own_chunks);
+    if (p.many) split(p.shared_tiles, 0, p.groups, p.groups == 2 ? 1 : 2, true);
+    const double together = split(p.many ? 0 : p.shared_tiles, p.own_many ? 0 : p.own_tiles, 4, 2, false);
+    if (p.own_many) split(0, p.own_tiles, 1, 2, true);
+    // One launch takes every sequence by itself where the chip has that done before the prefixes' reuse pays for joining, kJoin steps.
+    constexpr double kJoin = 2.5;
+    const int waves = few * c.kv_heads <= num_cu ? 8 : 4;
+    const int64_t each = chunks_of(shared_keys, waves) + chunks_of(own_keys, waves) + kStart;
+    const double apart = time_of(few * c.kv_heads * each, each, waves == 8 ? 1 : 2);
+    if (a.window != 0 || x.max_len < kTile || (!p.many && !p.own_many && apart <= together + kJoin)) {
+        const int copies = p.own_copies;
+        p = PrefixPlan{};
+        p.separate = true;
+        p.own_copies = copies;
+        p.own_tiles = (int)few;
+        p.waves = waves;
+        return p;
+    }
     p.bytes = (size_t)(p.shared_chunks + p.own_chunks) * a.tokens * a.heads * (c.head_dim + 1) * sizeof(float);
     return p;
 }
 
 template <int D, int F, bool F16, bool PAGED>
-void launch_few(const PrefixJob& job, Part part, int waves, hipStream_t s) {
-    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.tiles * (part == Part::kSeparate ? 1 : job.chunks)), block(64 * waves);
-    if (part == Part::kShared) launch_kernel(k_kv4_prefix<D, F, F16, PAGED, 4, Part::kShared>, grid, block, 0, s, job);
-    else if (part == Part::kOwn) launch_kernel(k_kv4_prefix<D, F, F16, PAGED, 4, Part::kOwn>, grid, block, 0, s, job);
-    else if (waves == 8) launch_kernel(k_kv4_prefix<D, F, F16, PAGED, 8, Part::kSeparate>, grid, block, 0, s, job);
-    else launch_kernel(k_kv4_prefix<D, F, F16, PAGED, 4, Part::kSeparate>, grid, block, 0, s, job);
+void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
+    if (p.separate) {
+        const dim3 grid = item_grid(job.cache.kv_heads, job.tiles);
+        if (p.waves == 8) launch_kernel(k_kv4_prefix_separate<D, F, F16, PAGED, 8>, grid, dim3(512), 0, s, job);
+        else launch_kernel(k_kv4_prefix_separate<D, F, F16, PAGED, 4>, grid, dim3(256), 0, s, job);
+        return;
+    }
+    const SharedPart shared = {p.many ? 0 : p.shared_tiles, p.shared_chunk, p.shared_chunks};
+    const int64_t items = (int64_t)shared.tiles * shared.chunks + (p.own_many ? 0 : (int64_t)p.own_tiles * p.own_chunks);
+    if (items) launch_kernel(k_kv4_prefix<D, F, F16, PAGED>, item_grid(job.cache.kv_heads, items), dim3(256), 0, s, job, shared);
 }
 template <int D, int F, bool F16>
-void launch_few(const PrefixJob& job, Part part, int waves, hipStream_t s) {
-    if (job.cache.page_shift < 6) launch_few<D, F, F16, true>(job, part, waves, s);
-    else launch_few<D, F, F16, false>(job, part, waves, s);
+void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
+    if (job.cache.page_shift < 6) launch_few<D, F, F16, true>(job, p, s);
+    else launch_few<D, F, F16, false>(job, p, s);
 }
 template <int D, bool F16>
-void launch_few(const PrefixJob& job, Part part, int copies, int waves, hipStream_t s) {
-    if (copies == 4) launch_few<D, 4, F16>(job, part, waves, s);
-    else if (copies == 2) launch_few<D, 2, F16>(job, part, waves, s);
-    else launch_few<D, 1, F16>(job, part, waves, s);
+void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
+    if (p.own_copies == 4) launch_few<D, 4, F16>(job, p, s);
+    else if (p.own_copies == 2) launch_few<D, 2, F16>(job, p, s);
+    else launch_few<D, 1, F16>(job, p, s);
 }
-void launch_few(const PrefixJob& job, Part part, int copies, int waves, hipStream_t s) {
+void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
     const bool f16 = job.a.dtype == RQ_F16;
-    if (job.cache.head_dim == 128) f16 ? launch_few<128, true>(job, part, copies, waves, s) : launch_few<128, false>(job, part, copies, waves, s);
-    else f16 ? launch_few<64, true>(job, part, copies, waves, s) : launch_few<64, false>(job, part, copies, waves, s);
+    if (job.cache.head_dim == 128) f16 ? launch_few<128, true>(job, p, s) : launch_few<128, false>(job, p, s);
+    else f16 ? launch_few<64, true>(job, p, s) : launch_few<64, false>(job, p, s);
 }
 
 }  // namespace
@@ -116,7 +162,7 @@ rq_kv4_prefix_plan_t kv4_prefix_plan(const Kv4& c, const Kv4Attention& a, const 
     r.waves = p.separate ? p.waves : p.many ? 4 * p.groups : 4;
     r.many = p.many;
     r.own_many = p.own_many;
-    r.shared_rows = p.separate ? 0 : p.many ? 128 : 16 / p.shared_copies;
+    r.shared_rows = p.separate ? 0 : p.many ? 128 : 16;
     r.own_rows = p.own_many ? 128 : 16 / p.own_copies;
     r.shared_chunk = p.shared_chunk;
     r.shared_chunks = p.shared_chunks;
@@ -134,21 +180,19 @@ int kv4_prefix_attention(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x
     static_cast<KvJob&>(job) = KvJob{c, a, a.heads / c.kv_heads, p.own_tiles, 0, p.own_chunk, p.own_chunks, wide(a.q, a.q_token, a.q_head),
                                      wide(a.o, a.o_token, a.o_head), workspace};
     job.p = x;
-    if (p.separate) {
-        launch_few(job, Part::kSeparate, p.own_copies, p.waves, s);
-        return launch_rc();
-    }
     job.part_chunks = p.shared_chunks + p.own_chunks;
     job.part_first = p.shared_chunks;
+    launch_few(job, p, s);
+    if (p.separate) return launch_rc();
     if (p.own_many) launch_prefix_many(job, Part::kOwn, 1, s);
-    else launch_few(job, Part::kOwn, p.own_copies, 4, s);
-    PrefixJob shared = job;
-    shared.tiles = p.shared_tiles;
-    shared.chunk = p.shared_chunk;
-    shared.chunks = p.shared_chunks;
-    shared.part_first = 0;
-    if (p.many) launch_prefix_many(shared, Part::kShared, p.groups, s);
-    else launch_few(shared, Part::kShared, p.shared_copies, 4, s);
+    if (p.many) {
+        PrefixJob shared = job;
+        shared.tiles = p.shared_tiles;
+        shared.chunk = p.shared_chunk;
+        shared.chunks = p.shared_chunks;
+        shared.part_first = 0;
+        launch_prefix_many(shared, Part::kShared, p.groups, s);
+    }
     job.chunks = job.part_chunks;
     launch_join(job, s);
     return launch_rc();

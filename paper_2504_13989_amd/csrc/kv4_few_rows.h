@@ -330,20 +330,29 @@ __device__ __forceinline__ int* part_workers(const KvJob& job) {
     return reinterpret_cast<int*>(part_sums<D, C>(job) + (int64_t)(job.workers + job.tiles) * job.cache.kv_heads * C);
 }
 
+// LDS of a workgroup.
+template <int D, int W>
+struct FewLds {
+    __attribute__((aligned(16))) float params[W][kParameters * kTile];
+    __attribute__((aligned(16))) float o[W][16][D + 4];
+    float l[W][16];
+};
+
 // SHARED: workers share the keys out, else a workgroup takes a row tile, or (Part kShared, kOwn) a chunk of its keys.
+// number: of the workgroup among those of a kv head.
 template <int D, int F, bool F16, bool PAGED, int W, bool SHARED, Part PART>
-__device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::kWhole, KvJob, PrefixJob>& job) {
+__device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::kWhole, KvJob, PrefixJob>& job, int number, FewLds<D, W>& in_lds,
+                                         std::conditional_t<SHARED, Shares, int>& shares) {
     static_assert(!SHARED || PART == Part::kWhole, "workers take whole sequences");
     constexpr bool CHUNKED = PART == Part::kShared || PART == Part::kOwn;
     constexpr int C = 16 / F, E = D / 4;          // rows of the workgroup; elements of a row in a lane
-    __shared__ __attribute__((aligned(16))) float lds_params[W][kParameters * kTile];
-    __shared__ __attribute__((aligned(16))) float lds_o[W][16][D + 4];
-    __shared__ float lds_l[W][16];
-    __shared__ std::conditional_t<SHARED, Shares, int> shares;
+    auto& lds_params = in_lds.params;
+    auto& lds_o = in_lds.o;
+    auto& lds_l = in_lds.l;
     const Kv4Attention& a = job.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int copy = (lane & 15) / C, g = lane >> 4;
-    const int kv = job.cache.kv_heads, number = item_number(), head = blockIdx.x;
+    const int kv = job.cache.kv_heads, head = blockIdx.x;
     const int head_at = head * ((D + 8) << job.cache.page_shift);    // of the kv head's block in a page
     const CodeBits bits;
     float* lds = lds_params[wave];
@@ -578,7 +587,9 @@ __device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::
 
 template <int D, int F, bool F16, bool PAGED, int W, bool SHARED>
 __global__ __launch_bounds__(64 * W, 2) void k_kv4_attention(KvJob job) {
-    few_rows<D, F, F16, PAGED, W, SHARED, Part::kWhole>(job);
+    __shared__ FewLds<D, W> lds;
+    __shared__ std::conditional_t<SHARED, Shares, int> shares;
+    few_rows<D, F, F16, PAGED, W, SHARED, Part::kWhole>(job, item_number(), lds, shares);
 }
 
 }  // namespace

@@ -9,7 +9,7 @@ struct PrefixPlan {
     int waves;                                    // of a workgroup then
     bool many, own_many;                          // kernel for many rows: for the prefixes, for what is behind them
     int groups;                                   // of waves that share a workgroup's keys
-    int shared_copies, own_copies;                // kernel for few rows: copies of the rows among the columns
+    int own_copies;                               // kernel for few rows: copies of a sequence's rows among the columns
     int shared_tiles, own_tiles;                  // row tiles at most
     int shared_chunk, shared_chunks, own_chunk, own_chunks;   // keys of a workgroup, chunks of a row tile
     size_t bytes;                                 // workspace

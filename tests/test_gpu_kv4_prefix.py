@@ -74,12 +74,12 @@ class Batch:
             first = [*c.rows(self.slots[0][g]), c.steps(self.slots[0][g])]
             for b in range(b, b + size):
                 own = [*c.rows(self.slots[1][b]), c.steps(self.slots[1][b])]
-                k, v, steps = (np.concatenate(t) for t in zip(first, own))
                 n = self.counts[b]
                 heads, kv = list(range(self.heads)), list(range(self.kv))
-                if n > 500:                        # (long ones: two heads of their own kv heads)
+                if n > 500 or sum(self.prefix) * len(self.q) > 1 << 19:    # (long ones: two heads of their own kv heads)
                     heads, kv = [0, self.heads - 1], [0, self.kv - 1]
-                w, wl, bound = ref.attention(x[at:at + n][:, heads], k[:, kv], v[:, kv], steps[:, kv], scale, causal, window)
+                k, v, steps = (np.concatenate([t[:, kv], u[:, kv]]) for t, u in zip(first, own))
+                w, wl, bound = ref.attention(x[at:at + n][:, heads], k, v, steps, scale, causal, window)
                 y = got[at:at + n][:, heads]
                 assert np.isfinite(y).all()
                 # (as for attention without a prefix: the join's roundings are those of the sums, 2^-16 in the bound)
@@ -131,12 +131,14 @@ SHARED = [
     ([1000], [70], None, [1] * 70, 16, 16, 128, 64, "f16", 0, 0),
     ([700, 1100], [60, 30], None, [1] * 90, 32, 8, 128, 32, "bf16", 0, 0),
     ([2000], [12], None, [1, 3, 2] * 4, 12, 12, 128, 16, "bf16", 0, 0),
-    ([700, 1100], [100, 60], None, [1] * 160, 32, 4, 128, 32, "bf16", 1, 0),
-    ([1100, 500, 0], [40, 30, 8], None, [1] * 78, 40, 8, 64, 64, "f16", 1, 0),
-    ([1100], [100], None, [1] * 100, 40, 8, 128, 16, "f16", 1, 0),
-    ([1300, 70], [30, 50], None, [1, 2, 3, 4] * 20, 16, 8, 64, 16, "bf16", 1, 0),
+    ([3000, 4100], [100, 60], None, [1, 1, 1, 4] * 40, 16, 4, 128, 32, "bf16", 0, 0),
+    ([9000, 0], [50, 3], None, [9] * 52 + [60], 4, 4, 64, 128, "f16", 0, 0),
+    ([4500, 300], [200, 60], None, [1] * 260, 64, 8, 128, 32, "bf16", 1, 0),
+    ([7000, 500, 0], [150, 100, 8], None, [1] * 258, 40, 8, 64, 64, "f16", 1, 0),
+    ([9000], [200], None, [1] * 200, 64, 8, 128, 16, "f16", 1, 0),
+    ([6000, 70], [30, 50], None, [1, 2, 3, 4] * 20, 48, 8, 64, 16, "bf16", 1, 0),
     ([1500, 100, 1300], [2, 1, 2], [1300, 2, 1100, 300, 1200], [1300, 2, 1100, 100, 1200], 24, 8, 64, 16, "bf16", 1, 1),
-    ([900, 100], [1, 2], [1300, 1100, 300], [1300, 1100, 100], 24, 8, 128, 64, "f16", 1, 1),
+    ([900, 100], [1, 2], [1300, 1100, 300], [1300, 1100, 100], 24, 8, 128, 64, "f16", 0, 1),
 ]
 
 

@@ -103,7 +103,7 @@ def prefix_plan(L, units=256, **kw):
 
 
 def test_prefix_plan_refuses(L):
-    assert prefix_plan(L).separate == 1
+    assert prefix_plan(L).separate == 0 and prefix_plan(L, max_prefix=500).separate == 1
     for bad in (dict(dtype=1), dict(tokens=0), dict(tokens=4), dict(heads=3), dict(groups=0), dict(groups=1 << 21), dict(batch=0, tokens=0), dict(window=-1),
                 dict(max_prefix=-1), dict(max_len=-1), dict(max_prefix=1 << 30), dict(units=-1)):
         assert prefix_plan(L, **bad) == ARG, bad
