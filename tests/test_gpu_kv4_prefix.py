@@ -206,7 +206,8 @@ def test_lengths_and_groups_out_of_range():
 
 
 @pytest.mark.parametrize("shape", [([200], [4], [20, 9, 1, 40], [20, 4, 1, 33], 6, 2, 64, 16), ([900], [70], [i % 80 + 1 for i in range(70)], [1] * 70, 16, 8, 64, 16),
-                                   ([900], [70], [i % 80 + 1 for i in range(70)], [1] * 70, 16, 16, 128, 64)])
+                                   ([900], [70], [i % 80 + 1 for i in range(70)], [1] * 70, 16, 16, 128, 64),
+                                   ([4500], [200], [i % 80 + 1 for i in range(200)], [1] * 200, 64, 8, 128, 64)])
 def test_what_a_query_does_not_see_does_not_reach_it(shape):
     """a key of one sequence's own, and one of the prefix that only queries in it do not see"""
     b = Batch(21, *shape)
@@ -237,7 +238,7 @@ def test_strides(pad, n):
 
 def test_in_graphs_with_one_workspace_and_on_another_stream():
     """two graphs of calls that share a caller's workspace, replayed in turn with eager calls between"""
-    bs = [Batch(23, [900], [70], [i % 30 + 1 for i in range(70)], [1] * 70, 16, 16, 64, 16), Batch(24, [800, 90], [40, 30], [i % 30 + 1 for i in range(70)], [1] * 70, 32, 8, 128, 64)]
+    bs = [Batch(23, [900], [70], [i % 30 + 1 for i in range(70)], [1] * 70, 16, 16, 64, 16), Batch(24, [3000, 90], [40, 30], [i % 30 + 1 for i in range(70)], [1] * 70, 32, 8, 128, 64)]
     ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
     graphs, outs = [], []
     for b in bs:
@@ -260,6 +261,38 @@ def test_in_graphs_with_one_workspace_and_on_another_stream():
     got = [b.attend(stream=s) for b in bs]
     s.synchronize()
     assert all(torch.equal(x, b.attend()) for x, b in zip(got, bs))
+
+
+@pytest.mark.parametrize("shape,form", [(([200], [4], [20, 9, 1, 40], [20, 4, 1, 33], 6, 2, 64, 16), (1, 0)),
+                                        (([3000], [60], [i % 30 + 3 for i in range(60)], [1, 2, 3] * 20, 8, 8, 64, 16, "f16"), (0, 0)),
+                                        (([4500], [200], [i % 30 + 3 for i in range(200)], [1, 2] * 100, 64, 8, 128, 64), (0, 1))])
+def test_rows_behind_the_last_sequence_stay(shape, form):
+    """queries padded to a size that a graph was captured with"""
+    b = Batch(25, *shape)
+    want, n, pad = b.attend(), sum(b.counts), 37
+    b.q = torch.cat([b.q, torch.full((pad, b.heads, b.d), float("nan"), dtype=b.q.dtype, device="cuda")])
+    p = b.plan()
+    assert (p.separate, p.many) == form
+    out, lse = torch.full_like(b.q, 7.0), torch.full(b.q.shape[:2], 7.0, device="cuda")
+    b.attend(out=out, lse=lse)
+    # (another number of queries: other chunks, and other roundings)
+    assert (out[:n].float() - want.float()).norm() <= 2.0 ** -7 * want.float().norm() and torch.isfinite(lse[:n]).all()
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+
+
+def test_two_calls_at_once():
+    """on two streams, with the cache in common and the workspaces that torch gives each"""
+    b = Batch(26, [4000], [60], [i % 30 + 1 for i in range(60)], [1] * 60, 32, 8, 128, 64)
+    other = torch.randn_like(b.q)
+    want = [b.attend(), b.attend(q=other)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        got = [b.attend(q=q, stream=s) for q, s in zip((b.q, other), streams)]
+        for s in streams:
+            s.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
 
 
 def test_offsets_beyond_four_gigabytes():
