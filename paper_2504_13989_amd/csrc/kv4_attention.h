@@ -1,4 +1,4 @@
-// What the kernels of attention over the 4-bit paged cache share (kernels_kv4_attention.hip: few queries, kernels_kv4_prompt.hip: many).
+// What the kernels of attention over the 4-bit paged cache share (kv4_few_rows.h: few rows, kv4_many_rows.h: many).
 #pragma once
 #include "kv4_layout.h"
 #include "wave_common.h"

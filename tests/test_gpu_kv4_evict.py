@@ -153,6 +153,16 @@ def test_evict_leaves_rows_without_a_place(in_place):
     assert torch.equal(values(cache), expected(before, index, table, table if in_place else to, 16, 12))
 
 
+def test_evict_into_other_pages_in_any_order():
+    """positions in no order, and the same one again"""
+    rng = np.random.default_rng(4)
+    cache = filled(rng, 30, 2, 128, 32, 2)
+    before, table, to = values(cache), np.arange(20).reshape(2, 10), np.arange(20, 30).reshape(2, 5)
+    index = rng.integers(0, 320, (2, 2, 2, 150))
+    rq.kv4_evict(cache, ints(index.tolist()), ints(table.tolist()), new_table=ints(to.tolist()))
+    assert torch.equal(values(cache), expected(before, index, table, to, 32, 30))
+
+
 def test_evict_of_what_stays_where_it_is():
     cache = filled(np.random.default_rng(3), 6, 2, 128, 16, 1)
     before, index = cache.data.clone(), torch.arange(50, dtype=torch.int32).expand(1, 2, 50).contiguous().cuda()

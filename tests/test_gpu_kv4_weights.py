@@ -233,6 +233,48 @@ def test_the_same_bits_again_and_in_a_graph():
             assert torch.equal(ws[i], want[i])
 
 
+@pytest.mark.parametrize("shape", [([300, 90], [30, 60], 4, 2, 64, 16), ([900, 500], [300, 400], 8, 2, 128, 64, "f16")])
+def test_queries_behind_the_last_sequence_do_not_count(shape):
+    t = Batch(14, *shape)
+    lse, n = t.lse(), len(t.q)
+    t.q = torch.cat([t.q, torch.full((41, t.heads, t.d), float("nan"), dtype=t.q.dtype, device="cuda")])
+    lse, w = torch.cat([lse, torch.full((41, t.heads), float("nan"), device="cuda")]), t.old.clone()
+    t.weigh(lse, w)
+    t.q = t.q[:n]
+    assert t.check(lse[:n], w, decay=1.0) <= 2.0 ** -18
+
+
+def test_two_calls_at_once_and_two_graphs_with_one_workspace():
+    t = Batch(15, [900, 500], [300, 400], 8, 2, 128, 64)
+    lse, want = t.lse(), t.old.clone()
+    t.weigh(lse, want)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [t.old.clone() for _ in streams]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for s, w in zip(streams, got):
+        t.weigh(lse, w, stream=s)
+    for s in streams:
+        s.synchronize()
+    assert all(torch.equal(w, want) for w in got)
+    other = Batch(16, [300, 90], [70, 60], 4, 4, 64, 16, "f16")
+    space, graphs, outs, wants = torch.empty(64 << 20, dtype=torch.uint8, device="cuda"), [], [], []
+    for b in (t, other):
+        lse, w, x = b.lse(), b.old.clone(), b.old.clone()
+        b.weigh(lse, x, workspace=space)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.weigh(lse, w, workspace=space)
+        graphs.append((g, lse)), outs.append(w), wants.append(x)
+    for _ in range(3):
+        for b, (g, _), w, x in zip((t, other), graphs, outs, wants):
+            w.copy_(b.old)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(w, x)
+
+
 def test_on_another_stream():
     t = Batch(12, [900, 90], [1, 1], 8, 2, 128, 64)
     lse, want = t.lse(), t.old.clone()
