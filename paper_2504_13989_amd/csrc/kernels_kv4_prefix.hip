@@ -96,7 +96,7 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
     const double together = split(p.many ? 0 : p.shared_tiles, p.own_many ? 0 : p.own_tiles, 4, 2, false);
     if (p.own_many) split(0, p.own_tiles, 1, 2, true);
     // One launch takes every sequence by itself where the chip has that done before the prefixes' reuse pays for joining, kJoin steps.
-    constexpr double kJoin = 2.5;
+    constexpr double kJoin = 1.7;
     const int waves = few * c.kv_heads <= num_cu ? 8 : 4;
     const int64_t each = chunks_of(shared_keys, waves) + chunks_of(own_keys, waves) + kStart;
     const double apart = time_of(few * c.kv_heads * each, each, waves == 8 ? 1 : 2);
