@@ -4,7 +4,11 @@
 // The rows of all sequences of a group are one set of rows against the prefix: its keys are read and unpacked once for 16 of them (kernel
 // for few rows) or 128 (kernel for many).  Each sequence's own positions are a call as any other's.  Both leave partial results, a row's
 // normalised sums and the logarithm of their weight for each chunk of keys, which are joined in a fixed order.  Where sharing does
-// not pay for the two launches more, a sequence's rows take the prefix and its own positions one after the other.
+// not pay for the launch more, a sequence's rows take the prefix and its own positions one after the other.
+//
+// One MI355X, bf16, 128 elements, 32 heads on 8: 64 queries behind 8192 positions, 300 of their own each: 33 us, 28 in the first launch, bound by
+// vector issue (590 instructions for 16 rows x 64 keys), 4.6 in the join; from whole tables 70.  Four behind 1000: 10.6, latency.  fp16, 12
+// sequences of 40 tokens, 64 heads on 8, 65411 positions: 1.1 ms, the many-row kernel's rate; from whole tables 1.5.
 #include "kv4_few_rows.h"
 #include "kv4_prefix.h"
 
@@ -51,6 +55,8 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
     p.own_copies = rows / a.batch <= 4 ? 4 : rows / a.batch <= 8 ? 2 : 1;
     const int64_t few = own_tiles(16 / p.own_copies), own_few = few * own_keys;
     const int64_t shared_few = shared_tiles(16) * shared_keys, shared_many = many_cost * shared_tiles(128) * shared_keys, own_many = many_cost * own_tiles(128) * own_keys;
+    // (a launch more for the rows behind the prefixes, a start and partial results of 128 rows: 30 us.  bf16, 32 heads on 8: 64 queries x 8192 few
+    // 34, many 44; x 32768 98, 73; 16 x 65536 54, 63.  fp16, 64 heads on 8: 4 sequences of 40 tokens x 8192 74, 97; 12 of 20 x 32768 387, 306.)
     p.many = (shared_few - shared_many) * c.kv_heads > 90 * (int64_t)num_cu;
     p.own_many = own_many < own_few && own_few * c.kv_heads > 256 * (int64_t)num_cu;
     // Chunks of as many tiles of keys as cost least, in steps of 1.5 us.  A workgroup takes `at_once` tiles a step and kStart steps besides; the
@@ -96,6 +102,7 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
     const double together = split(p.many ? 0 : p.shared_tiles, p.own_many ? 0 : p.own_tiles, 4, 2, false);
     if (p.own_many) split(0, p.own_tiles, 1, 2, true);
     // One launch takes every sequence by itself where the chip has that done before the prefixes' reuse pays for joining, kJoin steps.
+    // (32 heads on 8: 4 queries x 1000 apart 11.8, together 10.6; 16 x 1000 11.4 and 11.7, x 4000 20.8 and 13.3; 160 of 3 groups x 1000 28 and 33.)
     constexpr double kJoin = 1.7;
     const int waves = few * c.kv_heads <= num_cu ? 8 : 4;
     const int64_t each = chunks_of(shared_keys, waves) + chunks_of(own_keys, waves) + kStart;

@@ -89,7 +89,9 @@ __device__ __forceinline__ void spread(Rows& r, const RowTerms& t, int lane) {
 }
 
 // One query a sequence, at most sixteen heads a kv head.  F: copies of 16 / F rows among the sixteen, of which each takes every F-th 16 keys.
-// A wave takes every fourth tile of 64 keys of the workgroup's chunk.
+// A wave takes every fourth tile of 64 keys of the workgroup's chunk, and asks for the next one before this one's work.  Bound by memory: 16
+// sequences x 32 heads x 8192 positions, 319 MB, 60 us (5.4 TB/s; the keys alone 44, stores mixed with reads cost the rest); vector issue
+// 53 %, matrix cores 24 %.  1025 positions, 32 heads to 8: 5 us, launch and dependent loads.
 template <int D, int F, bool F16, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights(KvJob job, Kv4Weights out) {
     constexpr int C = 16 / F;
@@ -256,7 +258,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_weights_rows(KvJob job) {
 }
 
 // A workgroup takes 256 keys, 64 a wave, unpacked once into registers, and a share of the row tiles that see some of them; row tiles come
-// through LDS, the next one while this one is multiplied.
+// through LDS, the next one while this one is multiplied, and a tile's products stand between the exponentials of the one before.  Bound by
+// issue: 64 queries of 32 heads on 8 against 16384 positions 20 us of 25.5 (one after the other 31); two prompts of 4000 queries, 5003 positions,
+// window 1024, 14 heads of 64 on 2: 65 - 69 us in all, vector issue 50 %, matrix cores 23 %, 12 of them for laying queries out.
 template <int D, bool PAGED>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, Kv4Weights out, float* parts) {
     constexpr int S = D / 16, N = 2 * S * 64 / (64 * kWaves);        // steps; sixteens of bytes of a tile that a thread brings
