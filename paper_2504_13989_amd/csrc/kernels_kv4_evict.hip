@@ -1,6 +1,6 @@
 // Which positions of a cached sequence are kept, and the kept rows moved together (kv4_layout.h).
 //
-// select: a workgroup takes a row of weights, as integers in the order of the numbers, in registers up to 32768 of them.  The k-th largest is found
+// select: a workgroup takes a row of weights, as integers in the order of the numbers, in registers up to 57344 of them.  The k-th largest is found
 // in up to four passes of eight bits: how many there are of each digit among those whose bits before it are the ones found so far, until
 // all that are left of a digit are wanted.  Weights crowd in a few digits, so each has sixteen counters, one for every fourth lane of a
 // wave (2048 of one counter each: bound by lanes that wait for each other's additions, 4096 rows of 8192 in 101 us).  So 48.6, of which reading and
@@ -119,6 +119,22 @@ struct SelectRow {
     }
 };
 
+// The keys of a wave's 64 R weights x, from position `begin` on.  Weights are seldom anything but 0 .. infinity, whose bits have their order: two
+// instructions each for fourteen, which bind where a row is long (one of 131072: 120 and 87 us).
+template <int R>
+__device__ __forceinline__ void to_keys(uint32_t (&key)[R], const SelectRow& at, const float (&x)[R], int begin, int lane) {
+    bool plain = begin >= at.lo && begin + 64 * R <= at.hi;
+#pragma unroll
+    for (int r = 0; r < R; ++r) plain = plain && __float_as_uint(x[r]) <= 0x7f800000u;
+    if (__all(plain)) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = __float_as_uint(x[r]) | 0x80000000u;
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = at.key(begin + lane + 64 * r, x[r]);
+    }
+}
+
 // A row of at most 64 W R weights.  Wave w has the R * 64 from 64 R w on, lane by lane.
 template <int W, int R>
 __global__ __launch_bounds__(64 * W) void k_kv4_select(Kv4Select a, int64_t rows) {
@@ -130,14 +146,13 @@ __global__ __launch_bounds__(64 * W) void k_kv4_select(Kv4Select a, int64_t rows
     const SelectRow at(a, row);
     if (at.whole(a, 64 * W)) return;
     const int len = at.len, first = wave * (64 * R) + lane;
+    // (range-checked, 0 behind the last one: no 64 bits of address for each)
+    const auto weights = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(at.w), 0, 4 * len, 0x00020000);
+    float x[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) x[r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(weights, 4 * first, 256 * r, 0));
     uint32_t key[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int j = first + 64 * r;
-        key[r] = __float_as_uint(at.w[j < len ? j : len - 1]);
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) key[r] = at.key(first + 64 * r, __uint_as_float(key[r]));
+    to_keys<R>(key, at, x, first - lane, lane);
     const Threshold t = find_threshold<W>(digits, a.keep, [&](auto count) {
 #pragma unroll
         for (int r = 0; r < R; ++r) count(key[r]);
@@ -182,30 +197,48 @@ __global__ __launch_bounds__(64 * W) void k_kv4_select(Kv4Select a, int64_t rows
     }
 }
 
-// Rows of any length: the same, with the row read again for every pass.
-constexpr int kLongWaves = 16;
+// Rows of any length: the same, with the row read again for every pass, kLong weights a thread at once.  (One row of 131072: 87 us; with one at once 295.)
+constexpr int kLongWaves = 16, kLong = 8;
 __global__ __launch_bounds__(64 * kLongWaves) void k_kv4_select_long(Kv4Select a, int64_t rows) {
-    constexpr int W = kLongWaves, T = 64 * W;
+    constexpr int W = kLongWaves, S = 64 * W * kLong;
     __shared__ __attribute__((aligned(16))) Digits digits;
     __shared__ int taken_of[2][W], equal_of[2][W];
     const int64_t row = group_index();
     if (row >= rows) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const SelectRow at(a, row);
-    if (at.whole(a, T)) return;
-    const int len = at.len;
+    if (at.whole(a, 64 * W)) return;
+    const int len = at.len, first = wave * (64 * kLong) + lane;
+    const auto read = [&](uint32_t (&key)[kLong], int from) {        // the stretch of S weights from there on
+        float x[kLong];
+#pragma unroll
+        for (int r = 0; r < kLong; ++r) {
+            const int j = from + first + 64 * r;
+            x[r] = at.w[j < len ? j : len - 1];
+        }
+        to_keys<kLong>(key, at, x, from + wave * (64 * kLong), lane);
+    };
     const Threshold t = find_threshold<W>(digits, a.keep, [&](auto count) {
-        for (int64_t j = threadIdx.x; j < len; j += T) count(at.key(j, at.w[j]));
+        for (int from = 0; from < len; from += S) {
+            uint32_t key[kLong];
+            read(key, from);
+#pragma unroll
+            for (int r = 0; r < kLong; ++r) count(key[r]);
+        }
     });
     int n = 0, e = 0, turn = 0;                   // written, and ties met, before the stretch in hand
-    for (int64_t from = 0; from < len; from += T, turn ^= 1) {
-        const int64_t j = from + threadIdx.x;
-        const uint32_t key = j < len ? at.key(j, at.w[j]) : 0u;
-        const bool mine = j < len && key >= t.least, tie = t.ties && j < len && key == t.least - 1;
-        const uint64_t taken = __ballot(mine), equal = __ballot(tie);
+    for (int from = 0; from < len; from += S, turn ^= 1) {
+        uint32_t key[kLong];
+        read(key, from);
+        int mine = 0, ties = 0;
+#pragma unroll
+        for (int r = 0; r < kLong; ++r) {
+            mine += __builtin_popcountll(__ballot(key[r] >= t.least));
+            ties += __builtin_popcountll(__ballot(key[r] == t.least - 1));
+        }
         if (lane == 0) {
-            taken_of[turn][wave] = __builtin_popcountll(taken);
-            equal_of[turn][wave] = __builtin_popcountll(equal);
+            taken_of[turn][wave] = mine;
+            equal_of[turn][wave] = ties;
         }
         __syncthreads();
         int n0 = n, e0 = e;                       // ... and before this wave's part of it
@@ -217,8 +250,15 @@ __global__ __launch_bounds__(64 * kLongWaves) void k_kv4_select_long(Kv4Select a
             n += cn;
             e += ce;
         }
-        const int rank = e0 + below(equal);
-        if (mine || (tie && rank < t.ties)) at.out[n0 + below(taken) + (rank < t.ties ? rank : t.ties)] = (int)j;
+#pragma unroll
+        for (int r = 0; r < kLong; ++r) {
+            const bool taken = key[r] >= t.least, tie = key[r] == t.least - 1;
+            const uint64_t all = __ballot(taken), equal = __ballot(tie);
+            const int rank = e0 + below(equal);
+            if (taken || (tie && rank < t.ties)) at.out[n0 + below(all) + (rank < t.ties ? rank : t.ties)] = from + first + 64 * r;
+            n0 += __builtin_popcountll(all);
+            e0 += __builtin_popcountll(equal);
+        }
     }
 }
 
@@ -422,6 +462,7 @@ int kv4_select(const Kv4Select& a, hipStream_t s) {
     else if (a.n <= 8192) launch_select<8, 16>(a, rows, s);
     else if (a.n <= 16384) launch_select<16, 16>(a, rows, s);
     else if (a.n <= 32768) launch_select<16, 32>(a, rows, s);
+    else if (a.n <= 57344) launch_select<16, 56>(a, rows, s);       // (as many as a wave's registers hold; a row of 40000 24 us, read again for every pass 31)
     else launch_kernel(k_kv4_select_long, group_grid(rows, 64 * kLongWaves), dim3(64 * kLongWaves), 0, s, a, rows);
     return launch_rc();
 }

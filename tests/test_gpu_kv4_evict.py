@@ -25,7 +25,7 @@ def check_select(w, lens, keep, sinks=0, recent=0, **kw):
     return got
 
 
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 255, 1000, 1024, 1025, 4096, 4097, 8192, 9000, 20000, 32768, 33000])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 255, 1000, 1024, 1025, 4096, 4097, 8192, 9000, 20000, 32768, 33000, 40960, 57344, 57345, 70001])
 def test_select(n):
     rng = np.random.default_rng(n)
     w = torch.tensor(np.exp(3 * rng.standard_normal((3, 2, n))), dtype=torch.float32).cuda()
