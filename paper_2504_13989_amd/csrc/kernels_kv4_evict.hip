@@ -7,7 +7,7 @@
 // writing are 10 and 5: LDS additions and the waits between passes; 32 rows of 4099 in 7.9, four passes one after the other.
 // evict: codes and parameters move as they are, nothing is quantized again.  Bound by the lines of 128 bytes that are touched: a token's key codes
 // are 64 bytes (128 elements), its value codes a quarter of four tokens'.  1024 rows of 4096 positions to 1024, in place: 96 us for 443 MB that move
-// (4.6 TB/s, a large copy 4.9), 294 of them wanted; 32 rows to 1000 in other pages 6.9 us, a chain of loads (index, table, codes).
+// (4.6 TB/s, a large copy 4.9), 294 of them wanted; 32 rows to 1000 in other pages 5.5 us, a chain of loads (index, table, codes).
 #include "kv4_layout.h"
 #include "wave_common.h"
 
@@ -264,9 +264,9 @@ __global__ __launch_bounds__(64 * kLongWaves) void k_kv4_select_long(Kv4Select a
 
 // ---- evict
 
-constexpr int kTokens = 16;                       // of a wave: they lie in one page where they go
+constexpr int kTokens = 16;                       // of a wave that takes whole rows: they lie in one page where they go
 
-// Where four times kTokens rows come from, a row a lane: the page (-1: there is none), the place in it.
+// Where rows come from, a row a lane: the page (-1: there is none), the place in it.
 struct Sources {
     int page, place;
 };
@@ -277,64 +277,69 @@ __device__ __forceinline__ Sources find_sources(const Kv4& c, const Kv4Evict& a,
     return Sources{page < 0 ? -1 : page, at & ((1 << c.page_shift) - 1)};
 }
 
-// What a wave holds of its tokens.  Keys: lane l has part l % 4 of token l / 4.  Values: fours of tokens of a run, as the layout has them.
-// Parameters: lanes 0 .. 15 keys', 16 .. 31 values'.
+// What a wave holds of its kTokens * P tokens, of which it takes a P-th of the elements (part `part`), P 1 or 4.  Keys: a quarter of a token, of lane
+// l quarter l % 4 of token l / 4, or `part` of token l.  Values: fours of tokens of a run, as the layout has them.  Parameters: lanes 0 .. 15
+// keys', 16 .. 31 values'; P == 4: of token l, part 0 keys', 1 values'.
 template <int D>
 struct Held {
     uint32_t k[D / 32];
     uint32_t v[D / 64][4];
     uint32_t p;
-    int from;                                     // of token `lane & 15`: its page; -1: none
+    int from;                                     // of token `lane & 15`, or `lane`: its page; -1: none
 };
 
-// Tokens whose sources are those of lanes 16 n + 0 .. 15.  (Rows that are not there come from page 0, and go nowhere: no branch, behind which
+// Tokens whose sources are those of lanes kTokens P n and on.  (Rows that are not there come from page 0, and go nowhere: no branch, behind which
 // all loads would be waited for.)
-template <int D>
-__device__ __forceinline__ void load_rows(Held<D>& t, const uint8_t* base, const Kv4& c, const Sources& s, int n, int head_at, int lane) {
+template <int D, int P>
+__device__ __forceinline__ void load_rows(Held<D>& t, const uint8_t* base, const Kv4& c, const Sources& s, int n, int head_at, int part, int lane) {
     typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
-    const int p = 1 << c.page_shift;
-    t.from = __shfl(s.page, 16 * n + (lane & 15));
+    constexpr int cols = D / 4 / P;               // of a run of values
+    const int p = 1 << c.page_shift, first = P == 1 ? kTokens * n : 0, mine = P == 1 ? lane & 15 : lane;
+    t.from = P == 1 ? __shfl(s.page, first + mine) : s.page;
     const auto block = [&](int page) { return base + (uint64_t)(uint32_t)(page < 0 ? 0 : page) * (uint32_t)c.page_bytes + head_at; };
     {
-        const int from = __shfl(s.page, 16 * n + (lane >> 2)), in = __shfl(s.place, 16 * n + (lane >> 2));
-        const words x = *reinterpret_cast<const words*>(block(from) + in * (D / 2) + (lane & 3) * (D / 8));
+        const int from = P == 1 ? __shfl(s.page, first + (lane >> 2)) : s.page, in = P == 1 ? __shfl(s.place, first + (lane >> 2)) : s.place;
+        const words x = *reinterpret_cast<const words*>(block(from) + in * (D / 2) + (P == 1 ? lane & 3 : part) * (D / 8));
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) t.k[j] = x[j];
     }
 #pragma unroll
     for (int r = 0; r < D / 64; ++r) {
-        const int run = lane + 64 * r, four = run / (D / 4), within = run % (D / 4);
+        const int run = lane + 64 * r, four = run / cols, within = part * cols + run % cols;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int from = __shfl(s.page, 16 * n + 4 * four + e), in = __shfl(s.place, 16 * n + 4 * four + e);
+            const int from = __shfl(s.page, first + 4 * four + e), in = __shfl(s.place, first + 4 * four + e);
             t.v[r][e] = *reinterpret_cast<const uint16_t*>(block(from) + p * (D / 2) + (in >> 2) * (2 * D) + within * 8 + 2 * (in & 3));
         }
     }
-    const int in = __shfl(s.place, 16 * n + (lane & 15));
-    t.p = *reinterpret_cast<const uint32_t*>(block(t.from) + p * D + (lane >> 4 & 1) * 4 * p + 4 * in);
+    const int in = P == 1 ? __shfl(s.place, first + mine) : s.place, which = P == 1 ? lane >> 4 & 1 : part & 1;
+    t.p = *reinterpret_cast<const uint32_t*>(block(t.from) + p * D + which * 4 * p + 4 * in);
 }
 
-template <int D>
-__device__ __forceinline__ void store_rows(const Held<D>& t, uint8_t* base, const Kv4& c, int page, int i0, int head_at, int lane) {
+// page: of the tokens, P == 4: of token `lane` (in the cache, or t.from is -1).
+template <int D, int P>
+__device__ __forceinline__ void store_rows(const Held<D>& t, uint8_t* base, const Kv4& c, int page, int i0, int head_at, int part, int lane) {
     typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
-    const int p = 1 << c.page_shift, in = i0 & (p - 1);
-    uint8_t* block = base + (uint64_t)(uint32_t)page * (uint32_t)c.page_bytes + head_at;
-    if (__shfl(t.from, lane >> 2) >= 0) {
+    constexpr int cols = D / 4 / P;
+    const int p = 1 << c.page_shift;
+    const auto block = [&](int page) { return base + (uint64_t)(uint32_t)page * (uint32_t)c.page_bytes + head_at; };
+    const int token = P == 1 ? lane >> 2 : lane;
+    if ((P == 1 ? __shfl(t.from, token) : t.from) >= 0) {
         words x;
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) x[j] = t.k[j];
-        *reinterpret_cast<words*>(block + (in + (lane >> 2)) * (D / 2) + (lane & 3) * (D / 8)) = x;
+        *reinterpret_cast<words*>(block(page) + ((i0 + token) & (p - 1)) * (D / 2) + (P == 1 ? lane & 3 : part) * (D / 8)) = x;
     }
 #pragma unroll
     for (int r = 0; r < D / 64; ++r) {
-        const int run = lane + 64 * r, four = run / (D / 4), within = run % (D / 4);
+        const int run = lane + 64 * r, four = run / cols, within = part * cols + run % cols, to = P == 1 ? page : __shfl(page, 4 * four);
         bool there[4], all = true;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             there[e] = __shfl(t.from, 4 * four + e) >= 0;
             all = all && there[e];
         }
-        uint16_t* v = reinterpret_cast<uint16_t*>(block + p * (D / 2) + ((in >> 2) + four) * (2 * D) + within * 8);
+        uint16_t* v = reinterpret_cast<uint16_t*>(block(to) + p * (D / 2) + (((i0 >> 2) + four) & (p / 4 - 1)) * (2 * D) + within * 8);
         if (all) {
             *reinterpret_cast<u32x2*>(v) = u32x2{t.v[r][0] | (t.v[r][1] << 16), t.v[r][2] | (t.v[r][3] << 16)};
         } else {                                  // (rows that do not move leave others' bytes)
@@ -343,19 +348,32 @@ __device__ __forceinline__ void store_rows(const Held<D>& t, uint8_t* base, cons
                 if (there[e]) v[e] = (uint16_t)t.v[r][e];
         }
     }
-    if (lane < 32 && t.from >= 0) *reinterpret_cast<uint32_t*>(block + p * D + (lane >> 4) * 4 * p + 4 * (in + (lane & 15))) = t.p;
+    const int mine = P == 1 ? lane & 15 : lane, which = P == 1 ? lane >> 4 : part;
+    if (which < 2 && t.from >= 0) *reinterpret_cast<uint32_t*>(block(page) + p * D + which * 4 * p + 4 * ((i0 + mine) & (p - 1))) = t.p;
 }
 
 // A row of weights, in place, by a workgroup of T threads: stretch by stretch, each read before it is written.  (index[i] >= i: what is
 // written has been read.)
 template <int T>
 __device__ __forceinline__ void move_weights(float* w, const int32_t* index, const Kv4Evict& a) {
-    for (int i0 = 0; i0 < a.keep; i0 += T) {
-        const int i = i0 + (int)threadIdx.x, at = i < a.keep ? index[i] : -1;
-        const float x = at >= 0 && at < a.n ? w[at] : 0.0f;
+    constexpr int N = 8;                          // of a thread at once
+    for (int i0 = 0; i0 < a.keep; i0 += N * T) {
+        int at[N];
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int i = i0 + e * T + (int)threadIdx.x;
+            at[e] = i < a.keep ? index[i] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = at[e] >= 0 && at[e] < a.n ? w[at[e]] : 0.0f;
         __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
         __syncthreads();
-        if (i < a.keep) w[i] = x;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int i = i0 + e * T + (int)threadIdx.x;
+            if (i < a.keep) w[i] = x[e];
+        }
     }
     for (int i = a.keep + (int)threadIdx.x; i < a.n; i += T) w[i] = 0.0f;
 }
@@ -374,31 +392,41 @@ struct Row {
 
 // In place: a workgroup a row, stretch by stretch.  A position is read by stretches up to its own, which is written once all waves have
 // read theirs; what the next one reads lies behind it, and is asked for before that.
-constexpr int kPlaceWaves = 8;
-template <int D>
+//
+// P: workgroups of a row, each with a P-th of every token's elements.  One a row moves lines whole; where rows are few their stretches follow one
+// another too slowly (1.7 us), and four have a quarter of the stretches.  Positions 8192 to 4096, 8 heads of 128: 32 rows 54 us with one, 25 with
+// four; 64 rows 55 and 42; 128 rows 55 and 70; 1024 rows of 4096 to 1024 96 and 171.  One row, 65536 to 32768: 421 and 152.
+constexpr int kPlaceWaves = 8, kFewRows = 64;
+template <int D, int P>
 __global__ __launch_bounds__(64 * kPlaceWaves) void k_kv4_evict_in_place(Kv4 c, Kv4Evict a, int64_t rows) {
-    constexpr int S = kPlaceWaves * kTokens;
-    const int64_t row = group_index();
+    constexpr int S = kPlaceWaves * kTokens * P, B = 4 / P;          // a stretch; stretches whose sources a wave holds
+    const int64_t group = group_index(), row = group / P;
+    const int part = (int)(group - row * P);
     if (row >= rows) return;
     const Row at(row, c, a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t *index = a.index + row * a.keep, *table = a.table + (int64_t)at.seq * a.width;
     const int head_at = at.head * ((D + 8) << c.page_shift);
     uint8_t* base = c.data + at.layer * a.layer_bytes;
-    // the wave's tokens of four stretches: a lane each
-    const auto sources = [&](int first) { return find_sources(c, a, index, table, (int64_t)first + (lane >> 4) * S + wave * kTokens + (lane & 15)); };
-    Sources from = sources(0), later = sources(4 * S);
+    // the wave's tokens of B stretches: a lane each
+    const auto sources = [&](int first) {
+        return find_sources(c, a, index, table, P == 1 ? (int64_t)first + (lane >> 4) * S + wave * kTokens + (lane & 15) : (int64_t)first + wave * 64 + lane);
+    };
+    Sources from = sources(0), later = sources(B * S);
     int n = 0;                                    // of the stretch that is asked for next, among those of `from`
     Held<D> even, odd;
     const auto ask = [&](Held<D>& t, int i0) {    // stretch i0
-        if (n == 4) {
+        if (n == B) {
             n = 0;
             from = later;
-            later = sources(i0 + 4 * S);
+            later = sources(i0 + B * S);
         }
-        load_rows<D>(t, base, c, from, n++, head_at, lane);
+        load_rows<D, P>(t, base, c, from, n++, head_at, part, lane);
     };
     const auto move = [&](Held<D>& t, Held<D>& next, int i0) {
+        const int i = i0 + wave * kTokens * P;
+        int to = -1;                              // P == 4: the page that token `lane` goes to
+        if constexpr (P == 4) to = i + lane < a.keep ? table[(i + lane) >> c.page_shift] : -1;
         ask(next, i0 + S);
         // what this stretch has asked for is here, and so it is in the other waves
 #pragma unroll
@@ -408,10 +436,13 @@ __global__ __launch_bounds__(64 * kPlaceWaves) void k_kv4_evict_in_place(Kv4 c, 
         asm volatile("" : "+v"(t.p) : : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" : : : "memory");
-        const int i = i0 + wave * kTokens;
-        if (i < a.keep) {
+        if (P == 1 && i < a.keep) {
             const int page = table[i >> c.page_shift];
-            if (page >= 0 && page < c.pages) store_rows<D>(t, base, c, page, i, head_at, lane);
+            if (page >= 0 && page < c.pages) store_rows<D, P>(t, base, c, page, i, head_at, part, lane);
+        }
+        if (P == 4 && i < a.keep) {
+            if (to < 0 || to >= c.pages) t.from = -1;
+            store_rows<D, P>(t, base, c, to, i, head_at, part, lane);
         }
     };
     if (a.keep > 0 && c.pages > 0) {
@@ -421,7 +452,7 @@ __global__ __launch_bounds__(64 * kPlaceWaves) void k_kv4_evict_in_place(Kv4 c, 
             if (i0 + S < a.keep) move(odd, even, (int)i0 + S);
         }
     }
-    if (a.weights) move_weights<64 * kPlaceWaves>(a.weights + at.layer * a.w_layer + at.seq * a.w_seq + at.head * a.w_head, index, a);
+    if (a.weights && part == P - 1) move_weights<64 * kPlaceWaves>(a.weights + at.layer * a.w_layer + at.seq * a.w_seq + at.head * a.w_head, index, a);
 }
 
 // Into other pages: a wave sixteen tokens, and a workgroup for each row of weights.
@@ -444,8 +475,8 @@ __global__ __launch_bounds__(64 * kMoveWaves) void k_kv4_evict(Kv4 c, Kv4Evict a
     uint8_t* base = c.data + at.layer * a.layer_bytes;
     const int page = a.new_table[(int64_t)at.seq * a.new_width + (i >> c.page_shift)];
     Held<D> t;
-    load_rows<D>(t, base, c, find_sources(c, a, index, table, i + (lane & 15)), 0, head_at, lane);
-    if (page >= 0 && page < c.pages) store_rows<D>(t, base, c, page, i, head_at, lane);
+    load_rows<D, 1>(t, base, c, find_sources(c, a, index, table, i + (lane & 15)), 0, head_at, 0, lane);
+    if (page >= 0 && page < c.pages) store_rows<D, 1>(t, base, c, page, i, head_at, 0, lane);
 }
 
 template <int W, int R>
@@ -471,7 +502,9 @@ int kv4_evict(const Kv4& c, const Kv4Evict& a, hipStream_t s) {
     const int64_t rows = (int64_t)a.layers * a.batch * c.kv_heads;
     const bool wide = c.head_dim == 128;
     if (!a.new_table) {
-        launch_kernel(wide ? k_kv4_evict_in_place<128> : k_kv4_evict_in_place<64>, group_grid(rows, 64 * kPlaceWaves), dim3(64 * kPlaceWaves), 0, s, c, a, rows);
+        const dim3 block(64 * kPlaceWaves);
+        if (rows <= kFewRows) launch_kernel(wide ? k_kv4_evict_in_place<128, 4> : k_kv4_evict_in_place<64, 4>, group_grid(4 * rows, 64 * kPlaceWaves), block, 0, s, c, a, rows);
+        else launch_kernel(wide ? k_kv4_evict_in_place<128, 1> : k_kv4_evict_in_place<64, 1>, group_grid(rows, 64 * kPlaceWaves), block, 0, s, c, a, rows);
     } else {
         constexpr int S = kMoveWaves * kTokens;
         const int parts = (a.keep + S - 1) / S + (a.weights != nullptr);

@@ -108,7 +108,7 @@ def expected(before, index, table, to, page, pages):
 
 
 @pytest.mark.parametrize("in_place", [True, False])
-@pytest.mark.parametrize("d,page,kv,layers", [(128, 64, 2, 1), (64, 16, 3, 2), (128, 16, 1, 3), (64, 256, 2, 1), (128, 32, 5, 1)])
+@pytest.mark.parametrize("d,page,kv,layers", [(128, 64, 2, 1), (64, 16, 3, 2), (128, 16, 1, 3), (64, 256, 2, 1), (128, 32, 5, 1), (64, 16, 43, 2), (128, 64, 67, 2)])
 @pytest.mark.parametrize("lens,keep", [([300, 17, 0, 120], 100), ([1, 500], 1), ([260, 260, 259], 16), ([400], 399), ([300, 300], 129)])
 def test_evict(in_place, d, page, kv, layers, lens, keep):
     rng = np.random.default_rng(d + keep)

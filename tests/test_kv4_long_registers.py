@@ -13,6 +13,6 @@ def test_workgroups_that_a_unit_holds(kernels):  # noqa: F811
     """Two waves a SIMD, of the weights' kernel for single queries three, of selection and eviction as many as there are rows for."""
     vgprs = {k: v[0] for k, v in kernels.items()}
     for name, forms, most in (("k_kv4_prefixI", 24, 256), ("k_kv4_prefix_separateI", 48, 256), ("k_kv4_weights_manyI", 4, 256), ("k_kv4_weightsI", 24, 170),
-                              ("k_kv4_selectI", 6, 128), ("k_kv4_evict", 4, 96)):
+                              ("k_kv4_selectI", 6, 128), ("k_kv4_evict", 6, 96)):
         mine = {k: v for k, v in vgprs.items() if name in k}
         assert len(mine) == forms and max(mine.values()) <= most, (name, mine)
