@@ -146,11 +146,12 @@ __global__ __launch_bounds__(64 * W) void k_kv4_select(Kv4Select a, int64_t rows
     const SelectRow at(a, row);
     if (at.whole(a, 64 * W)) return;
     const int len = at.len, first = wave * (64 * R) + lane;
-    // (range-checked, 0 behind the last one: no 64 bits of address for each)
+    // (range-checked, 0 behind the last one: no 64 bits of address for each.  The check is of the vector offset and the instruction's alone, so that
+    // nothing stands in the scalar one.)
     const auto weights = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(at.w), 0, 4 * len, 0x00020000);
     float x[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(weights, 4 * first, 256 * r, 0));
+    for (int r = 0; r < R; ++r) x[r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(weights, 4 * first + 256 * r, 0, 0));
     uint32_t key[R];
     to_keys<R>(key, at, x, first - lane, lane);
     const Threshold t = find_threshold<W>(digits, a.keep, [&](auto count) {
