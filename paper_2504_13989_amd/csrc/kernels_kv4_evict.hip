@@ -3,7 +3,7 @@
 // select: a workgroup takes a row of weights, as integers in the order of the numbers, in registers up to 57344 of them.  The k-th largest is found
 // in up to four passes of eight bits: how many there are of each digit among those whose bits before it are the ones found so far, until
 // all that are left of a digit are wanted.  Weights crowd in a few digits, so each has sixteen counters, one for every fourth lane of a
-// wave (2048 of one counter each: bound by lanes that wait for each other's additions, 4096 rows of 8192 in 101 us).  So 48.6, of which reading and
+// wave (2048 of one counter each: bound by lanes that wait for each other's additions, 4096 rows of 8192 in 101 us).  So 48, of which reading and
 // writing are 10 and 5: LDS additions and the waits between passes; 32 rows of 4099 in 7.9, four passes one after the other.
 // evict: codes and parameters move as they are, nothing is quantized again.  Bound by the lines of 128 bytes that are touched: a token's key codes
 // are 64 bytes (128 elements), its value codes a quarter of four tokens'.  1024 rows of 4096 positions to 1024, in place: 96 us for 443 MB that move
