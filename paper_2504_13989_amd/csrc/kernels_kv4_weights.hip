@@ -454,6 +454,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_kv4_weights_many(KvJob job, 
         lds_barrier();
         for (int tile = t0; tile < t1; tile += 2) {
             take(tile, even, odd);
+            if (tile == t0) sum[0] = sum[1] = 0.0f;        // (of the rows before the first tile: NaN for a key that is not finite, seen or not)
             take(tile + 1, odd, even);            // (where there is no such tile, the last one again, whose weights are not taken)
         }
         if ((t1 - t0) % 2 == 0)

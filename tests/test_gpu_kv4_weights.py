@@ -305,3 +305,32 @@ def test_refusals():
             t.weigh(other, w)
     with pytest.raises(ValueError):
         rq.kv4_attention_weights(t.h, t.cache, t.q[:1], lse[:1], t.table, t.kv_lens, w)
+
+
+#         lens, counts, heads, kv, d, page, window | positions of keys that are not finite and that no query sees, beside others in their block that some do
+UNSEEN = [
+    ([300], [20], 2, 1, 64, 16, 30, [10, 63, 64, 200, 250]),
+    ([700, 513], [100, 3], 4, 2, 128, 64, 200, [300, 383, 400]),
+    ([300], [1], 20, 1, 128, 32, 100, [3, 130, 199]),                # (one query, more heads than the kernel for single ones takes)
+    ([300], [1], 4, 2, 64, 64, 30, [3, 200, 260, 269]),
+    ([900], [1], 7, 1, 128, 16, 600, [70, 290, 299]),
+]
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("decay", [0.0, 0.5])
+@pytest.mark.parametrize("case", range(len(UNSEEN)))
+def test_keys_that_are_not_finite_and_that_no_query_sees(case, decay, value):
+    """their weights decay as any that are not seen"""
+    *shape, window, at = UNSEEN[case]
+    t = Batch(20 + case, *shape, rotate=False)
+    lse, want = t.lse(window=window), t.old.clone()
+    t.weigh(lse, want, window=window, decay=decay)
+    assert t.check(lse, want, decay=decay, window=window) <= 2.0 ** -18
+    bad = torch.zeros((len(at), t.kv, t.d), device="cuda")
+    bad[..., 3] = value
+    rq.kv4_append(None, t.cache, bad, bad, torch.tensor([int(t.slots[0][j]) for j in at]).cuda())
+    assert torch.equal(t.lse(window=window), lse)
+    w = t.old.clone()
+    t.weigh(lse, w, window=window, decay=decay)
+    assert torch.equal(w, want)
