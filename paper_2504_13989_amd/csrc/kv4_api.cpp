@@ -234,7 +234,7 @@ int rq_kv4_attention_weights(const rq_hadamard_t* h, const rq_kv4_t* cache, cons
 int rq_kv4_select(const float* weights, int layers, int batch, int kv_heads, int64_t n, int64_t w_layer_stride, int64_t w_seq_stride,
                   int64_t w_head_stride, const int32_t* kv_lens, int64_t keep, int64_t sinks, int64_t recent, int32_t* index, void* stream) {
     if (layers < 0 || layers > (1 << 16) || batch < 0 || batch > (1 << 20) || kv_heads < 1 || kv_heads > RQ_KV4_MAX_HEADS) return RQ_ERR_ARG;
-    if (n < 0 || n > (1 << 30) || keep < 0 || keep > (1 << 30) || sinks < 0 || recent < 0 || sinks + recent > keep) return RQ_ERR_ARG;
+    if (n < 0 || n > (1 << 30) || keep < 0 || keep > (1 << 30) || sinks < 0 || recent < 0 || recent > keep || sinks > keep - recent) return RQ_ERR_ARG;
     if (w_layer_stride < 0 || w_seq_stride < 0 || w_head_stride < 0) return RQ_ERR_ARG;
     if ((int64_t)layers * batch * kv_heads >= (int64_t)1 << 31) return RQ_ERR_ARG;
     if (layers == 0 || batch == 0 || keep == 0) return RQ_OK;

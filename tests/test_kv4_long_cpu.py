@@ -154,3 +154,8 @@ def test_common_pages():
     assert pool.common_pages("ad") == 0
     pool.extend("d", 64)
     assert pool.common_pages("ad") == 0
+
+
+def test_select_refuses_sums_that_leave_64_bits(L):
+    for sinks, recent in ((1 << 62, 1 << 62), ((1 << 63) - 1, 1), (1, (1 << 63) - 1), ((1 << 63) - 1, (1 << 63) - 1), (8, 3), (0, 11)):
+        assert L.rq_kv4_select(64, 2, 3, 4, 50, 600, 200, 50, 64, 10, sinks, recent, 64, None) == ARG, (sinks, recent)
