@@ -268,7 +268,7 @@ size_t rq_kv4_prefix_attention_workspace(const rq_kv4_t* cache, int64_t tokens, 
                                          int64_t max_prefix, int64_t max_len) {
     rq::Kv4 c;
     if (cache_of(cache, &c) != RQ_OK || shape_ok(c, tokens, heads, batch, window, max_len) != RQ_OK || tokens == 0 || batch == 0) return 0;
-    if (groups < 1 || groups > (1 << 20) || max_prefix < 0 || max_prefix + max_len > (1 << 30)) return 0;
+    if (groups < 1 || groups > (1 << 20) || max_prefix < 0 || max_prefix > (1 << 30) - max_len) return 0;
     const int cu = num_cu();
     if (cu <= 0) return 0;
     rq::Kv4Attention a{};
@@ -288,7 +288,7 @@ int rq_kv4_prefix_attention_plan(const rq_kv4_t* cache, int dtype, int64_t token
     if (rc != RQ_OK) return rc;
     if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
     if (!plan || (dtype != RQ_BF16 && dtype != RQ_F16) || compute_units < 0) return RQ_ERR_ARG;
-    if (groups < 1 || groups > (1 << 20) || max_prefix < 0 || max_prefix + max_len > (1 << 30)) return RQ_ERR_ARG;
+    if (groups < 1 || groups > (1 << 20) || max_prefix < 0 || max_prefix > (1 << 30) - max_len) return RQ_ERR_ARG;
     if (tokens == 0 || batch == 0 || (decode && tokens != batch)) return RQ_ERR_ARG;
     const int cu = compute_units ? compute_units : num_cu();
     if (cu <= 0) return RQ_ERR_HIP;
@@ -315,7 +315,7 @@ int rq_kv4_prefix_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const
     if (!rotation_ok(h, c.head_dim) || (dtype != RQ_BF16 && dtype != RQ_F16)) return RQ_ERR_ARG;
     if ((rc = shape_ok(c, tokens, heads, batch, window, max_len)) != RQ_OK) return rc;
     if (width < 0 || prefix_width < 0 || (causal != 0 && causal != 1) || !(scale > 0.0f) || !std::isfinite(scale)) return RQ_ERR_ARG;
-    if (groups < 0 || groups > (1 << 20) || max_prefix < 0 || max_prefix + max_len > (1 << 30)) return RQ_ERR_ARG;
+    if (groups < 0 || groups > (1 << 20) || max_prefix < 0 || max_prefix > (1 << 30) - max_len) return RQ_ERR_ARG;
     if (q_token_stride < 0 || q_head_stride < 0 || o_token_stride < 0 || o_head_stride < 0) return RQ_ERR_ARG;
     if ((tokens > 1 && o_token_stride < c.head_dim) || (heads > 1 && o_head_stride < c.head_dim)) return RQ_ERR_ARG;
     if (!q_start && tokens != batch) return RQ_ERR_ARG;                    // a token a sequence

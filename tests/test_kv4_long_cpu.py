@@ -159,3 +159,12 @@ def test_common_pages():
 def test_select_refuses_sums_that_leave_64_bits(L):
     for sinks, recent in ((1 << 62, 1 << 62), ((1 << 63) - 1, 1), (1, (1 << 63) - 1), ((1 << 63) - 1, (1 << 63) - 1), (8, 3), (0, 11)):
         assert L.rq_kv4_select(64, 2, 3, 4, 50, 600, 200, 50, 64, 10, sinks, recent, 64, None) == ARG, (sinks, recent)
+
+
+def test_prefix_attention_refuses_sums_that_leave_64_bits(L):
+    for most in ((1 << 63) - 1, (1 << 63) - 32, (1 << 62) + 1, (1 << 30) - 63, 1 << 30):
+        assert prefix_plan(L, max_prefix=most, max_len=64) == ARG, most
+        assert L.rq_kv4_prefix_attention_workspace(cache(), 3, 4, 1, 3, 1, 0, most, 64) == 0, most
+        assert L.rq_kv4_prefix_attention(None, cache(), 64, 0, 3, 4, 512, 128, 64, 1, (1 << 31) - 1, 64, 64, 64, 3, 4, 64, None, 0.1, 1, 0, most, 64,
+                                         4096, 512, 128, None, None, 0, None) == ARG, most
+    assert prefix_plan(L, max_prefix=(1 << 30) - 64, max_len=64).shared_chunks > 0
