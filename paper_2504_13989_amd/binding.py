@@ -426,5 +426,7 @@ def kv4_select(weights, kv_lens, keep: int, sinks: int = 0, recent: int = 0, ind
 def kv4_evict(cache: KV4Cache, index, table, new_table=None, weights=None, stream=None) -> None:
     """rq_kv4_evict: position i of each kv head becomes its position index[(layer,) b, head, i] (int32, ascending), in place or in the pages of
     new_table (int32 [batch, new width]), in all layers of the cache.  weights (float32 [(layers,) batch, kv_heads, positions]) move along,
-    and are 0 behind."""
+    and are 0 behind.
+    In place only where no other sequence holds the pages (PagePool.shared_pages(seq) == 0): forked sequences that still share some
+    would lose their tokens, so they take new_table."""
     (_nat or _native()).kv4_evict(cache.data, cache.kv_heads, cache.head_dim, cache.page_size, index, table, new_table, weights, stream)

@@ -92,6 +92,11 @@ class PagePool:
             n = next((i for i in range(n) if table[i] != first[i]), n)
         return n
 
+    def shared_pages(self, seq) -> int:
+        """How many of the sequence's pages other sequences hold too.  A sequence that has some is not evicted in place (kv4_evict without
+        new_table): the others' tokens lie in the same pages."""
+        return sum(self._held[page] > 1 for page in self._tables[seq])
+
     def truncate(self, seq, length: int) -> None:
         """The sequence's first `length` tokens; pages behind them are freed."""
         if not 0 <= length <= self._lens[seq]:

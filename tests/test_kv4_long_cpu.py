@@ -168,3 +168,26 @@ def test_prefix_attention_refuses_sums_that_leave_64_bits(L):
         assert L.rq_kv4_prefix_attention(None, cache(), 64, 0, 3, 4, 512, 128, 64, 1, (1 << 31) - 1, 64, 64, 64, 3, 4, 64, None, 0.1, 1, 0, most, 64,
                                          4096, 512, 128, None, None, 0, None) == ARG, most
     assert prefix_plan(L, max_prefix=(1 << 30) - 64, max_len=64).shared_chunks > 0
+
+
+def test_shared_pages():
+    pool = PagePool(40, 16)
+    pool.add("a")
+    assert pool.shared_pages("a") == 0
+    pool.extend("a", 50)
+    assert pool.shared_pages("a") == 0
+    pool.fork("a", "b")
+    pool.fork("b", "c")
+    assert [pool.shared_pages(s) for s in "abc"] == [4, 4, 4]
+    pool.extend("b", 20)                           # its fourth page is its own then, and so is the fifth
+    assert [pool.shared_pages(s) for s in "abc"] == [4, 3, 4]
+    pool.truncate("c", 20)
+    assert [pool.shared_pages(s) for s in "abc"] == [3, 3, 2]
+    pool.free("a")
+    assert [pool.shared_pages(s) for s in "bc"] == [2, 2]
+    pool.compact()
+    assert [pool.shared_pages(s) for s in "bc"] == [2, 2]
+    pool.free("c")
+    assert pool.shared_pages("b") == 0
+    with pytest.raises(KeyError):
+        pool.shared_pages("c")
