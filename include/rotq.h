@@ -515,7 +515,8 @@ int rq_kv4_attention_plan(const rq_kv4_t* cache, int dtype, int64_t tokens, int 
 
 /*
  * Bytes of device workspace rq_kv4_prefix_attention needs for such a call on the current device; 0 where it needs none and on bad
- * arguments.  decode: q_start will be NULL.
+ * arguments.  At most 2^30 (but for a query whose heads alone take more): partial results are fp32 and two of each result at least, and calls
+ * with more of them take their queries in turns, the same kernels one after the other.  decode: q_start will be NULL.
  */
 size_t rq_kv4_prefix_attention_workspace(const rq_kv4_t* cache, int64_t tokens, int heads, int groups, int batch, int decode, int window,
                                          int64_t max_prefix, int64_t max_len);

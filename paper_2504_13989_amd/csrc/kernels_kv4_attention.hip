@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv4_join(KvJob job) {
     const int lane = threadIdx.x & 63;
     const int64_t row = group_index() * kWaves + (threadIdx.x >> 6), rows = (int64_t)a.tokens * a.heads;
     if (row >= rows) return;
-    const int tokens = a.q_start ? a.q_start[a.batch] : a.tokens;    // (rows behind the last sequence have no results)
+    const int tokens = a.q_start ? a.q_start[a.batch] - job.first_token : a.tokens;      // (rows behind the last sequence have no results)
     const float* sums = job.part + (int64_t)job.chunks * rows * D + row;
     float top = -INFINITY;
     for (int c = lane; c < job.chunks; c += 64) top = fmaxf(top, sums[c * rows]);

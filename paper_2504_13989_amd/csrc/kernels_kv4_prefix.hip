@@ -18,17 +18,18 @@ namespace {
 // The kernel for few rows.  The first of a kv head's workgroups take prefixes, the others what is behind them: either fills what the other
 // leaves of the chip.
 struct SharedPart {
-    int tiles, chunk, chunks;
+    int first_tile, tiles, chunk, chunks;
 };
 template <int D, int F, bool F16, bool PAGED>
 __global__ __launch_bounds__(256, 2) void k_kv4_prefix(PrefixJob job, SharedPart shared) {
     __shared__ FewLds<D, 4> lds;
     int none;
-    const int number = item_number(), first = shared.tiles * shared.chunks;
+    const int number = item_number(), first = (shared.tiles - shared.first_tile) * shared.chunks;
     if (number >= first) {
         few_rows<D, F, F16, PAGED, 4, false, Part::kOwn>(job, number - first, lds, none);
         return;
     }
+    job.first_tile = shared.first_tile;
     job.tiles = shared.tiles;
     job.chunk = shared.chunk;
     job.chunks = shared.chunks;
@@ -41,6 +42,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_kv4_prefix_separate(PrefixJob job
     int none;
     few_rows<D, F, F16, PAGED, W, false, Part::kSeparate>(job, item_number(), lds, none);
 }
+
+constexpr size_t kMostBytes = (size_t)1 << 30;    // of workspace
 
 PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num_cu) {
     const int group = a.heads / c.kv_heads;
@@ -116,37 +119,53 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
         p.waves = waves;
         return p;
     }
-    p.bytes = (size_t)(p.shared_chunks + p.own_chunks) * a.tokens * a.heads * (c.head_dim + 1) * sizeof(float);
+    // Partial results of as many tokens as kMostBytes hold (one at least), in turns of alike length: two chunks of 8 sequences of 4096 queries, 64
+    // heads of 128, would take 2.2 GB.  A turn has thousands of row tiles, and a tile that two turns share is all that is taken twice.
+    const size_t token_bytes = (size_t)(p.shared_chunks + p.own_chunks) * a.heads * (c.head_dim + 1) * sizeof(float);
+    const int64_t most_tokens = (int64_t)(kMostBytes / token_bytes), turns = chunks_of(a.tokens, most_tokens > 1 ? most_tokens : 1);
+    p.slice = (int)chunks_of(a.tokens, turns);
+    p.bytes = p.slice * token_bytes;
     return p;
 }
 
 template <int D, int F, bool F16, bool PAGED>
-void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
+void launch_few(const PrefixJob& job, const SharedPart& shared, const PrefixPlan& p, hipStream_t s) {
     if (p.separate) {
         const dim3 grid = item_grid(job.cache.kv_heads, job.tiles);
         if (p.waves == 8) launch_kernel(k_kv4_prefix_separate<D, F, F16, PAGED, 8>, grid, dim3(512), 0, s, job);
         else launch_kernel(k_kv4_prefix_separate<D, F, F16, PAGED, 4>, grid, dim3(256), 0, s, job);
         return;
     }
-    const SharedPart shared = {p.many ? 0 : p.shared_tiles, p.shared_chunk, p.shared_chunks};
-    const int64_t items = (int64_t)shared.tiles * shared.chunks + (p.own_many ? 0 : (int64_t)p.own_tiles * p.own_chunks);
+    const int64_t items = (int64_t)(shared.tiles - shared.first_tile) * shared.chunks + (int64_t)(job.tiles - job.first_tile) * job.chunks;
     if (items) launch_kernel(k_kv4_prefix<D, F, F16, PAGED>, item_grid(job.cache.kv_heads, items), dim3(256), 0, s, job, shared);
 }
 template <int D, int F, bool F16>
-void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
-    if (job.cache.page_shift < 6) launch_few<D, F, F16, true>(job, p, s);
-    else launch_few<D, F, F16, false>(job, p, s);
+void launch_few(const PrefixJob& job, const SharedPart& shared, const PrefixPlan& p, hipStream_t s) {
+    if (job.cache.page_shift < 6) launch_few<D, F, F16, true>(job, shared, p, s);
+    else launch_few<D, F, F16, false>(job, shared, p, s);
 }
 template <int D, bool F16>
-void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
-    if (p.own_copies == 4) launch_few<D, 4, F16>(job, p, s);
-    else if (p.own_copies == 2) launch_few<D, 2, F16>(job, p, s);
-    else launch_few<D, 1, F16>(job, p, s);
+void launch_few(const PrefixJob& job, const SharedPart& shared, const PrefixPlan& p, hipStream_t s) {
+    if (p.own_copies == 4) launch_few<D, 4, F16>(job, shared, p, s);
+    else if (p.own_copies == 2) launch_few<D, 2, F16>(job, shared, p, s);
+    else launch_few<D, 1, F16>(job, shared, p, s);
 }
-void launch_few(const PrefixJob& job, const PrefixPlan& p, hipStream_t s) {
+// `job`: sequences by themselves, or what is behind the prefixes; `shared`: the prefixes.  Either may have no row tiles.
+void launch_few(const PrefixJob& job, const SharedPart& shared, const PrefixPlan& p, hipStream_t s) {
     const bool f16 = job.a.dtype == RQ_F16;
-    if (job.cache.head_dim == 128) f16 ? launch_few<128, true>(job, p, s) : launch_few<128, false>(job, p, s);
-    else f16 ? launch_few<64, true>(job, p, s) : launch_few<64, false>(job, p, s);
+    if (job.cache.head_dim == 128) f16 ? launch_few<128, true>(job, shared, p, s) : launch_few<128, false>(job, shared, p, s);
+    else f16 ? launch_few<64, true>(job, shared, p, s) : launch_few<64, false>(job, shared, p, s);
+}
+
+// Row tiles of BM rows that have rows of tokens begin .. end - 1, where tiles begin at floor(first row / BM) + number (find_rows, find_group_rows) for
+// `stretches` of rows; `tiles`: of all tokens.
+struct Tiles {
+    int first, end;
+};
+Tiles tiles_of_tokens(int bm, int group, int begin, int end, int stretches, int tiles) {
+    // (a row's place is that of its stretch's first one and what it lies behind it, each rounded down)
+    const int64_t first = (int64_t)begin * group / bm - 1, last = ((int64_t)end * group - 1) / bm + stretches - 1;
+    return Tiles{(int)(first > 0 ? first : 0), (int)(last + 1 < tiles ? last + 1 : tiles)};
 }
 
 }  // namespace
@@ -187,21 +206,40 @@ int kv4_prefix_attention(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x
     static_cast<KvJob&>(job) = KvJob{c, a, a.heads / c.kv_heads, p.own_tiles, 0, p.own_chunk, p.own_chunks, wide(a.q, a.q_token, a.q_head),
                                      wide(a.o, a.o_token, a.o_head), workspace};
     job.p = x;
+    if (p.separate) {
+        launch_few(job, SharedPart{}, p, s);
+        return launch_rc();
+    }
     job.part_chunks = p.shared_chunks + p.own_chunks;
     job.part_first = p.shared_chunks;
-    launch_few(job, p, s);
-    if (p.separate) return launch_rc();
-    if (p.own_many) launch_prefix_many(job, Part::kOwn, 1, s);
-    if (p.many) {
-        PrefixJob shared = job;
-        shared.tiles = p.shared_tiles;
-        shared.chunk = p.shared_chunk;
-        shared.chunks = p.shared_chunks;
-        shared.part_first = 0;
-        launch_prefix_many(shared, Part::kShared, p.groups, s);
+    const int shared_bm = p.many ? 128 : 16, own_bm = p.own_many ? 128 : 16 / p.own_copies;
+    const int own_each = (job.group + own_bm - 1) / own_bm;           // row tiles of a token that is a sequence
+    for (job.slice = 0; job.slice < a.tokens; job.slice = job.slice_end) {
+        job.slice_end = job.slice + (p.slice < a.tokens - job.slice ? p.slice : a.tokens - job.slice);
+        const Tiles own = a.q_start ? tiles_of_tokens(own_bm, job.group, job.slice, job.slice_end, a.batch, p.own_tiles)
+                                    : Tiles{job.slice * own_each, job.slice_end * own_each};
+        const Tiles prefixes = tiles_of_tokens(shared_bm, job.group, job.slice, job.slice_end, x.groups, p.shared_tiles);
+        PrefixJob part = job;
+        part.first_tile = own.first;
+        part.tiles = own.end;
+        if (p.own_many) launch_prefix_many(part, Part::kOwn, 1, s);
+        if (p.own_many) part.first_tile = part.tiles = 0;
+        launch_few(part, p.many ? SharedPart{} : SharedPart{prefixes.first, prefixes.end, p.shared_chunk, p.shared_chunks}, p, s);
+        if (p.many) {
+            part.first_tile = prefixes.first;
+            part.tiles = prefixes.end;
+            part.chunk = p.shared_chunk;
+            part.chunks = p.shared_chunks;
+            part.part_first = 0;
+            launch_prefix_many(part, Part::kShared, p.groups, s);
+        }
+        part.chunks = job.part_chunks;
+        part.first_token = job.slice;
+        part.a.tokens = job.slice_end - job.slice;
+        part.a.o = static_cast<uint16_t*>(a.o) + job.slice * a.o_token;
+        part.a.lse = a.lse ? a.lse + (int64_t)job.slice * a.heads : nullptr;
+        launch_join(part, s);
     }
-    job.chunks = job.part_chunks;
-    launch_join(job, s);
     return launch_rc();
 }
 

@@ -12,7 +12,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void k_prefix_many(PrefixJob job) 
 
 template <int D, bool F16, bool PAGED>
 void launch(const PrefixJob& job, Part part, int groups, hipStream_t s) {
-    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)job.tiles * job.chunks), block(256 * groups);
+    const dim3 grid = item_grid(job.cache.kv_heads, (int64_t)(job.tiles - job.first_tile) * job.chunks), block(256 * groups);
     if (part == Part::kOwn) {
         launch_kernel(k_prefix_many<D, 1, F16, PAGED, Part::kOwn>, grid, block, 0, s, job);
         return;

@@ -14,6 +14,7 @@ struct KvJob {
     int chunk, chunks;                            // many rows: keys of a chunk, chunks (bound)
     bool wide_q, wide_o;                          // rows of q, of o begin on 16 bytes
     float* part;                                  // workspace
+    int first_token;                              // joining chunks: what has been taken off the tokens' numbers
 };
 
 // Which positions a launch takes.  kWhole: a sequence's.  Where sequences share a prefix: kShared: the prefixes, the rows of all sequences of a
@@ -22,6 +23,8 @@ enum class Part { kWhole, kShared, kOwn, kSeparate };
 struct PrefixJob : KvJob {
     Kv4Prefix p;
     int part_first, part_chunks;                  // partial results [chunks][tokens][heads]: the launch's first, all there are
+    int first_tile;                               // row tiles of the launch: from there to `tiles`
+    int slice, slice_end;                         // tokens whose results it writes, which the partial results have
 };
 
 namespace {
@@ -308,6 +311,8 @@ struct Place {
 };
 // Row r of a tile's sequence: its token.
 __device__ __forceinline__ int token_of(const KvJob& job, const Place& p, int r) { return p.nq == 1 ? 0 : r / job.group; }
+// Whether a tile's sequence (or group of them) has tokens of the launch's.
+__device__ __forceinline__ bool in_slice(const PrefixJob& job, const Place& p) { return p.q0 + p.nq > job.slice && p.q0 < job.slice_end; }
 
 // Grid of `items` workgroups for each kv head, and a workgroup's number in it.
 inline dim3 item_grid(int kv_heads, int64_t items) {

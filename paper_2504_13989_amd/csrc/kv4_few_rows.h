@@ -361,6 +361,7 @@ __device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::
     if constexpr (CHUNKED) {
         tile = number / job.chunks;
         chunk = number - tile * job.chunks;
+        tile += job.first_tile;
     }
     if constexpr (SHARED) {
         const int each = share_out<C>(job, shares);
@@ -400,6 +401,8 @@ __device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::
         } else {
             if (!find_rows<C>(job, tile, at)) return;                // (SHARED: such a tile has no units)
         }
+        if constexpr (CHUNKED)
+            if (!in_slice(job, at)) return;
         const int rows = at.nq * job.group, n = at.base + (lane & 15) % C;
         const bool there = n < rows;
         const int token = there ? token_of(job, at, n) : 0;
@@ -562,12 +565,14 @@ __device__ __forceinline__ void few_rows(const std::conditional_t<PART == Part::
             for (int e = 0; e < per; ++e) z[e] *= by;
             const float total = top + __builtin_amdgcn_logf(sum);
             if constexpr (CHUNKED) {
-                const int token_m = token_of(job, at, at.base + mine), h = head * job.group + at.base + mine - token_m * job.group;
-                const int64_t rows_all = (int64_t)a.tokens * a.heads, part = (job.part_first + chunk) * rows_all + (int64_t)(at.q0 + token_m) * a.heads + h;
-                float* o = job.part + part * D + d;
+                const int token_m = token_of(job, at, at.base + mine), h = head * job.group + at.base + mine - token_m * job.group, t = at.q0 + token_m;
+                const int64_t rows_all = (int64_t)(job.slice_end - job.slice) * a.heads, part = (job.part_first + chunk) * rows_all + (int64_t)(t - job.slice) * a.heads + h;
+                if (t >= job.slice && t < job.slice_end) {
+                    float* o = job.part + part * D + d;
 #pragma unroll
-                for (int e = 0; e < per; ++e) o[e] = z[e];
-                if (d == 0) job.part[job.part_chunks * rows_all * D + part] = total;
+                    for (int e = 0; e < per; ++e) o[e] = z[e];
+                    if (d == 0) job.part[job.part_chunks * rows_all * D + part] = total;
+                }
             } else if (SHARED && !all) {
                 const int64_t slot = ((int64_t)(number + tile) * kv + head) * C + mine;
                 float* o = job.part + slot * D + d;

@@ -441,6 +441,8 @@ __device__ __forceinline__ void many_rows(const std::conditional_t<PART == Part:
         if (!find_rows<BM>(job, job.tiles - 1 - tile_no, at)) return;
         find_keys<BM>(job, at, a.kv_lens[at.b]);
     }
+    if constexpr (PARTS)
+        if (!in_slice(job, at)) return;
     const int rows = at.nq * job.group, row = at.base + 32 * wave;
 
     // the chunk's share of the keys that the workgroup's rows see
@@ -608,12 +610,15 @@ __device__ __forceinline__ void many_rows(const std::conditional_t<PART == Part:
     float lse = l == 0.0f ? -INFINITY : r.m + __builtin_amdgcn_logf(l);
     if constexpr (!EXACT) lse -= kUp;
     const int t_row = at.q0 + e_token, h_row = head * job.group + e_of;
-    int part_first = 0, part_chunks = job.chunks;
+    int part_first = 0, part_chunks = job.chunks, slice = 0, tokens = a.tokens;
     if constexpr (PARTS) {
         part_first = job.part_first;
         part_chunks = job.part_chunks;
+        slice = job.slice;
+        tokens = job.slice_end - slice;
+        if (t_row < slice || t_row >= job.slice_end) return;
     }
-    const int64_t part_row = ((int64_t)(part_first + chunk) * a.tokens + t_row) * a.heads + h_row;
+    const int64_t part_row = ((int64_t)(part_first + chunk) * tokens + t_row - slice) * a.heads + h_row;
     float* part = job.part + part_row * D;
     uint16_t* out = static_cast<uint16_t*>(a.o) + (int64_t)t_row * a.o_token + (int64_t)h_row * a.o_head;
     constexpr int B = D / 4 / 2;                  // fours of elements that the lane has
@@ -627,7 +632,7 @@ __device__ __forceinline__ void many_rows(const std::conditional_t<PART == Part:
         else store_row<4, F16>(out + 4 * four, y, job.wide_o);
     }
     if (e_lane < 32) {
-        if (PARTS || job.chunks > 1) job.part[(int64_t)part_chunks * a.tokens * a.heads * D + part_row] = lse;
+        if (PARTS || job.chunks > 1) job.part[(int64_t)part_chunks * tokens * a.heads * D + part_row] = lse;
         else if (a.lse) a.lse[(int64_t)t_row * a.heads + h_row] = lse * kLn2;
     }
 }

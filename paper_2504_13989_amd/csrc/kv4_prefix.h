@@ -12,6 +12,7 @@ struct PrefixPlan {
     int own_copies;                               // kernel for few rows: copies of a sequence's rows among the columns
     int shared_tiles, own_tiles;                  // row tiles at most
     int shared_chunk, shared_chunks, own_chunk, own_chunks;   // keys of a workgroup, chunks of a row tile
+    int slice;                                    // tokens that the workspace holds partial results of: those of a call are taken in turns
     size_t bytes;                                 // workspace
 };
 
