@@ -532,7 +532,14 @@ size_t rq_kv4_prefix_attention_workspace(const rq_kv4_t* cache, int64_t tokens, 
  *   group_start  [in]  DEVICE, groups + 1 int32, ascending from 0 to batch
  *   table, kv_lens, max_len   of what is behind the prefixes; max_prefix: no prefix is longer, at most prefix_width * page_size;
  *                max_prefix + max_len at most 2^30
- * Other arguments, what is rounded, and errors as rq_kv4_attention; the same call gives the same bits.
+ * Other arguments and errors as rq_kv4_attention; the same call gives the same bits.
+ * What is rounded: as in rq_kv4_attention, for prefixes and what is behind them by the kernel that takes either.  Which one does goes by the
+ * rows of a whole group, not of a sequence: bf16 results of single queries, too, come from keys, values and probabilities of the prefix
+ * rounded to fp16 each where many of them share a long one (rq_kv4_prefix_attention_plan: many; own_many: what is behind).
+ * Where it is of no use: with a window that hides positions, or with max_prefix below 64, each sequence takes its prefix and its own
+ * positions by itself, on one workgroup for each 16 of its queries x heads or fewer, however long (plan: separate).  There, and for sequences that
+ * share little of what they see, rq_kv4_attention on whole tables is as fast or faster: 16 x 32 heads behind 4096 positions, window 1024,
+ * 10.8 and 11.0 us; two sequences of 8 heads behind 65536, window 60000, 23 and 195; one of 131072 positions behind 32, 28 and 489.
  */
 int rq_kv4_prefix_attention(const rq_hadamard_t* h, const rq_kv4_t* cache, const void* Q, int dtype, int64_t tokens, int heads,
                             int64_t q_token_stride, int64_t q_head_stride, const int32_t* prefix_table, int groups, int prefix_width,
@@ -569,7 +576,9 @@ int rq_kv4_prefix_attention_plan(const rq_kv4_t* cache, int dtype, int64_t token
  *   decay        [in]  0 .. 1
  *   weights      [inout] DEVICE, element [b][y][j] at b * w_seq_stride + y * w_head_stride + j; rows of max_len must not overlap
  *   max_len      [in]  times batch, at most 2^37
- *   workspace    [in]  DEVICE, >= rq_kv4_attention_weights_workspace(...) bytes, 16-byte aligned, scratch; NULL where that is 0
+ *   workspace    [in]  DEVICE, >= rq_kv4_attention_weights_workspace(...) bytes, 16-byte aligned, scratch; NULL where that is 0 (none for single
+ *                      queries of 16 heads a kv head at most; else 4 head_dim + 16 bytes for each query and head, and 4 for each position and kv
+ *                      head in each share of the queries)
  * The same call gives the same bits.  Errors: RQ_ERR_ARG, RQ_ERR_HIP.
  */
 size_t rq_kv4_attention_weights_workspace(const rq_kv4_t* cache, int64_t tokens, int heads, int batch, int decode, int window, int64_t max_len);

@@ -401,7 +401,8 @@ def kv4_prefix_attention(h: Optional[Hadamard], cache: KV4Cache, q, prefix_table
                          max_len: Optional[int] = None, out=None, lse=None, workspace=None, stream=None):
     """rq_kv4_prefix_attention: kv4_attention for sequences that begin alike.  Sequences group_start[g] .. group_start[g + 1] - 1 (int32
     [groups + 1]) have prefix_lens[g] positions (int32 [groups]) in the pages prefix_table[g] (int32 [groups, prefix width]) in common; table
-    and kv_lens are those of what is behind them, a sequence's own."""
+    and kv_lens are those of what is behind them, a sequence's own.
+    Nothing is shared with a window that hides positions, nor of prefixes shorter than 64: kv4_attention on whole tables is faster there."""
     return (_nat or _native()).kv4_prefix_attention(_rotation(h), cache.data, cache.kv_heads, cache.head_dim, cache.page_size, q, prefix_table,
                                                     prefix_lens, group_start, table, kv_lens, q_start, scale, causal, window, max_prefix, max_len,
                                                     out, lse, workspace, stream)

@@ -105,7 +105,10 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
     const double together = split(p.many ? 0 : p.shared_tiles, p.own_many ? 0 : p.own_tiles, 4, 2, false);
     if (p.own_many) split(0, p.own_tiles, 1, 2, true);
     // One launch takes every sequence by itself where the chip has that done before the prefixes' reuse pays for joining, kJoin steps.
-    // (32 heads on 8: 4 queries x 1000 apart 11.8, together 10.6; 16 x 1000 11.4 and 11.7, x 4000 20.8 and 13.3; 160 of 3 groups x 1000 28 and 33.)
+    // (Apart and together, 25 own positions, bf16, 32 heads of 128 on 8: 2 to 16 queries x 300 10.1 and 11.4 .. 11.8, x 700 11.1 and 10.1 .. 10.6, x 1000 12.1 and
+    // 10.3 .. 10.8, x 4000 23.3 and 12.7 .. 13.8; 32 x 700 11.3 and 12.5, x 2000 16.1 and 13.4.  fp16, 16 heads of 64 in 2 groups, 100 own: 4 x 500 7.6 and 11.3,
+    // 16 x 1000 9.3 and 11.8, x 4000 17.9 and 13.7; 160 x 1000 37 and 27.  The rule errs by 1.3 at most for the former, by 2.5 .. 3.8 for 16 x 500, 4 x 1000 and
+    // 16 x 1000 of the latter, which it takes together.)
     constexpr double kJoin = 1.7;
     const int waves = few * c.kv_heads <= num_cu ? 8 : 4;
     const int64_t each = chunks_of(shared_keys, waves) + chunks_of(own_keys, waves) + kStart;
@@ -120,7 +123,8 @@ PrefixPlan plan(const Kv4& c, const Kv4Attention& a, const Kv4Prefix& x, int num
         return p;
     }
     // Partial results of as many tokens as kMostBytes hold (one at least), in turns of alike length: two chunks of 8 sequences of 4096 queries, 64
-    // heads of 128, would take 2.2 GB.  A turn has thousands of row tiles, and a tile that two turns share is all that is taken twice.
+    // heads of 128, would take 2.2 GB.  A turn has thousands of row tiles, and the tiles of a sequence or group that two turns share at their border
+    // are all that is taken twice (64 x 2048 queries of 64 heads on 8 behind 8192, bf16: 33.0 ms in 8 turns, 32.3 in one with 8.1 GB).
     const size_t token_bytes = (size_t)(p.shared_chunks + p.own_chunks) * a.heads * (c.head_dim + 1) * sizeof(float);
     const int64_t most_tokens = (int64_t)(kMostBytes / token_bytes), turns = chunks_of(a.tokens, most_tokens > 1 ? most_tokens : 1);
     p.slice = (int)chunks_of(a.tokens, turns);
